@@ -305,6 +305,89 @@ ql_status qlinear_rope_qkv(const void* q_dev, const void* k_dev, const void* v_d
 ql_status qlinear_residual_rmsnorm(const void* x_dev, const void* residual_dev, const void* gamma_dev, float eps, float gamma_offset,
                                    void* h_out_dev, void* y_out_dev, int32_t M, int32_t K, int32_t device, void* cuda_stream);
 
+/* ------------------------------------------------------------------ the operators of a serving step around the layers
+ *
+ * Angle tables of the rotary embedding (for qlinear_rope_qkv and qlinear_paged_append): for positions p = first .. first + n_pos - 1 and the
+ * rot / 2 pairs of a head
+ *     cos_dev[p - first, i] = m cos(p f_i),   sin_dev[p - first, i] = m sin(p f_i),   f_i = base^(-2 i / rot)
+ * with the angle taken in 64 bits.  `scaling` (NULL: none) stretches the frequencies for contexts longer than a model was trained on:
+ *     QL_ROPE_LINEAR   f_i / factor
+ *     QL_ROPE_NTK      base * factor^(rot / (rot - 2)) in the place of base
+ *     QL_ROPE_LLAMA3   pairs that turn `fast` times or more within `original` positions stay, those that turn `slow` times or less get f_i / factor, those
+ *                      between a mean of the two, linear in the turns (the Llama 3.1 family: factor 8, slow 1, fast 4, original 8192)
+ *     QL_ROPE_YARN     the same with a ramp over the pairs' NUMBERS, from the pair that turns `fast` times (32; rounded down) to the one that turns
+ *                      `slow` times (1; rounded up), and m = 0.1 ln(factor) + 1 (otherwise m = 1)
+ * cos_dev, sin_dev: fp32 [n_pos, rot / 2], 16-byte aligned, on `device`; rot a multiple of 16, at most 512; base > 1; factor >= 1; fast > slow > 0.
+ * Asynchronous, allocates nothing.  Errors: QL_ERR_INVALID_ARG, QL_ERR_ARCH, QL_ERR_CUDA. */
+typedef enum { QL_ROPE_NONE = 0, QL_ROPE_LINEAR = 1, QL_ROPE_NTK = 2, QL_ROPE_LLAMA3 = 3, QL_ROPE_YARN = 4 } ql_rope_kind;
+typedef struct {
+    int32_t kind, original;
+    double factor, slow, fast;
+} qlinear_rope_scaling;
+ql_status qlinear_rope_tables(float* cos_dev, float* sin_dev, int32_t first, int32_t n_pos, int32_t rot, double base, const qlinear_rope_scaling* scaling, int32_t device, void* cuda_stream);
+
+/* A paged KV cache held in 4 bits.  A pool of n_pages pages, each page_size tokens (a power of two from 16 to 1024) of h_kv heads of d_h (64, 128 or 256)
+ * elements, keys and values; 32 consecutive elements of a vector share a scale, one per token and group as in the int4 weights (Section 4.2):
+ *     s = min(fp16(max|v| / 7), 9352),   q = round-half-to-even(v / s) clamped to +-7       (IEEE fp32; a group whose scale is zero holds zeros)
+ * i.e. 0.5625 bytes an element.  Values must be finite (others give some number of the group's range).  The layout inside a page is the library's.
+ *   pool_dev   n_pages * qlinear_paged_page_bytes(desc) bytes on `device`, 256-byte aligned, owned by the caller, ZERO when the handle is made.
+ *
+ * The calls below take a BATCH: sequence b of B has the rows q_start[b] .. q_start[b + 1] - 1 of the call's T rows (its new tokens, its last ones) and
+ * kv_len[b] tokens with them; token j of it lies in page table[b * table_ld + j / page_size], j < table_width * page_size.  table, kv_len and q_start [B + 1] are int32 device
+ * memory, read by the kernels: a captured call follows what they hold when it is replayed.  Entries of the table that no visible token needs are not looked at, and
+ * those outside the pool (-1, say) give a token no place: it is not stored, reads as zero and is not attended to.  Rows of no sequence (before q_start[0], from q_start[B] on:
+ * a padded batch) are left as they are, in every output; a sequence whose rows do not lie in [0, T) has none, and no row may be two sequences'.  B <= QL_PAGED_MAX_SEQUENCES.  Two rows must not
+ * stand for one place of the pool in one append.
+ *
+ * qlinear_paged_append: row t with position p = kv_len[b] - rows + its number in the sequence (p < 0: left as a row of no sequence).  With tables (cos_dev, sin_dev fp32 [n_pos, rot / 2]; NULL: no
+ *   rotation) the first `rot` (a multiple of 16, <= d_h) elements of every query and key head are turned by the angles of row min(p, n_pos - 1), in pairs of the two
+ *   halves (interleaved 0: i with i + rot / 2) or of neighbours (1: 2i with 2i + 1):  a = x cos - y sin, b = y cos + x sin, rounded to fp16.  The key, rotated, and the value go to
+ *   the cache; the query to q_out_dev (q_dev NULL: no queries; q_out_dev may be q_dev with the same leading dimension, and must not overlap it otherwise).
+ *   k_dev, v_dev: fp16, head i of row t at t * k_ld + i * d_h; q_dev, q_out_dev: the same with h_q heads.  16-byte aligned, leading dimensions multiples of 8 (slices of one
+ *   q/k/v projection are).
+ * qlinear_paged_read: fp16(q s) of the rows' tokens, k_out_dev and v_out_dev fp16 [T, h_kv, d_h] (rows = kv_len for a whole sequence).
+ * qlinear_paged_attention: out[t, h] = sum_j softmax_j(x_j) v_j with x_j = scale q.k_j, or softcap * tanh(scale q.k_j / softcap) where softcap > 0, over the visible tokens of the
+ *   row's sequence: j <= p, j < kv_len, and p - j < window where window > 0.  Query head h reads KV head h / (h_q / h_kv).  A row that sees nothing gives zeros.  max_q: no sequence has
+ *   more rows (rows beyond it are left as they are); scores, softmax and sums in fp32, weights and values fp16.  out_dev must not overlap q_dev.
+ *   workspace_dev: qlinear_paged_attention_workspace bytes of the caller's, 16-byte aligned, overwritten; calls that may overlap need one each.
+ * Asynchronous, allocate nothing; appends must be ordered against the calls that read the same pages.
+ * Errors: QL_ERR_INVALID_ARG, QL_ERR_UNSUPPORTED (create: the descriptor), QL_ERR_CUDA, QL_ERR_DEVICE_TIMEOUT (see qlinear_forward; qlinear_paged_device_status is
+ * qlinear_device_status for this handle's device). */
+#define QL_PAGED_MAX_SEQUENCES 4096
+typedef struct qlinear_paged_s* qlinear_paged_t;
+typedef struct {
+    int32_t n_pages, page_size, h_kv, d_h;
+} qlinear_paged_desc;
+size_t qlinear_paged_page_bytes(const qlinear_paged_desc* desc);
+ql_status qlinear_paged_create(const qlinear_paged_desc* desc, void* pool_dev, int device, qlinear_paged_t* out);
+ql_status qlinear_paged_destroy(qlinear_paged_t h);
+ql_status qlinear_paged_device_status(qlinear_paged_t h, uint32_t* detail);
+ql_status qlinear_paged_append(qlinear_paged_t h, const void* q_dev, int64_t q_ld, const void* k_dev, int64_t k_ld, const void* v_dev, int64_t v_ld, void* q_out_dev, int64_t q_out_ld, int32_t h_q,
+                               const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T,
+                               const float* cos_dev, const float* sin_dev, int32_t n_pos, int32_t rot, int32_t interleaved, void* cuda_stream);
+ql_status qlinear_paged_read(qlinear_paged_t h, const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T,
+                             void* k_out_dev, void* v_out_dev, void* cuda_stream);
+size_t qlinear_paged_attention_workspace(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t max_q);
+ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q_dev, int64_t q_ld, void* out_dev, int64_t out_ld, int32_t h_q, const int32_t* table, int64_t table_ld, int32_t table_width,
+                                  const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T, int32_t max_q, float scale, float softcap, int32_t window,
+                                  void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/* Adjusts the logits of an LM head before sampling.  Row r of `rows` has the history tokens[start[r]] .. tokens[start[r + 1] - 1], its first n_prompt[r] tokens the prompt
+ * (n_prompt NULL: none), the others the output.  For every token v of the vocabulary, x = logits[r, v] in fp32:
+ *     seen in the history:               x = x > 0 ? x / repetition[r] : x * repetition[r]
+ *     n > 0 times in the output:         x = x - frequency[r] * n - presence[r]
+ *     listed in the row's biases:        x = x + bias_values[i], i the last entry of v among bias_ids[bias_start[r]] .. bias_ids[bias_start[r + 1] - 1]
+ *     bit v % 32 of mask[r, v / 32] 0:   x = -infinity (whatever the logit was, NaN too)
+ * and out[r, v] = x in the logits' type (fp16, or fp32 with is_fp32).  tokens (with start), bias_ids (with values and start) and mask may be NULL: nothing of the kind; repetition NULL: 1,
+ * presence, frequency NULL: 0.  Tokens and ids outside [0, vocab) are passed over.  logits_dev, out_dev: rows of leading dimension ld, out_ld >= vocab, any alignment; out_dev may be
+ * logits_dev with ld == out_ld, and must not overlap it otherwise.  mask int32 words, mask_ld >= ceil(vocab / 32) of them a row.  rows <= 65535.
+ * Asynchronous, allocates nothing.  Errors: QL_ERR_INVALID_ARG, QL_ERR_ARCH, QL_ERR_CUDA. */
+ql_status qlinear_adjust_logits(const void* logits_dev, int64_t ld, void* out_dev, int64_t out_ld, int32_t rows, int32_t vocab, int32_t is_fp32,
+                                const int32_t* tokens, int32_t n_tokens, const int32_t* start, const int32_t* n_prompt,
+                                const float* repetition, const float* presence, const float* frequency,
+                                const int32_t* bias_ids, const float* bias_values, const int32_t* bias_start, int32_t n_biases,
+                                const void* mask, int64_t mask_ld, int32_t device, void* cuda_stream);
+
 /* The stage qlinear_forward takes M tokens on this handle for (0 if h is NULL or M < 1). */
 int32_t qlinear_path_for(qlinear_t h, int32_t M);
 

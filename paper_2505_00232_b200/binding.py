@@ -25,6 +25,8 @@ EXPORTS = (
     "qlinear_packed_size", "qlinear_pack", "qlinear_unpack", "qlinear_create", "qlinear_forward", "qlinear_forward_group", "qlinear_forward_batch", "qlinear_forward_gated", "qlinear_forward_a8", "qlinear_quantize_activations", "qlinear_kv_append", "qlinear_kv_scores", "qlinear_kv_output", "qlinear_kv_output_uses_tmp", "qlinear_kv_append_heads", "qlinear_kv_scores_heads", "qlinear_kv_output_heads", "qlinear_embed", "qlinear_residual_rmsnorm", "qlinear_rope_qkv",
     "qlinear_path_for", "qlinear_debug_unpack_device", "qlinear_debug_expire_wait", "qlinear_debug_null_launch", "qlinear_device_status", "qlinear_decode_static", "qlinear_destroy",
     "qlinear_status_string", "qlinear_version", "qlinear_debug_plan", "qlinear_debug_plan_kv_output", "qlinear_debug_takes_batch_kernel", "qlinear_debug_kv_hold", "qlinear_debug_route", "qlinear_debug_plan_a8", "qlinear_debug_config_reads",
+    "qlinear_rope_tables", "qlinear_paged_page_bytes", "qlinear_paged_create", "qlinear_paged_destroy", "qlinear_paged_device_status", "qlinear_paged_append", "qlinear_paged_read",
+    "qlinear_paged_attention_workspace", "qlinear_paged_attention", "qlinear_adjust_logits",
 )
 
 
@@ -36,6 +38,14 @@ class QLinearError(RuntimeError):
 
 class qlinear_desc(ctypes.Structure):
     _fields_ = [("N", ctypes.c_int32), ("K", ctypes.c_int32), ("bits", ctypes.c_int32), ("group", ctypes.c_int32)]
+
+
+class qlinear_paged_desc(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("h_kv", ctypes.c_int32), ("d_h", ctypes.c_int32)]
+
+
+class qlinear_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("original", ctypes.c_int32), ("factor", ctypes.c_double), ("slow", ctypes.c_double), ("fast", ctypes.c_double)]
 
 
 def _load() -> ctypes.CDLL:
@@ -117,6 +127,22 @@ def _load() -> ctypes.CDLL:
     lib.qlinear_debug_plan_a8.restype = i32
     lib.qlinear_debug_kv_hold.restype = ctypes.c_int
     lib.qlinear_debug_config_reads.restype = ctypes.c_uint32
+    i64, f32, size = ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+    batch = [vp, i64, i32, vp, vp, i32, i32]                             # table, table_ld, table_width, kv_len, q_start, B, T
+    lib.qlinear_rope_tables.argtypes = [vp, vp, i32, i32, i32, ctypes.c_double, ctypes.POINTER(qlinear_rope_scaling), i32, vp]
+    lib.qlinear_paged_page_bytes.argtypes = [ctypes.POINTER(qlinear_paged_desc)]
+    lib.qlinear_paged_page_bytes.restype = size
+    lib.qlinear_paged_create.argtypes = [ctypes.POINTER(qlinear_paged_desc), vp, ctypes.c_int, ctypes.POINTER(vp)]
+    lib.qlinear_paged_destroy.argtypes = [vp]
+    lib.qlinear_paged_device_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
+    lib.qlinear_paged_append.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, i32, *batch, vp, vp, i32, i32, i32, vp]
+    lib.qlinear_paged_read.argtypes = [vp, *batch, vp, vp, vp]
+    lib.qlinear_paged_attention_workspace.argtypes = [vp, i32, i32, i32]
+    lib.qlinear_paged_attention_workspace.restype = size
+    lib.qlinear_paged_attention.argtypes = [vp, vp, i64, vp, i64, i32, *batch, i32, f32, f32, i32, vp, size, vp]
+    lib.qlinear_adjust_logits.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, i32, vp]
+    for f in ("qlinear_rope_tables", "qlinear_paged_create", "qlinear_paged_destroy", "qlinear_paged_device_status", "qlinear_paged_append", "qlinear_paged_read", "qlinear_paged_attention", "qlinear_adjust_logits"):
+        getattr(lib, f).restype = ctypes.c_int
     return lib
 
 
@@ -186,21 +212,23 @@ def qlinear_unpack(desc: Desc, packed: np.ndarray):
 # that is not the common form of the call (subclasses, tracing, wrong shapes, ...), and the Python below it then does the call, or raises.
 # Measured, us per call of the host: QLinear.forward at one token 6.7 -> 3.5 to 4.0 (by machine), qlinear_forward_group of three layers 14.0 -> 5.8,
 # qlinear_residual_rmsnorm 11.1 -> 4.3, qlinear_rope_qkv 15.5 -> 4.8, KVCache.output 11.0 -> 5.3.
-_half = _raw_stream = _device = _native = None
+_half = _raw_stream = _device = _native = _serving = None
 _NATIVE_API = ("qlinear_forward", "qlinear_forward_a8", "qlinear_forward_group", "qlinear_forward_gated", "qlinear_residual_rmsnorm", "qlinear_rope_qkv", "qlinear_embed",
                "qlinear_kv_append_heads", "qlinear_kv_scores_heads", "qlinear_kv_output_heads", "qlinear_kv_output", "qlinear_kv_output_uses_tmp")
+_SERVING_API = ("qlinear_paged_append", "qlinear_paged_read", "qlinear_paged_attention_workspace", "qlinear_paged_attention", "qlinear_adjust_logits")
 
 
 def _bind_torch():
     """torch is imported with the first device object, not with the package (packing needs none of it).  Returns the native module."""
-    global _half, _raw_stream, _device, _native
+    global _half, _raw_stream, _device, _native, _serving
     import torch
     if _native is None:
         from . import _native as native, build                           # (no fallback: the build makes it beside libqlinear.so)
         if native.built_for != build.installed_torch()[1]:
             raise ImportError(f"_native.so was built for {native.built_for}, not for {build.installed_torch()[1]}: run paper_2505_00232_b200/build.py")
         native.init(_check, *(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in _NATIVE_API))
-        _native = native
+        native._serving.init(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in _SERVING_API))
+        _native, _serving = native, native._serving
     # (a torch without CUDA has neither entry point: its own error comes from the calls that need a device)
     _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
@@ -399,6 +427,218 @@ def qlinear_rope_qkv(q, k, v, pos, cos, sin, B: int, S: int, h_q: int, h_kv: int
     _check(lib.qlinear_rope_qkv(p(q), p(k), p(v), p(pos), p(cos), p(sin), cos.shape[0], p(q_out), p(k_out), p(v_out), B, S, h_q, h_kv, d_h,
                                 dev, _stream_ptr(stream)), "qlinear_rope_qkv")
     return q_out, k_out, v_out
+
+
+ROPE_SCALINGS = {None: 0, "linear": 1, "ntk": 2, "llama3": 3, "yarn": 4}
+_ROPE_TURNS = {3: (1.0, 4.0), 4: (1.0, 32.0)}                            # (slow, fast) that the models with these scalings use
+
+
+def _on_stream(device, stream):
+    """(raw handle, context): the caller's stream, or the current one of the device; what is allocated in the context belongs to it."""
+    import torch
+    if stream is not None:
+        return stream.cuda_stream, torch.cuda.stream(stream)
+    if _raw_stream is None:
+        _bind_torch()
+    return _raw_stream(device.index), torch.cuda.device(device)
+
+
+def qlinear_rope_tables(n_pos: int, rot: int, base: float = 10000.0, scaling=None, factor: float = 1.0, original: int = 8192, slow=None, fast=None, first: int = 0, device=None, stream=None):
+    """(cos, sin) fp32 CUDA [n_pos, rot / 2] of the positions first .. first + n_pos - 1, with the frequency scaling of a long context (None, "linear", "ntk",
+    "llama3", "yarn"; the formulas: include/qlinear.h), for qlinear_rope_qkv and PagedKV.append."""
+    import torch
+    kind = ROPE_SCALINGS.get(scaling)
+    if kind is None or n_pos < 0 or rot < 0:
+        raise QLinearError(QL_ERR_INVALID_ARG, "qlinear_rope_tables (unknown scaling or negative size)")
+    turns = _ROPE_TURNS.get(kind, (1.0, 2.0))
+    s = qlinear_rope_scaling(kind, original, factor, turns[0] if slow is None else slow, turns[1] if fast is None else fast)
+    device = torch.device("cuda" if device is None else device)
+    if device.type != "cuda":
+        raise QLinearError(QL_ERR_INVALID_ARG, "qlinear_rope_tables (device must be a CUDA device)")
+    if device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    st, where = _on_stream(device, stream)
+    with where:
+        cos, sin = (torch.empty((n_pos, rot // 2), dtype=torch.float32, device=device) for _ in range(2))
+    _check(lib.qlinear_rope_tables(cos.data_ptr(), sin.data_ptr(), first, n_pos, rot, base, ctypes.byref(s), device.index, st), "qlinear_rope_tables")
+    return cos, sin
+
+
+def qlinear_adjust_logits(logits, tokens=None, start=None, n_prompt=None, repetition=None, presence=None, frequency=None, bias_ids=None, bias_values=None, bias_start=None, mask=None,
+                          out=None, stream=None):
+    """logits fp16 or fp32 CUDA [rows, vocab] (rows may be strided) -> the same type and shape: penalties for the tokens of every row's history
+    (tokens int32 [n], start int32 [rows + 1], n_prompt int32 [rows]; repetition, presence, frequency fp32 [rows]), biases (bias_ids int32 [m], bias_values fp32 [m], bias_start int32
+    [rows + 1]), and the mask of allowed tokens (int32 [rows, >= ceil(vocab / 32)], one bit a token).  out may be logits."""
+    y = (_serving or _bind_torch()._serving).adjust_logits(logits, tokens, start, n_prompt, repetition, presence, frequency, bias_ids, bias_values, bias_start, mask, out, _raw(stream))
+    if y is not None:
+        return y
+    import torch
+    where = "qlinear_adjust_logits"
+    def vector(t, dtype, n):
+        return t is None or (t.dtype == dtype and t.device == logits.device and t.dim() == 1 and t.is_contiguous() and (n is None or t.shape[0] == n))
+    def rows_of(t, dtype):
+        return t.dtype == dtype and t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)
+    if logits.dtype not in (torch.float16, torch.float32) or not rows_of(logits, logits.dtype):
+        raise QLinearError(QL_ERR_INVALID_ARG, where + " (logits must be fp16 or fp32 CUDA [rows, vocab])")
+    R, V = logits.shape
+    if (tokens is None) != (start is None) or not vector(tokens, torch.int32, None) or not vector(start, torch.int32, R + 1) or not vector(n_prompt, torch.int32, R) \
+            or not all(vector(t, torch.float32, R) for t in (repetition, presence, frequency)):
+        raise QLinearError(QL_ERR_INVALID_ARG, where + " (history: int32 tokens, start [rows + 1], n_prompt [rows]; fp32 penalties [rows])")
+    if len({bias_ids is None, bias_values is None, bias_start is None}) != 1 or not vector(bias_ids, torch.int32, None) \
+            or not vector(bias_values, torch.float32, None if bias_ids is None else bias_ids.shape[0]) or not vector(bias_start, torch.int32, R + 1):
+        raise QLinearError(QL_ERR_INVALID_ARG, where + " (biases: int32 ids, fp32 values, int32 start [rows + 1])")
+    if mask is not None and (not rows_of(mask, torch.int32) or mask.device != logits.device or mask.shape[0] != R or mask.shape[1] < (V + 31) // 32):
+        raise QLinearError(QL_ERR_INVALID_ARG, where + " (mask must be int32 [rows, ceil(vocab / 32)])")
+    st, here = _on_stream(logits.device, stream)
+    if out is None:
+        with here:
+            out = torch.empty((R, V), dtype=logits.dtype, device=logits.device)
+    elif not rows_of(out, logits.dtype) or tuple(out.shape) != (R, V) or out.device != logits.device:
+        raise QLinearError(QL_ERR_INVALID_ARG, where + " (bad out tensor)")
+    ptr = lambda t: None if t is None else t.data_ptr()
+    count = lambda t: 0 if t is None else t.shape[0]
+    ld = lambda t: max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+    _check(lib.qlinear_adjust_logits(ptr(logits), ld(logits), ptr(out), ld(out), R, V, int(logits.dtype == torch.float32), ptr(tokens), count(tokens), ptr(start), ptr(n_prompt),
+                                     ptr(repetition), ptr(presence), ptr(frequency), ptr(bias_ids), ptr(bias_values), ptr(bias_start), count(bias_ids),
+                                     ptr(mask), 0 if mask is None else ld(mask), logits.device.index, st), where)
+    return out
+
+
+class PagedKV:
+    """A paged KV cache held in 4 bits (qlinear_paged_* in include/qlinear.h): the pool of pages, and the calls on a batch of sequences.
+
+    A batch is (page_table int32 [B, pages], kv_len int32 [B], q_start int32 [B + 1]) on the cache's device: the rows q_start[b] .. q_start[b + 1] - 1 of a
+    call are the last tokens of sequence b, which has kv_len[b] with them.  Which pages a sequence gets is the caller's business."""
+
+    def __init__(self, n_pages: int, page_size: int, h_kv: int, d_h: int, device=None):
+        import torch
+        _bind_torch()
+        self.n_pages, self.page_size, self.h_kv, self.d_h = n_pages, page_size, h_kv, d_h
+        desc = qlinear_paged_desc(n_pages, page_size, h_kv, d_h)
+        size = int(lib.qlinear_paged_page_bytes(ctypes.byref(desc)))
+        if size == 0:
+            raise QLinearError(QL_ERR_UNSUPPORTED, "PagedKV (page_size a power of two from 16 to 1024, d_h 64, 128 or 256)")
+        self.pool = torch.zeros((n_pages, size), dtype=torch.uint8, device="cuda" if device is None else device)
+        self.device = self.pool.device
+        # (the pool's zeros are written on the current stream; calls on others come behind them)
+        torch.cuda.current_stream(self.device).synchronize()
+        h = ctypes.c_void_p()
+        _check(lib.qlinear_paged_create(ctypes.byref(desc), self.pool.data_ptr(), self.device.index, ctypes.byref(h)), "qlinear_paged_create")
+        self._h = h
+        self._native = (h.value, h_kv, d_h, self.device.index)
+
+    def _rows(self, t, heads, where):
+        """(leading dimension of t, its heads): fp16 [T, heads * d_h] or [T, heads, d_h], the elements of a row in order."""
+        d = self.d_h
+        ok = t.dtype == _half and t.device == self.device and t.dim() in (2, 3) and (t.shape[-1] == d if t.dim() == 3 else t.shape[1] % d == 0)
+        ok = ok and t.stride(-1) == 1 and (t.dim() == 2 or t.shape[1] == 1 or t.stride(1) == d)
+        n = 0 if not ok else t.shape[1] if t.dim() == 3 else t.shape[1] // d
+        if not ok or n < 1 or (heads is not None and n != heads):
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (rows must be fp16 CUDA [T, heads * d_h] or [T, heads, d_h] on the cache's device)")
+        return (max(t.stride(0), n * d) if t.shape[0] <= 1 else t.stride(0)), n
+
+    def _batch(self, page_table, kv_len, q_start, T, where):
+        import torch
+        ok = all(t.dtype == torch.int32 and t.device == self.device for t in (page_table, kv_len, q_start)) and page_table.dim() == 2
+        B, W = page_table.shape if ok else (0, 0)
+        if not ok or tuple(kv_len.shape) != (B,) or tuple(q_start.shape) != (B + 1,) or not kv_len.is_contiguous() or not q_start.is_contiguous() or (W > 1 and page_table.stride(1) != 1):
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (int32 page_table [B, pages], kv_len [B], q_start [B + 1] on the cache's device)")
+        return page_table.data_ptr() if page_table.numel() else None, max(page_table.stride(0), W) if B <= 1 else page_table.stride(0), W, kv_len.data_ptr(), q_start.data_ptr(), B, T
+
+    def append(self, k, v, page_table, kv_len, q_start, q=None, cos=None, sin=None, interleaved: bool = False, q_out=None, stream=None):
+        """Writes the keys and values of the batch's new tokens to their pages, queries and keys turned by the tables on the way; returns the turned queries, shaped like q (None without)."""
+        y = _serving.paged_append(self._native, k, v, page_table, kv_len, q_start, q, cos, sin, interleaved, q_out, _raw(stream))
+        if y is not None:
+            return y if q is not None else None
+        import torch
+        where = "qlinear_paged_append"
+        T = k.shape[0]
+        k_ld, _ = self._rows(k, self.h_kv, where)
+        v_ld, _ = self._rows(v, self.h_kv, where)
+        batch = self._batch(page_table, kv_len, q_start, T, where)
+        if v.shape[0] != T or (q is not None and q.shape[0] != T):
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (q, k and v differ in rows)")
+        rot = n_pos = 0
+        if (cos is None) != (sin is None):
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (cos and sin come together)")
+        if cos is not None:
+            if any(t.dtype != torch.float32 or t.device != self.device or t.dim() != 2 or not t.is_contiguous() for t in (cos, sin)) or cos.shape != sin.shape:
+                raise QLinearError(QL_ERR_INVALID_ARG, where + " (cos, sin must be contiguous fp32 CUDA [n_pos, rot / 2])")
+            n_pos, rot = cos.shape[0], 2 * cos.shape[1]
+        st, here = _on_stream(self.device, stream)
+        q_ld = out_ld = h_q = 0
+        if q is not None:
+            q_ld, h_q = self._rows(q, None, where)
+            if q_out is None:
+                with here:
+                    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out_ld, n = self._rows(q_out, h_q, where)
+            if q_out.shape != q.shape:
+                raise QLinearError(QL_ERR_INVALID_ARG, where + " (bad q_out tensor)")
+        elif q_out is not None:
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (q_out without q)")
+        ptr = lambda t: None if t is None else t.data_ptr()
+        _check(lib.qlinear_paged_append(self._h, ptr(q), q_ld, k.data_ptr(), k_ld, v.data_ptr(), v_ld, ptr(q_out), out_ld, h_q, *batch, ptr(cos), ptr(sin), n_pos, rot, int(bool(interleaved)), st), where)
+        return q_out
+
+    def read(self, page_table, kv_len, q_start, T: int, stream=None):
+        """(k, v) fp16 [T, h_kv, d_h]: what the cache holds of the batch's T rows (zeros where the table gives them no page)."""
+        y = _serving.paged_read(self._native, page_table, kv_len, q_start, T, _raw(stream))
+        if y is not None:
+            return y
+        import torch
+        where = "qlinear_paged_read"
+        if T < 0:
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (negative T)")
+        batch = self._batch(page_table, kv_len, q_start, T, where)
+        st, here = _on_stream(self.device, stream)
+        with here:
+            k, v = (torch.empty((T, self.h_kv, self.d_h), dtype=torch.float16, device=self.device) for _ in range(2))
+        _check(lib.qlinear_paged_read(self._h, *batch, k.data_ptr(), v.data_ptr(), st), where)
+        return k, v
+
+    def attention(self, q, page_table, kv_len, q_start, max_q: int, scale=None, softcap: float = 0.0, window: int = 0, out=None, stream=None):
+        """q fp16 [T, h_q * d_h] or [T, h_q, d_h] -> fp16 [T, h_q, d_h]: causal attention of the batch's rows over their sequences in the cache; no sequence
+        has more than max_q rows.  scale None: 1 / sqrt(d_h)."""
+        scale = self.d_h ** -0.5 if scale is None else scale
+        y = _serving.paged_attention(self._native, q, page_table, kv_len, q_start, max_q, scale, softcap, window, out, _raw(stream))
+        if y is not None:
+            return y
+        import torch
+        where = "qlinear_paged_attention"
+        q_ld, h_q = self._rows(q, None, where)
+        T = q.shape[0]
+        batch = self._batch(page_table, kv_len, q_start, T, where)
+        if h_q % self.h_kv or max_q < 0:
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (query heads a multiple of the KV heads, max_q >= 0)")
+        st, here = _on_stream(self.device, stream)
+        size = lib.qlinear_paged_attention_workspace(self._h, h_q, batch[5], max_q)
+        with here:
+            if out is None:
+                out = torch.empty((T, h_q, self.d_h), dtype=torch.float16, device=self.device)
+            work = torch.empty(size, dtype=torch.uint8, device=self.device)
+        out_ld, n = self._rows(out, h_q, where)
+        if out.shape[0] != T:
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (bad out tensor)")
+        _check(lib.qlinear_paged_attention(self._h, q.data_ptr(), q_ld, out.data_ptr(), out_ld, h_q, *batch, max_q, scale, softcap, window, work.data_ptr(), size, st), where)
+        return out
+
+    def device_status(self):
+        detail = ctypes.c_uint32(0)
+        st = lib.qlinear_paged_device_status(self._h, ctypes.byref(detail))
+        return int(st), int(detail.value)
+
+    def close(self) -> None:
+        if getattr(self, "_h", None):
+            lib.qlinear_paged_destroy(self._h)
+            self._h = None
+            self._native = (0, 0, 0, 0)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class QLinear:

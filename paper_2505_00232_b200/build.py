@@ -12,8 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqlinear.so")
 NATIVE = os.path.join(HERE, "_native.so")
 HEADER = os.path.join("..", "..", "include", "qlinear.h")
-SOURCES = ["qlinear.cu", "pack.cpp"]
-DEPS = SOURCES + ["layout.h", "dequant.cuh", "sm100_ptx.cuh", "embed.cuh", "gemv.cuh", "gemv_rows.cuh", "gemv_cols.cuh", "gemv_a8.cuh", "kv.cuh", "gemv_stream.cuh", "gemm.cuh", "gemm_mid.cuh", "gemm_rows.cuh", "gemm_pair.cuh", "gemm_pair_ta.cuh", "gemm_narrow.cuh", "norm.cuh", "rope.cuh", HEADER]
+SOURCES = ["qlinear.cu", "serving.cu", "pack.cpp"]
+DEPS = SOURCES + ["layout.h", "dequant.cuh", "sm100_ptx.cuh", "embed.cuh", "gemv.cuh", "gemv_rows.cuh", "gemv_cols.cuh", "gemv_a8.cuh", "kv.cuh", "gemv_stream.cuh", "gemm.cuh", "gemm_mid.cuh", "gemm_rows.cuh", "gemm_pair.cuh", "gemm_pair_ta.cuh", "gemm_narrow.cuh", "norm.cuh", "rope.cuh", "host.h", "paged.cuh", "paged_attention.cuh", "rope_tables.cuh", "logits.cuh", HEADER]
 
 
 def _stale(target: str, deps) -> bool:
@@ -67,7 +67,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
            "-Xcompiler", "-fPIC,-O3,-fopenmp,-falign-functions=64,-falign-loops=64", "-shared", "-cudart", "static",
-           "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES] + ["-lgomp"]
+           "-t", "0", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES] + ["-lgomp"]
     cmd[1:1] = os.environ.get("QL_EXTRA_NVCC_FLAGS", "").split()   # extra compiler flags, e.g. -DNAME for an experiment build
     if verbose:
         cmd.insert(1, "-Xptxas")

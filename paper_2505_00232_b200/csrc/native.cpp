@@ -16,6 +16,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <climits>
 
 #include "../../include/qlinear.h"
@@ -50,15 +51,20 @@ bool modes_are_on()
            at::impl::PythonTorchFunctionTLS::stack_len() > 0;
 }
 
-// The tensor of a Python object, if it is a dense contiguous CUDA tensor of the type and no subclass or wrapper of one.
-const at::Tensor* plain(PyObject* o, at::ScalarType type)
+// The tensor of a Python object, if it is a CUDA tensor of the type with strides and no subclass or wrapper of one.
+const at::Tensor* strided(PyObject* o, at::ScalarType type)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.defined() || !t.is_cuda() || t.scalar_type() != type || t.layout() != at::kStrided || !t.is_contiguous()) return nullptr;
+    if (!t.defined() || !t.is_cuda() || t.scalar_type() != type || t.layout() != at::kStrided) return nullptr;
     if (t.key_set().has_any(c10::DispatchKeySet({DispatchKey::Python, DispatchKey::FuncTorchBatched, DispatchKey::FuncTorchGradWrapper, DispatchKey::Functionalize, DispatchKey::Conjugate,
                                                  DispatchKey::Negative, DispatchKey::ZeroTensor}))) return nullptr;
     return &t;
+}
+const at::Tensor* plain(PyObject* o, at::ScalarType type)                // and contiguous
+{
+    const at::Tensor* t = strided(o, type);
+    return t && t->is_contiguous() ? t : nullptr;
 }
 bool is_matrix(const at::Tensor* t, int64_t rows, int64_t cols) { return t && t->dim() == 2 && t->size(0) == rows && t->size(1) == cols; }
 
@@ -353,19 +359,228 @@ PyObject* kv_output(PyObject*, PyObject* const* a, Py_ssize_t)           // (V l
     });
 }
 
+// ---------------------------------------------------------------------------- the operators of a serving step (the submodule _serving)
+struct ServingApi {
+    decltype(&qlinear_paged_append) append;
+    decltype(&qlinear_paged_read) read;
+    decltype(&qlinear_paged_attention_workspace) workspace;
+    decltype(&qlinear_paged_attention) attention;
+    decltype(&qlinear_adjust_logits) adjust_logits;
+} serving;
+
+bool small_int(PyObject* o, int64_t* v)                                  // a Python int from 0 to INT_MAX
+{
+    if (!PyLong_CheckExact(o)) return false;
+    *v = PyLong_AsLongLong(o);
+    if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+    return *v >= 0 && *v <= INT_MAX;
+}
+bool real(PyObject* o, float* v)
+{
+    const double d = PyFloat_AsDouble(o);
+    if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+    *v = (float)d;
+    return true;
+}
+// The rows of a matrix whose elements lie side by side; the stride of a single row is its length.
+bool matrix_rows(const at::Tensor* t, int64_t* ld)
+{
+    if (!t || t->dim() != 2 || (t->size(1) > 1 && t->stride(1) != 1)) return false;
+    *ld = t->size(0) > 1 ? t->stride(0) : std::max(t->stride(0), t->size(1));
+    return true;
+}
+
+// `_native` of PagedKV: (handle, h_kv, d_h, device)
+struct Paged { qlinear_paged_t h; int64_t h_kv, d; int device; };
+bool paged_of(PyObject* t, Paged* p)
+{
+    if (!PyTuple_CheckExact(t) || PyTuple_GET_SIZE(t) != 4) return false;
+    p->h = static_cast<qlinear_paged_t>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(t, 0)));
+    p->h_kv = PyLong_AsLongLong(PyTuple_GET_ITEM(t, 1));
+    p->d = PyLong_AsLongLong(PyTuple_GET_ITEM(t, 2));
+    p->device = (int)PyLong_AsLong(PyTuple_GET_ITEM(t, 3));
+    return p->h != nullptr;
+}
+struct Rows { const at::Tensor* t; int64_t T, ld, heads; };
+bool rows_of(PyObject* o, const Paged& p, Rows* r)                       // fp16 [T, heads * d] or [T, heads, d]
+{
+    const at::Tensor* t = r->t = strided(o, at::kHalf);
+    if (!t || t->get_device() != p.device || (t->dim() != 2 && t->dim() != 3)) return false;
+    const int64_t last = t->dim() - 1;
+    if (t->stride(last) != 1 || (last == 1 ? t->size(1) % p.d != 0 : t->size(2) != p.d || (t->size(1) > 1 && t->stride(1) != p.d))) return false;
+    r->T = t->size(0);
+    r->heads = last == 1 ? t->size(1) / p.d : t->size(1);
+    r->ld = r->T > 1 ? t->stride(0) : std::max(t->stride(0), r->heads * p.d);
+    return r->heads >= 1 && r->heads <= INT_MAX && r->T <= INT_MAX;
+}
+struct Batch { const int32_t *table, *kv_len, *q_start; int64_t ld; int32_t width, B; };
+bool batch_of(PyObject* const* a, const Paged& p, Batch* b)              // (page table, kv_len, q_start)
+{
+    const at::Tensor *t = strided(a[0], at::kInt), *n = plain(a[1], at::kInt), *s = plain(a[2], at::kInt);
+    if (!matrix_rows(t, &b->ld) || !n || !s || n->dim() != 1 || s->dim() != 1 || n->size(0) != t->size(0) || s->size(0) != t->size(0) + 1 || t->size(0) > INT_MAX || t->size(1) > INT_MAX) return false;
+    if (t->get_device() != p.device || n->get_device() != p.device || s->get_device() != p.device) return false;
+    b->table = t->numel() ? static_cast<const int32_t*>(t->data_ptr()) : nullptr;
+    b->kv_len = static_cast<const int32_t*>(n->data_ptr());
+    b->q_start = static_cast<const int32_t*>(s->data_ptr());
+    b->width = (int32_t)t->size(1);
+    b->B = (int32_t)t->size(0);
+    return true;
+}
+void* stream_on(int device) { return c10::cuda::getCurrentCUDAStream(device).stream(); }
+
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t)        // (cache, k, v, table, kv_len, q_start, q, cos, sin, interleaved, q_out, stream) -> queries, or True without any
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Rows k, v, q{}, o{};
+        Batch b;
+        if (a[11] != Py_None || !paged_of(a[0], &p) || !rows_of(a[1], p, &k) || !rows_of(a[2], p, &v) || k.heads != p.h_kv || v.heads != p.h_kv || k.T != v.T || !batch_of(a + 3, p, &b)) Py_RETURN_NONE;
+        const bool with_q = a[6] != Py_None, make = with_q && a[10] == Py_None;
+        if (with_q ? !rows_of(a[6], p, &q) || q.T != k.T : a[10] != Py_None) Py_RETURN_NONE;
+        if (with_q && !make && (!rows_of(a[10], p, &o) || !o.t->sizes().equals(q.t->sizes()))) Py_RETURN_NONE;
+        const at::Tensor *c = nullptr, *s = nullptr;
+        if ((a[7] == Py_None) != (a[8] == Py_None)) Py_RETURN_NONE;
+        if (a[7] != Py_None) {
+            c = plain(a[7], at::kFloat); s = plain(a[8], at::kFloat);
+            if (!c || !s || c->dim() != 2 || !is_matrix(s, c->size(0), c->size(1)) || c->get_device() != p.device || s->get_device() != p.device || c->size(0) > INT_MAX || c->size(1) > INT_MAX / 2) Py_RETURN_NONE;
+        }
+        const int interleaved = PyObject_IsTrue(a[9]);
+        if (interleaved < 0) return nullptr;
+        at::Tensor made;
+        const void *kp = k.t->data_ptr(), *vp = v.t->data_ptr(), *qp = with_q ? q.t->data_ptr() : nullptr;
+        const float *cp = c ? static_cast<const float*>(c->data_ptr()) : nullptr, *sp = s ? static_cast<const float*>(s->data_ptr()) : nullptr;
+        const int32_t n_pos = c ? (int32_t)c->size(0) : 0, rot = c ? (int32_t)(2 * c->size(1)) : 0;
+        void* st = stream_on(p.device);
+        if (!done([&] {
+                if (make) { made = half_like(*q.t, q.t->sizes()); o.t = &made; o.ld = q.heads * p.d; }
+                return serving.append(p.h, qp, q.ld, kp, k.ld, vp, v.ld, with_q ? o.t->data_ptr() : nullptr, o.ld, (int32_t)q.heads, b.table, b.ld, b.width, b.kv_len, b.q_start, b.B, (int32_t)k.T,
+                                      cp, sp, n_pos, rot, interleaved, st);
+            }, "qlinear_paged_append")) return nullptr;
+        if (!with_q) Py_RETURN_TRUE;
+        return make ? THPVariable_Wrap(std::move(made)) : Py_NewRef(a[10]);
+    });
+}
+
+PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t)          // (cache, table, kv_len, q_start, T, stream)
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Batch b;
+        int64_t T;
+        if (a[5] != Py_None || !paged_of(a[0], &p) || !batch_of(a + 1, p, &b) || !small_int(a[4], &T)) Py_RETURN_NONE;
+        at::Tensor k, v;
+        void* st = stream_on(p.device);
+        const at::Device device(at::kCUDA, (c10::DeviceIndex)p.device);
+        if (!done([&] {
+                k = at::detail::empty_cuda({T, p.h_kv, p.d}, at::kHalf, device, std::nullopt);
+                v = at::detail::empty_cuda({T, p.h_kv, p.d}, at::kHalf, device, std::nullopt);
+                return serving.read(p.h, b.table, b.ld, b.width, b.kv_len, b.q_start, b.B, (int32_t)T, k.data_ptr(), v.data_ptr(), st);
+            }, "qlinear_paged_read")) return nullptr;
+        PyObject* r = PyTuple_New(2);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(std::move(k)));
+        PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(std::move(v)));
+        return r;
+    });
+}
+
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t)     // (cache, q, table, kv_len, q_start, max_q, scale, softcap, window, out, stream)
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Rows q, o{};
+        Batch b;
+        int64_t max_q, window;
+        float scale, softcap;
+        if (a[10] != Py_None || !paged_of(a[0], &p) || !rows_of(a[1], p, &q) || q.heads % p.h_kv || !batch_of(a + 2, p, &b) || !small_int(a[5], &max_q) || !real(a[6], &scale) || !real(a[7], &softcap) ||
+            !small_int(a[8], &window)) Py_RETURN_NONE;
+        const bool make = a[9] == Py_None;
+        if (!make && (!rows_of(a[9], p, &o) || o.T != q.T || o.heads != q.heads)) Py_RETURN_NONE;
+        at::Tensor made, work;
+        const void* qp = q.t->data_ptr();
+        void* st = stream_on(p.device);
+        const size_t bytes = serving.workspace(p.h, (int32_t)q.heads, b.B, (int32_t)max_q);
+        if (!done([&] {
+                if (make) { made = half_like(*q.t, {q.T, q.heads, p.d}); o.t = &made; o.ld = q.heads * p.d; }
+                work = at::detail::empty_cuda({(int64_t)bytes}, at::kByte, q.t->device(), std::nullopt);
+                return serving.attention(p.h, qp, q.ld, o.t->data_ptr(), o.ld, (int32_t)q.heads, b.table, b.ld, b.width, b.kv_len, b.q_start, b.B, (int32_t)q.T, (int32_t)max_q, scale, softcap, (int32_t)window,
+                                         work.data_ptr(), bytes, st);
+            }, "qlinear_paged_attention")) return nullptr;
+        return make ? THPVariable_Wrap(std::move(made)) : Py_NewRef(a[9]);
+    });
+}
+
+// (logits, tokens, start, n_prompt, repetition, presence, frequency, bias_ids, bias_values, bias_start, mask, out, stream)
+PyObject* adjust_logits(PyObject*, PyObject* const* a, Py_ssize_t)
+{
+    return guarded([&]() -> PyObject* {
+        const at::Tensor* x = strided(a[0], at::kHalf);
+        const bool fp32 = !x;
+        if (!x) x = strided(a[0], at::kFloat);
+        int64_t ld, out_ld = 0, mask_ld = 0;
+        if (a[12] != Py_None || !matrix_rows(x, &ld) || x->size(0) > INT_MAX || x->size(1) > INT_MAX) Py_RETURN_NONE;
+        const int64_t R = x->size(0), V = x->size(1);
+        if ((a[1] == Py_None) != (a[2] == Py_None) || (a[7] == Py_None) != (a[8] == Py_None) || (a[7] == Py_None) != (a[9] == Py_None)) Py_RETURN_NONE;
+        const void* ptr[10];
+        int64_t len[10] = {};
+        static constexpr at::ScalarType type[10] = {at::kHalf, at::kInt, at::kInt, at::kInt, at::kFloat, at::kFloat, at::kFloat, at::kInt, at::kFloat, at::kInt};
+        for (int i = 1; i < 10; ++i) {
+            ptr[i] = nullptr;
+            if (a[i] == Py_None) continue;
+            const at::Tensor* t = plain(a[i], type[i]);
+            if (!t || t->dim() != 1 || t->get_device() != x->get_device() || t->size(0) > INT_MAX) Py_RETURN_NONE;
+            const int64_t want = i == 1 || i == 7 ? t->size(0) : i == 2 || i == 9 ? R + 1 : i == 8 ? len[7] : R;
+            if (t->size(0) != want) Py_RETURN_NONE;
+            ptr[i] = t->data_ptr();
+            len[i] = t->size(0);
+        }
+        const void* mask = nullptr;
+        if (a[10] != Py_None) {
+            const at::Tensor* m = strided(a[10], at::kInt);
+            if (!matrix_rows(m, &mask_ld) || m->size(0) != R || m->size(1) < (V + 31) / 32 || m->get_device() != x->get_device()) Py_RETURN_NONE;
+            mask = m->data_ptr();
+        }
+        const bool make = a[11] == Py_None;
+        at::Tensor made;
+        const at::Tensor* out = make ? &made : strided(a[11], fp32 ? at::kFloat : at::kHalf);
+        if (!make && (!matrix_rows(out, &out_ld) || out->size(0) != R || out->size(1) != V || out->get_device() != x->get_device())) Py_RETURN_NONE;
+        const int dev = x->get_device();
+        void *xp = x->data_ptr(), *st = stream_on(dev);
+        if (!done([&] {
+                if (make) { made = at::detail::empty_cuda({R, V}, fp32 ? at::kFloat : at::kHalf, x->device(), std::nullopt); out_ld = V; }
+                const auto i32 = [&](int i) { return static_cast<const int32_t*>(ptr[i]); };
+                const auto f32 = [&](int i) { return static_cast<const float*>(ptr[i]); };
+                return serving.adjust_logits(xp, ld, out->data_ptr(), out_ld, (int32_t)R, (int32_t)V, fp32, i32(1), (int32_t)len[1], i32(2), i32(3), f32(4), f32(5), f32(6), i32(7), f32(8), i32(9), (int32_t)len[7],
+                                             mask, mask_ld, dev, st);
+            }, "qlinear_adjust_logits")) return nullptr;
+        return make ? THPVariable_Wrap(std::move(made)) : Py_NewRef(a[11]);
+    });
+}
+
+template <typename A>
+PyObject* take_entry_points(A* to, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != (Py_ssize_t)(sizeof(A) / sizeof(void*))) { PyErr_SetString(PyExc_TypeError, "native.init: the entry points"); return nullptr; }
+    for (Py_ssize_t i = 0; i < n; ++i) reinterpret_cast<void**>(to)[i] = PyLong_AsVoidPtr(a[i]);
+    Py_RETURN_NONE;
+}
+PyObject* init_serving(PyObject*, PyObject* const* a, Py_ssize_t n) { return take_entry_points(&serving, a, n); }   // (addresses in the order of ServingApi)
+
 // (check, addresses of the entry points in the order of Api)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    void** to = reinterpret_cast<void**>(&api);
-    if (n != 1 + (Py_ssize_t)(sizeof(Api) / sizeof(void*))) { PyErr_SetString(PyExc_TypeError, "native.init: one check and the entry points"); return nullptr; }
-    for (Py_ssize_t i = 1; i < n; ++i) to[i - 1] = PyLong_AsVoidPtr(a[i]);
-    Py_XSETREF(check_status, Py_NewRef(a[0]));
-    Py_RETURN_NONE;
+    if (n < 1) { PyErr_SetString(PyExc_TypeError, "native.init: one check and the entry points"); return nullptr; }
+    PyObject* r = take_entry_points(&api, a + 1, n - 1);
+    if (r) Py_XSETREF(check_status, Py_NewRef(a[0]));
+    return r;
 }
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(init), FAST(forward), FAST(forward_a8), FAST(forward_group), FAST(forward_gated), FAST(residual_rmsnorm), FAST(rope_qkv), FAST(embed),
                          FAST(kv_append), FAST(kv_scores), FAST(kv_scores_one), FAST(kv_output_heads), FAST(kv_output), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef serving_methods[] = {{"init", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(init_serving)), METH_FASTCALL, nullptr}, FAST(paged_append), FAST(paged_read), FAST(paged_attention), FAST(adjust_logits),
+                                 {nullptr, nullptr, 0, nullptr}};
+PyModuleDef serving_module = {PyModuleDef_HEAD_INIT, "_native._serving", nullptr, -1, serving_methods, nullptr, nullptr, nullptr, nullptr};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -374,5 +589,8 @@ PyMODINIT_FUNC PyInit__native(void)
 {
     PyObject* m = PyModule_Create(&module);
     if (m && PyModule_AddStringConstant(m, "built_for", QL_BUILT_FOR)) Py_CLEAR(m);   // (the versions of torch and Python; see build.py)
+    PyObject* s = m ? PyModule_Create(&serving_module) : nullptr;
+    if (m && (!s || PyModule_AddObjectRef(m, "_serving", s))) Py_CLEAR(m);
+    Py_XDECREF(s);
     return m;
 }

@@ -1,5 +1,5 @@
 // C-ABI of the qlinear library: handle life cycle, stage-aware dispatch (paper Section 3.7) and the
-// launchers of the decode and prefill kernels.  Single translation unit for all device code.
+// launchers of the decode and prefill kernels.  (The operators of a serving step around the layers: serving.cu.)
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -12,6 +12,7 @@
 #include <new>
 
 #include "../../include/qlinear.h"
+#include "host.h"
 #include "layout.h"
 
 namespace ql {
@@ -289,33 +290,6 @@ GemvPlan plan_gemv(const Layout& L, int n_rb, int M, int num_sms, bool gated = f
             }
         }
     return best;
-}
-
-template <typename Kern, typename Params>
-cudaError_t launch(Kern kern, const Params& prm, dim3 grid, dim3 block, size_t smem, cudaStream_t st, int cluster, bool pdl)
-{
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attrs[2];
-    int na = 0;
-    if (cluster > 1) {
-        attrs[na].id = cudaLaunchAttributeClusterDimension;
-        attrs[na].val.clusterDim.x = cluster;
-        attrs[na].val.clusterDim.y = 1;
-        attrs[na].val.clusterDim.z = 1;
-        ++na;
-    }
-    if (pdl) {
-        attrs[na].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attrs[na].val.programmaticStreamSerializationAllowed = 1;
-        ++na;
-    }
-    cfg.attrs = attrs;
-    cfg.numAttrs = na;
-    return cudaLaunchKernelEx(&cfg, kern, prm);
 }
 
 // cudaFuncSetAttribute once per (kernel instantiation, device); `flags` is that instantiation's table.
@@ -1108,18 +1082,6 @@ __global__ void __launch_bounds__(32) expire_wait_kernel()
     if (threadIdx.x == 0) mbar_wait<true>(smem_u32(&bar), 0, abort_word, 0x9A0);   // gives up, records the code
 }
 
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-        if (prev == dev) prev = -1;
-    }
-    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
-};
-
 }  // namespace
 
 namespace {
@@ -1167,6 +1129,35 @@ inline bool device_timed_out(const qlinear_s* h)
 }
 
 }  // namespace
+
+namespace ql {
+bool pdl_enabled() { return config().pdl; }
+ql_status device_sms(int device, int* sms)
+{
+    static std::atomic<int> known[kMaxDevices];
+    if (device < 0 || device >= kMaxDevices) return QL_ERR_INVALID_ARG;
+    if ((*sms = known[device].load(std::memory_order_relaxed)) > 0) return QL_OK;
+    int n_dev = 0, major = 0;
+    if (cudaGetDeviceCount(&n_dev) != cudaSuccess) { cudaGetLastError(); return QL_ERR_CUDA; }
+    if (device >= n_dev) return QL_ERR_INVALID_ARG;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device) != cudaSuccess ||
+        cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) { cudaGetLastError(); return QL_ERR_CUDA; }
+    if (major != 10) return QL_ERR_ARCH;
+    known[device].store(*sms, std::memory_order_relaxed);
+    return QL_OK;
+}
+ql_status shared_state(int device, SharedState* out)
+{
+    ql_status st = device_sms(device, &out->sms);
+    if (st != QL_OK) return st;
+    DeviceGuard guard(device);
+    if (!guard.ok) { cudaGetLastError(); return QL_ERR_CUDA; }
+    std::lock_guard<std::mutex> lock(g_dev_mutex);
+    st = device_state_init(device, out->sms, &g_dev[device]);
+    out->status_host = g_dev[device].status_host;
+    return st;
+}
+}  // namespace ql
 
 extern "C" ql_status qlinear_create(const qlinear_desc* d, const void* packed_dev, int device, qlinear_t* out)
 {
@@ -1888,25 +1879,28 @@ extern "C" ql_status qlinear_debug_expire_wait(qlinear_t h, void* stream)
     return cudaGetLastError() == cudaSuccess ? QL_OK : QL_ERR_CUDA;
 }
 
-extern "C" ql_status qlinear_device_status(qlinear_t h, uint32_t* detail)
+ql_status ql::device_status(int device, uint32_t* detail)
 {
-    if (!h) return QL_ERR_INVALID_ARG;
-    DeviceGuard guard(h->device);
+    DeviceState& dev = g_dev[device];
+    DeviceGuard guard(device);
     if (!guard.ok) { cudaGetLastError(); return QL_ERR_CUDA; }
     unsigned int flag[2] = {0, 0};
     if (cudaDeviceSynchronize() != cudaSuccess) { cudaGetLastError(); return QL_ERR_CUDA; }
     if (cudaMemcpyFromSymbol(flag, g_device_flag, sizeof(flag)) != cudaSuccess) { cudaGetLastError(); return QL_ERR_CUDA; }
+    if (flag[0] == 0) flag[0] = *reinterpret_cast<volatile unsigned int*>(dev.status_host);   // (a kernel of serving.cu reports there only)
     if (detail) *detail = flag[0];
     if (flag[0] == 0) return QL_OK;
     // Clear the condition, and with it whatever an abandoned launch left in the shared arrival counters.
     const unsigned int zero[2] = {0, 0};
     cudaMemcpyToSymbol(g_device_flag, zero, sizeof(zero));
-    h->dev->status_host[0] = 0;
-    cudaMemset(h->dev->gemm_counters, 0, gemm_pair_counter_count(h->dev->sms) * sizeof(unsigned int));
-    if (h->dev->stream_counters) cudaMemset(h->dev->stream_counters, 0, (size_t)kStreamMaxRsb * 8 * sizeof(unsigned int));
+    dev.status_host[0] = 0;
+    cudaMemset(dev.gemm_counters, 0, gemm_pair_counter_count(dev.sms) * sizeof(unsigned int));
+    if (dev.stream_counters) cudaMemset(dev.stream_counters, 0, (size_t)kStreamMaxRsb * 8 * sizeof(unsigned int));
     cudaDeviceSynchronize();
     return QL_ERR_DEVICE_TIMEOUT;
 }
+
+extern "C" ql_status qlinear_device_status(qlinear_t h, uint32_t* detail) { return h ? device_status(h->device, detail) : QL_ERR_INVALID_ARG; }
 
 extern "C" ql_status qlinear_destroy(qlinear_t h)
 {
