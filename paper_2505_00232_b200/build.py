@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libqlinear.so")
 NATIVE = os.path.join(HERE, "_native.so")
 HEADER = os.path.join("..", "..", "include", "qlinear.h")
 SOURCES = ["qlinear.cu", "serving.cu", "pack.cpp"]
-DEPS = SOURCES + ["layout.h", "dequant.cuh", "sm100_ptx.cuh", "embed.cuh", "gemv.cuh", "gemv_rows.cuh", "gemv_cols.cuh", "gemv_a8.cuh", "kv.cuh", "gemv_stream.cuh", "gemm.cuh", "gemm_mid.cuh", "gemm_rows.cuh", "gemm_pair.cuh", "gemm_pair_ta.cuh", "gemm_narrow.cuh", "norm.cuh", "rope.cuh", "host.h", "paged.cuh", "paged_attention.cuh", "rope_tables.cuh", "logits.cuh", HEADER]
+DEPS = SOURCES + ["layout.h", "dequant.cuh", "sm100_ptx.cuh", "embed.cuh", "gemv.cuh", "gemv_rows.cuh", "gemv_cols.cuh", "gemv_a8.cuh", "kv.cuh", "gemv_stream.cuh", "gemm.cuh", "gemm_mid.cuh", "gemm_rows.cuh", "gemm_pair.cuh", "gemm_pair_ta.cuh", "gemm_narrow.cuh", "norm.cuh", "rope.cuh", "host.h", "paged.cuh", "paged_attention.cuh", "paged_tiles.cuh", "rope_tables.cuh", "logits.cuh", HEADER]
 
 
 def _stale(target: str, deps) -> bool:

@@ -25,6 +25,7 @@ namespace ql {
 
 constexpr int kAttnWarps = 8;
 constexpr int kAttnCols = 8;
+constexpr int kAttnMaxRows = 32;                                         // query rows per KV head that this kernel takes (8 at a time); more: paged_tiles.cuh
 template <int D> struct AttnRing {
     static constexpr int kBlock = paged_block_bytes(D);
     static constexpr int kStages = D == 64 ? 6 : D == 128 ? 4 : 3;
@@ -37,8 +38,8 @@ struct PagedAttnParams {
     PagedBatch batch;
     const __half* q;             // row t, head h at q + t * q_ld + h * D
     __half* out;                 // the same with out_ld
-    float* partial;              // [2 * gridDim.x][8 columns * D of o, 8 of m, 8 of l]
-    int2* parts;                 // per segment: the slot of its first part, and the last CTA that holds one
+    float* partial;              // [2 * gridDim.x][rows * D of o, rows of m, rows of l]; slot 0 of a CTA: the part that its span begins with
+    int4* split;                 // per CTA: sequence (-1: none), KV head, row block of the segment that begins in its span and ends in another's, and 2 * (the last CTA that holds a part) + (the first part's slot)
     int64_t q_ld, out_ld;
     int32_t h_q, group, max_q, row_blocks, window;
     float scale, softcap;        // (softcap 0: none)
@@ -129,6 +130,14 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
     const int64_t w0 = (int64_t)blockIdx.x * span, w1 = min(total, w0 + span);
     uint8_t* ring = smem + warp * (S * kBlock);
     const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
+    if (tid == 0) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    for (int b = blockIdx.x; b < p.batch.B; b += p.grid) {               // rows of sequences that see nothing: zeros
+        int t0;
+        const int rows = min(paged_rows(p.batch, b, &t0), p.max_q);
+        if (pre[b + 1] > pre[b]) continue;
+        for (int64_t e = tid; e < (int64_t)rows * p.h_q * (D / 8); e += kAttnWarps * 32)
+            *reinterpret_cast<uint4*>(p.out + (t0 + e / (p.h_q * (D / 8))) * p.out_ld + 8 * (e % (p.h_q * (D / 8)))) = make_uint4(0, 0, 0, 0);
+    }
 
     for (int64_t w = w0; w < w1;) {
         // the segment (sequence, KV head, 8 rows) and the part [ua, ub) of its blocks
@@ -332,7 +341,6 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
         }
         __syncthreads();
         const bool whole = ua == 0 && ub == blocks;
-        const int64_t segment = (int64_t)b * segs + seg;
         float* part = p.partial + (int64_t)(2 * blockIdx.x + (w == w0 ? 0 : 1)) * (kAttnCols * (D + 2));
         for (int e = tid * 4; e < kAttnCols * D; e += kAttnWarps * 32 * 4) {
             const int col = e / D, d = e - col * D, r = r0 + col;
@@ -356,52 +364,43 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
                 *reinterpret_cast<uint2*>(p.out + (int64_t)(t0 + i) * p.out_ld + (int64_t)(head * p.group + r - i * p.group) * D + d) = *reinterpret_cast<const uint2*>(y);
             }
         }
-        if (tid == 0 && ua == 0) {
-            const int64_t end = w + blocks - 1;
-            p.parts[segment] = make_int2(2 * blockIdx.x + (w == w0 ? 0 : 1), (int)(end / span));
-        }
+        if (tid == 0 && ua == 0 && !whole) p.split[blockIdx.x] = make_int4(b, head, seg - head * p.row_blocks, 2 * (int)((w + blocks - 1) / span) + (w == w0 ? 0 : 1));
         w += ub - ua;
         __syncthreads();                                                 // (the ring is free again)
     }
 }
 
-// Joins the parts of the segments that more than one CTA held, in order, and writes zeros where a sequence has nothing to see.  One warp per
-// column.
-template <int D>
-__global__ void __launch_bounds__(kAttnWarps * 32) paged_combine_kernel(const PagedAttnParams p)
+// Joins the parts of the segment that begins in a CTA's span and ends in another's, in order: CTA blockIdx.x's, rows 8 blockIdx.y and so on, a warp per row.
+template <int D, int ROWS>
+__global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnParams p)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int V = D / 32;                                            // values of a lane
-    const int segs = p.batch.h_kv * p.row_blocks, b = blockIdx.x / segs, seg = blockIdx.x - b * segs;
-    const int head = seg / p.row_blocks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = (seg - head * p.row_blocks) * kAttnCols + warp;
-    int first, t0;
-    const int n_rows = min(paged_rows(p.batch, b, &t0), p.max_q) * p.group;
-    if (r >= n_rows) return;
-    float acc[V], l = 0.f;
+    constexpr int64_t kStride = ROWS * (D + 2);
+    const int4 split = p.split[blockIdx.x];
+    if (split.x < 0) return;
+    const int row = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, r = split.z * ROWS + row, c0 = blockIdx.x, c1 = split.w >> 1, slot = split.w & 1;
+    int t0;
+    if (r >= min(paged_rows(p.batch, split.x, &t0), p.max_q) * p.group) return;
+    float m = -1e30f, l = 0.f, acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
-    if (attn_blocks(p, b, &first) > 0) {
-        const int2 parts = p.parts[blockIdx.x];
-        const int c0 = parts.x >> 1;
-        if (c0 == parts.y) return;
-        // (slot 0 of a CTA: the part that its span begins with; the parts behind a segment's first are all such)
-        const int64_t stride = kAttnCols * (D + 2);
-        float m = -1e30f;
-        for (int c = c0 + lane; c <= parts.y; c += 32) m = fmaxf(m, p.partial[(c == c0 ? parts.x : 2 * c) * stride + kAttnCols * D + warp]);
+    const auto part_of = [&](int c) { return p.partial + (2 * c + (c == c0 ? slot : 0)) * kStride; };
+    for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, part_of(c)[ROWS * D + row]);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        for (int c = c0; c <= parts.y; ++c) {
-            const float* part = p.partial + (c == c0 ? parts.x : 2 * c) * stride;
-            const float f = exp2_fast(part[kAttnCols * D + warp] - m);
-            l += part[kAttnCols * D + kAttnCols + warp] * f;
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll 4
+    for (int c = c0; c <= c1; ++c) {
+        const float* part = part_of(c);
+        const float f = exp2_fast(part[ROWS * D + row] - m);
+        l += part[ROWS * D + ROWS + row] * f;
 #pragma unroll
-            for (int e = 0; e < V; ++e) acc[e] = fmaf(part[warp * D + V * lane + e], f, acc[e]);
-        }
+        for (int e = 0; e < V; ++e) acc[e] = fmaf(part[row * D + V * lane + e], f, acc[e]);
     }
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
     const int i = r / p.group;
-    __half* to = p.out + (int64_t)(t0 + i) * p.out_ld + (int64_t)(head * p.group + r - i * p.group) * D + V * lane;
+    __half* to = p.out + (int64_t)(t0 + i) * p.out_ld + (int64_t)(split.y * p.group + r - i * p.group) * D + V * lane;
 #pragma unroll
     for (int e = 0; e < V; e += 2) *reinterpret_cast<__half2*>(to + e) = __floats2half2_rn(acc[e] * inv, acc[e + 1] * inv);
 }

@@ -1,0 +1,564 @@
+// Attention of many query rows over the paged 4-bit cache of paged.cuh (prompts, chunks of them): the same operator as paged_attention.cuh, with the
+// products on the 5th-generation tensor cores.
+//
+// A CTA works on a segment: 256 query rows (row = token * group + head of the group; 128 rows at d_h 256) of one KV head, and steps through the keys that any of
+// them sees, 128 (64) at a time.  Per step and tile of 128 rows:
+//     S = Q K^T      tcgen05.mma, both operands in shared memory, S in tensor memory (fp32)
+//     P = exp2(S c - m) as fp16, written over S in tensor memory by the softmax warps, a thread per row
+//     O += P V       tcgen05.mma with P from tensor memory, O in tensor memory (fp32)
+// so the scores never leave the SM and no thread needs another's row.  The maximum m of a row is raised, and O rescaled, only when it is passed by 2^8; O is
+// free for that when S is complete (the products of a CTA are complete in order).  Keys and values are unpacked from the cache's integers by warps of their own
+// to fp16(q s), which go to shared memory in the operands' swizzled layout: K as rows of elements, V as rows of elements too, read transposed.
+//
+// Warps 0-3, 4-7: softmax of the two tiles (at d_h 256 one tile of 128 rows with two buffers of S, and warps 4-7 unpack as well); warps 8-11: unpack;
+// warp 12: issues the products.  The two tiles alternate: while one's softmax runs, the tensor core has the other's products.
+//
+// Work: the (segment, step) pairs of the whole batch, numbered through, in one span of equal length per CTA, as in paged_attention.cuh; a segment cut by a span's end
+// leaves its rows' (m, l, O) in the workspace for paged_combine_kernel.
+#pragma once
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "dequant.cuh"
+#include "paged.cuh"
+#include "paged_attention.cuh"
+#include "sm100_ptx.cuh"
+
+namespace ql {
+
+template <int D> struct TileShape {
+    static constexpr int NT = D == 256 ? 1 : 2;                          // tiles of 128 rows
+    static constexpr int N = D == 256 ? 64 : 128;                        // keys of a step
+    static constexpr int NB = D / 64;                                    // panels of 64 elements
+    static constexpr int kRows = 128 * NT;
+    static constexpr int kBlocks = N / kPagedBlock;                      // blocks of 16 tokens of a step
+    static constexpr int kUnpackWarps = NT == 2 ? 4 : 8;
+    static constexpr int kItems = kBlocks * NB / kUnpackWarps;           // (block, panel) pairs of a warp and step
+    static constexpr int kPanelQ = 128 * 128, kPanelKV = N * 128;        // bytes
+    static constexpr int kQ = NT * NB * kPanelQ, kStage = NB * kPanelKV;
+    static constexpr int kMaxSegments = 64;                              // of a CTA between two meetings
+    static constexpr int kOffQ = 0, kOffK = kQ, kOffV = kOffK + 2 * kStage, kOffPre = kOffV + 2 * kStage;
+    static constexpr uint32_t kO = NT == 2 ? 256 : 0, kS = NT == 2 ? 0 : 256;             // columns of tensor memory
+};
+constexpr int kTileThreads = 512;
+
+struct TileSegment {
+    int32_t head, row0, n_rows, t0, pos0, end, step0, n, slot;           // rows of the sequence row0 .. (n_rows of it), row 0's token and position, keys [.., end), steps step0 .. + n
+    int64_t table;                                                       // (offset of the sequence's row of the page table)
+};
+
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* r)
+{
+    // the load and its wait form one statement so that no use of r[] can be scheduled between them
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+                 "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]),
+                   "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]),
+                   "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31]), "=f"(r[32]), "=f"(r[33]), "=f"(r[34]), "=f"(r[35]),
+                   "=f"(r[36]), "=f"(r[37]), "=f"(r[38]), "=f"(r[39]), "=f"(r[40]), "=f"(r[41]), "=f"(r[42]), "=f"(r[43]), "=f"(r[44]), "=f"(r[45]), "=f"(r[46]), "=f"(r[47]),
+                   "=f"(r[48]), "=f"(r[49]), "=f"(r[50]), "=f"(r[51]), "=f"(r[52]), "=f"(r[53]), "=f"(r[54]), "=f"(r[55]), "=f"(r[56]), "=f"(r[57]), "=f"(r[58]), "=f"(r[59]),
+                   "=f"(r[60]), "=f"(r[61]), "=f"(r[62]), "=f"(r[63])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const uint32_t r[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// A wait of a whole warp: its lanes agree on the outcome (what follows is warp-collective).
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t code) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, code)); }
+template <int R> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
+template <int R> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+
+// Steps of N keys that the rows [row0, row0 + kRows) of a sequence see: *first the first of them.  rows_all rows of len tokens, n_rows (times group) of them served.
+template <int N, int kRows>
+__device__ __forceinline__ int tile_steps(int row0, int n_rows, int rows_all, int len, int held, int group, int window, int* first)
+{
+    const int pos0 = len - rows_all, i0 = row0 / group, i1 = (min(row0 + kRows, n_rows) - 1) / group;
+    const int end = min(min(pos0 + i1 + 1, len), held);
+    *first = 0;
+    if (row0 >= n_rows || end <= 0) return 0;
+    if (window > 0) *first = (int)max((int64_t)pos0 + i0 + 1 - window, (int64_t)0) / N;
+    return max(0, (end + N - 1) / N - *first);
+}
+
+template <int D, bool CAP>
+__global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const PagedAttnParams p)
+{
+    using T = TileShape<D>;
+    constexpr int NT = T::NT, N = T::N, NB = T::NB;
+    extern __shared__ __align__(128) uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    int* pre = reinterpret_cast<int*>(smem + T::kOffPre);                // [B + 1]: steps (of all row tiles, per head) before sequence b
+    __shared__ __align__(8) uint64_t bars[17];
+    __shared__ TileSegment segs[T::kMaxSegments];
+    __shared__ int n_segs;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile uint32_t abort_flag[4];
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, c = lane & 3;
+    const uint32_t bar0 = smem_u32(bars);
+    // barriers: K, V full and empty (two stages), S, P and O per buffer, Q per tile, the end
+    const auto kf = [&](int s) { return bar0 + 8 * s; };
+    const auto ke = [&](int s) { return bar0 + 8 * (2 + s); };
+    const auto vf = [&](int s) { return bar0 + 8 * (4 + s); };
+    const auto ve = [&](int s) { return bar0 + 8 * (6 + s); };
+    const auto sf = [&](int s) { return bar0 + 8 * (8 + s); };
+    const auto pf = [&](int s) { return bar0 + 8 * (10 + s); };
+    const auto of = [&](int s) { return bar0 + 8 * (12 + s); };
+    const auto qf = [&](int t) { return bar0 + 8 * (14 + t); };
+    const uint32_t done = bar0 + 8 * 16;
+    const uint32_t sbase = smem_u32(smem);
+    if (tid == 0) {
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(kf(s), T::kUnpackWarps); mbar_init(vf(s), T::kUnpackWarps);
+            mbar_init(ke(s), 1); mbar_init(ve(s), 1);
+            mbar_init(sf(s), 1); mbar_init(pf(s), 4);
+            mbar_init(of(s), 1); mbar_init(qf(s), 4);
+        }
+        mbar_init(done, 1);
+        abort_flag[0] = abort_flag[1] = abort_flag[2] = abort_flag[3] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 12) tmem_alloc(smem_u32(&tmem_slot), 512);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (tid == 0) abort_flag[2] = abort_flag[3] = 1;                     // (from here on, waiting counts against the time limit)
+
+    const PagedBatch& bt = p.batch;
+    const int held = (int)min((int64_t)bt.table_width << (bt.log2_blocks + 4), (int64_t)INT32_MAX);
+    // ---- the plan: steps per sequence, their sums
+    for (int b = warp; b < bt.B; b += kTileThreads / 32) {
+        int t0, first, sum = 0;
+        const int rows_all = paged_rows(bt, b, &t0), n_rows = min(rows_all, p.max_q) * p.group, len = bt.kv_len[b];
+        for (int r = lane; r * T::kRows < n_rows; r += 32) sum += tile_steps<N, T::kRows>(r * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &first);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) pre[b + 1] = sum;
+    }
+    if (tid == 0) pre[0] = 0;
+    __syncthreads();
+    if (warp == 0) {
+        int carry = 0;
+        for (int b0 = 0; b0 < bt.B; b0 += 32) {
+            int v = b0 + lane < bt.B ? pre[b0 + lane + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v += u;
+            }
+            v += carry;
+            if (b0 + lane < bt.B) pre[b0 + lane + 1] = v;
+            carry = __shfl_sync(0xffffffffu, v, 31);
+        }
+    }
+    // rows of row tiles that see nothing at all: zeros (there are none unless the first or the last row tile is one)
+    for (int b = blockIdx.x; b < bt.B; b += gridDim.x) {
+        int t0, first;
+        const int rows_all = paged_rows(bt, b, &t0), n_rows = min(rows_all, p.max_q) * p.group, len = bt.kv_len[b];
+        if (n_rows <= 0) continue;
+        const auto steps = [&](int row) { return tile_steps<N, T::kRows>(row / T::kRows * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &first); };
+        if (steps(0) > 0 && steps(n_rows - 1) > 0) continue;
+        for (int64_t e = tid; e < (int64_t)n_rows * bt.h_kv * (D / 8); e += kTileThreads) {
+            const int m = (int)(e % (D / 8)), row = (int)(e / (D / 8) % n_rows), head = (int)(e / (D / 8) / n_rows), i = row / p.group;
+            if (steps(row) == 0) *reinterpret_cast<uint4*>(p.out + (int64_t)(t0 + i) * p.out_ld + (int64_t)(head * p.group + row - i * p.group) * D + 8 * m) = make_uint4(0, 0, 0, 0);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
+    const int64_t total = (int64_t)pre[bt.B] * bt.h_kv, span = max((total + p.grid - 1) / p.grid, (int64_t)1);
+    const int64_t w_first = (int64_t)blockIdx.x * span, w_end = min(total, w_first + span);
+    if (tid == 12 * 32) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+
+    // Rounds of at most kMaxSegments segments; every role has a loop of its own (its share of the registers).
+    struct Round { int64_t w; uint32_t it0, seg0, steps; int n; bool on; } rd{w_first, 0, 0, 0, 0, w_first < w_end};
+    const auto begin_round = [&]() {                                     // (the list is complete)
+        __syncwarp();
+        __syncthreads();
+        rd.n = n_segs;
+        rd.steps = 0;
+        for (int s = 0; s < rd.n; ++s) rd.steps += segs[s].n;
+    };
+    const auto end_round = [&]() {
+        __syncwarp();
+        __syncthreads();
+        rd.w += rd.steps;
+        rd.it0 += rd.steps;                                              // steps and segments before the next round
+        rd.seg0 += rd.n;
+        rd.on = rd.w < w_end && !abort_flag[0];
+        __syncthreads();                                                 // (the list may be written again)
+    };
+    if (warp < 4 * NT) {
+        more_registers<192>();
+        while (rd.on) {
+        begin_round();
+            // ================================================================ softmax: thread = row
+            const int t = NT == 2 ? warp >> 2 : 0, wq = warp & 3, in_tile = 32 * wq + lane;
+            const uint32_t lanes = (uint32_t)(32 * wq) << 16, to = tmem + lanes + T::kO + D * t;
+            constexpr float kLog2e = 1.4426950408889634f;
+            const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * kLog2e, 1e-30f);   // (never 0: hidden scores are -infinity)
+            const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
+            const auto load_q = [&](const TileSegment& s) {              // this tile's rows, 16 lanes per row of 128 elements
+                constexpr int kChunks = D / 8;
+#pragma unroll 4
+                for (int e = in_tile; e < 128 * kChunks; e += 128) {
+                    const int row = e / kChunks, ch = e - row * kChunks, rr = s.row0 + 128 * t + row;
+                    uint4 u = make_uint4(0, 0, 0, 0);
+                    if (rr < s.n_rows) {
+                        const int i = rr / p.group;
+                        u = *reinterpret_cast<const uint4*>(p.q + (int64_t)(s.t0 + i) * p.q_ld + (int64_t)(s.head * p.group + rr - i * p.group) * D + 8 * ch);
+                        u.x ^= sign; u.y ^= sign; u.z ^= sign; u.w ^= sign;
+                    }
+                    *reinterpret_cast<uint4*>(smem + T::kOffQ + (t * NB + (ch >> 3)) * T::kPanelQ + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = u;
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(qf(t));
+            };
+            load_q(segs[0]);
+            uint32_t it = rd.it0;
+            bool ok = true;
+            for (int si = 0; si < rd.n && ok; ++si) {
+                const TileSegment s = segs[si];
+                const int rr = s.row0 + 128 * t + in_tile, i = rr / p.group, pos = s.pos0 + i;
+                const int last = rr < s.n_rows ? min(pos, s.end - 1) : -1, lowest = p.window > 0 ? pos - p.window : -1;
+                float m = -1e30f, l[4] = {0.f, 0.f, 0.f, 0.f};
+                const int32_t* table = bt.table + s.table;
+                const auto page_of = [&](int step) {                     // (lane: the page of the block `lane` from that step on)
+                    const int at = (step * T::kBlocks + lane) >> bt.log2_blocks;
+                    return at < bt.table_width ? table[at] : -1;
+                };
+                constexpr int kAhead = 32 / T::kBlocks;                  // steps of one look-up
+                int pg = page_of(s.step0);
+                uint32_t held_blocks = 0;
+                for (int j = 0; j < s.n; ++j, ++it) {
+                    if (j % kAhead == 0) {
+                        held_blocks = __ballot_sync(0xffffffffu, pg >= 0 && pg < bt.n_pages);
+                        pg = page_of(s.step0 + j + kAhead);
+                    }
+                    const uint32_t blocks = (held_blocks >> (T::kBlocks * (j % kAhead))) & ((1u << T::kBlocks) - 1);
+                    const int slot = NT == 2 ? t : it & 1;
+                    if (!warp_wait(sf(slot), NT == 2 ? it & 1 : (it >> 1) & 1, abort_flag, 0xA00 + slot)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t ts = tmem + lanes + T::kS + N * slot;
+                    float x[N];
+#pragma unroll
+                    for (int e = 0; e < N; e += 64) tmem_ld64(ts + e, x + e);
+                    if (CAP) {
+#pragma unroll
+                        for (int e = 0; e < N; ++e) x[e] = attn_score<true>(x[e], mag, p.softcap);
+                    }
+                    const int hi = last - (s.step0 + j) * N, lo = lowest - (s.step0 + j) * N;
+                    if (__any_sync(0xffffffffu, hi < N - 1 || lo >= 0) || blocks != (1u << T::kBlocks) - 1) {
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            if (e > hi || e <= lo || !(blocks >> (e >> 4) & 1)) x[e] = -INFINITY;
+                    }
+                    float mx[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                    for (int e = 4; e < N; e += 4) {
+                        mx[0] = fmaxf(mx[0], x[e]); mx[1] = fmaxf(mx[1], x[e + 1]);
+                        mx[2] = fmaxf(mx[2], x[e + 2]); mx[3] = fmaxf(mx[3], x[e + 3]);
+                    }
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * cc;
+                    if (__any_sync(0xffffffffu, top > m + 8.f)) {        // the maximum is raised, and with it the scale of the sums
+                        const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
+                        m = mn;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) l[e] *= f;
+                        if (j > 0) {
+                            if (NT == 1) {                               // (S of this step may be complete before the values of the one before)
+                                if (!warp_wait(of((it - 1) & 1), ((it - 1) >> 1) & 1, abort_flag, 0xA10)) { ok = false; break; }
+                                tc_fence_after();
+                            }
+#pragma unroll 1
+                            for (int d = 0; d < D; d += 16) {
+                                uint32_t o[16];
+                                tmem_ld16(to + d, o);
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st16_async(to + d, o);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < N; e += 32) {
+                        uint32_t h[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const float a = exp2_fast(fmaf(x[e + 2 * k], cc, -m)), b = exp2_fast(fmaf(x[e + 2 * k + 1], cc, -m));
+                            l[2 * (k & 1)] += a;
+                            l[2 * (k & 1) + 1] += b;
+                            const __half2 ab = __floats2half2_rn(a, b);
+                            h[k] = *reinterpret_cast<const uint32_t*>(&ab);
+                        }
+                        tmem_st16_async(ts + e / 2, h);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(pf(slot));
+                }
+                if (!ok) break;
+                if (si + 1 < rd.n) load_q(segs[si + 1]);                    // (every product with this segment's queries is complete)
+                if (!warp_wait(of(NT == 2 ? t : (it - 1) & 1), NT == 2 ? (it - 1) & 1 : ((it - 1) >> 1) & 1, abort_flag, 0xA20 + t)) { ok = false; break; }
+                tc_fence_after();
+                const float sum = (l[0] + l[1]) + (l[2] + l[3]);
+                if (s.slot < 0) {
+                    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                    __half* dst = p.out + (int64_t)(s.t0 + i) * p.out_ld + (int64_t)(s.head * p.group + rr - i * p.group) * D;
+#pragma unroll 1
+                    for (int d = 0; d < D; d += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(to + d, o);
+                        uint32_t h[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const __half2 y = __floats2half2_rn(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
+                            h[e] = *reinterpret_cast<const uint32_t*>(&y);
+                        }
+                        if (rr < s.n_rows) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(dst + d + 8 * e) = make_uint4(h[4 * e], h[4 * e + 1], h[4 * e + 2], h[4 * e + 3]);
+                        }
+                    }
+                } else {
+                    float* part = p.partial + (int64_t)(2 * blockIdx.x + s.slot) * (T::kRows * (D + 2));
+                    const int row = 128 * t + in_tile;
+#pragma unroll 1
+                    for (int d = 0; d < D; d += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(to + d, o);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4*>(part + row * D + d + 4 * e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    }
+                    part[T::kRows * D + row] = m;
+                    part[T::kRows * D + T::kRows + row] = sum;
+                }
+                tc_fence_before();
+            }
+        end_round();
+        }
+    } else if (warp < 12) {
+        fewer_registers<88>();
+        while (rd.on) {
+        begin_round();
+            // ================================================================ unpack: K and V of every step to shared memory
+            const int uw = warp - 4 * NT;
+            // this warp's (block, panel) pairs: pair kItems * uw + i, panels innermost
+            uint4 kw[T::kItems], vw[T::kItems];
+            uint2 ks[T::kItems], vs[T::kItems];
+            int si_l = 0, j_l = 0;                                       // the step whose integers are requested next
+            int si_p = 0, j_p = 0, pg = -1;                              // the step whose pages are looked up next; the pages of the one before (lane: block)
+            const auto next = [&](int& si, int& j) { if (++j == segs[si].n) { j = 0; ++si; } };
+            const auto look_up = [&]() {
+                if (si_p >= rd.n) return;
+                const int at = ((segs[si_p].step0 + j_p) * T::kBlocks + (lane & (T::kBlocks - 1))) >> bt.log2_blocks;
+                const int v = at < bt.table_width ? bt.table[segs[si_p].table + at] : -1;
+                pg = v >= 0 && v < bt.n_pages ? v : 0;                   // (scores of blocks without a page are hidden: any page will do)
+                next(si_p, j_p);
+            };
+            const auto block_of = [&](int i, int step, int head) {
+                const int blk = (T::kItems * uw + i) / NB, u = step * T::kBlocks + blk;
+                const int page = __shfl_sync(0xffffffffu, pg, blk);
+                return bt.pool + ((((int64_t)page * bt.h_kv + head) << bt.log2_blocks) + (u & ((1 << bt.log2_blocks) - 1))) * paged_block_bytes(D);
+            };
+            const uint8_t* src[T::kItems];
+            const auto request_k = [&]() {
+#pragma unroll
+                for (int i = 0; i < T::kItems; ++i) {
+                    const int pn = (T::kItems * uw + i) % NB;
+                    src[i] = block_of(i, segs[si_l].step0 + j_l, segs[si_l].head);
+                    kw[i] = *reinterpret_cast<const uint4*>(src[i] + 512 * pn + 16 * lane);
+                    ks[i] = *reinterpret_cast<const uint2*>(src[i] + paged_k_scales(D) + g * (8 * NB) + 8 * pn);
+                }
+            };
+            const auto request_v = [&]() {
+#pragma unroll
+                for (int i = 0; i < T::kItems; ++i) {
+                    const int pn = (T::kItems * uw + i) % NB;
+                    vw[i] = *reinterpret_cast<const uint4*>(src[i] + paged_v_data(D) + 512 * pn + 16 * lane);
+                    vs[i] = *reinterpret_cast<const uint2*>(src[i] + paged_v_scales(D) + (2 * pn + (g >> 2)) * 32 + 8 * c);
+                }
+            };
+            const auto put = [&](uint8_t* row, int chunk, uint32_t word, uint32_t scale) {
+                uint32_t h[4];
+                unpack_int4_word(word, h);
+                *reinterpret_cast<uint4*>(row + chunk * 16) = make_uint4(h2_mul(h[0], scale), h2_mul(h[1], scale), h2_mul(h[2], scale), h2_mul(h[3], scale));
+            };
+            look_up();
+            request_k();
+            request_v();
+            look_up();
+            next(si_l, j_l);
+            for (uint32_t q = 0; q < rd.steps; ++q) {
+                const uint32_t it = rd.it0 + q, st = it & 1, par = ((it >> 1) & 1) ^ 1;
+                if (!warp_wait(ke(st), par, abort_flag, 0xA30 + st)) break;
+#pragma unroll
+                for (int i = 0; i < T::kItems; ++i) {
+                    const int item = T::kItems * uw + i, blk = item / NB, pn = item % NB;
+                    uint8_t* panel = smem + T::kOffK + st * T::kStage + pn * T::kPanelKV + (16 * blk + g) * 128;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {                        // (the group by the row's parity: 8 lanes of a store have 8 chunks)
+                        const bool second = (k ^ g) & 1;
+                        const uint32_t sc = second ? ks[i].y : ks[i].x;
+                        const int chunk = ((second ? 4 : 0) + c) ^ g;
+                        put(panel, chunk, second ? kw[i].y : kw[i].x, __byte_perm(sc, sc, 0x1010));
+                        put(panel + 8 * 128, chunk, second ? kw[i].w : kw[i].z, __byte_perm(sc, sc, 0x3232));
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(kf(st));
+                const bool more = q + 1 < rd.steps;
+                if (more) request_k();
+                if (!warp_wait(ve(st), par, abort_flag, 0xA40 + st)) break;
+#pragma unroll
+                for (int i = 0; i < T::kItems; ++i) {
+                    const int item = T::kItems * uw + i, blk = item / NB, pn = item % NB;
+                    uint8_t* panel = smem + T::kOffV + st * T::kStage + pn * T::kPanelKV;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int row = 2 * c + (k & 1) + 8 * (k >> 1);
+                        const uint32_t sc = k & 2 ? vs[i].y : vs[i].x, word = k == 0 ? vw[i].x : k == 1 ? vw[i].y : k == 2 ? vw[i].z : vw[i].w;
+                        put(panel + (16 * blk + row) * 128, g ^ (row & 7), word, __byte_perm(sc, sc, k & 1 ? 0x3232 : 0x1010));
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(vf(st));
+                if (more) {
+                    request_v();
+                    look_up();
+                    next(si_l, j_l);
+                }
+            }
+        end_round();
+        }
+    } else {
+        fewer_registers<40>();                                           // (one instruction for the four warps)
+        while (rd.on && warp == 12) {
+        // ---- the next segments: (sequence, row tile, KV head), and the part of the steps that lies in the span
+        {
+            int n = 0;
+            int64_t ww = rd.w;
+            while (ww < w_end && n < T::kMaxSegments) {
+                int lo = 0, hi = bt.B;                                   // pre[lo] * h_kv <= ww < pre[hi] * h_kv
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if ((int64_t)pre[mid] * bt.h_kv <= ww) lo = mid;
+                    else hi = mid;
+                }
+                int t0;
+                const int rows_all = paged_rows(bt, lo, &t0), n_rows = min(rows_all, p.max_q) * p.group, len = bt.kv_len[lo];
+                int64_t local = ww - (int64_t)pre[lo] * bt.h_kv;
+                int r = 0, steps = 0, first = 0;
+                for (int r0 = 0;; r0 += 32) {                            // the row tile: sums over 32 at a time
+                    int f, v = tile_steps<N, T::kRows>((r0 + lane) * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &f);
+                    const int mine = v;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const int u = __shfl_up_sync(0xffffffffu, v, o);
+                        if (lane >= o) v += u;
+                    }
+                    const uint32_t beyond = __ballot_sync(0xffffffffu, (int64_t)v * bt.h_kv > local);
+                    if (beyond) {
+                        const int at = __ffs(beyond) - 1;
+                        r = r0 + at;
+                        steps = __shfl_sync(0xffffffffu, mine, at);
+                        first = __shfl_sync(0xffffffffu, f, at);
+                        local -= (int64_t)(__shfl_sync(0xffffffffu, v, at) - steps) * bt.h_kv;
+                        break;
+                    }
+                    local -= (int64_t)__shfl_sync(0xffffffffu, v, 31) * bt.h_kv;
+                }
+                const int head0 = (int)(local / steps);
+                int ua = (int)(local - (int64_t)head0 * steps);
+                for (int head = head0; head < bt.h_kv && ww < w_end && n < T::kMaxSegments; ++head, ua = 0, ++n) {
+                    const int ub = (int)min((int64_t)steps, ua + (w_end - ww));
+                    const bool whole = ua == 0 && ub == steps;
+                    if (lane == 0) {
+                        segs[n] = TileSegment{head, r * T::kRows, n_rows, t0, len - rows_all, min(len, held), first + ua, ub - ua, whole ? -1 : ww == w_first ? 0 : 1, lo * bt.table_ld};
+                        if (ua == 0 && !whole) p.split[blockIdx.x] = make_int4(lo, head, r, (int)((ww + steps - 1) / span) * 2 + (ww == w_first ? 0 : 1));
+                    }
+                    ww += ub - ua;
+                }
+            }
+            if (lane == 0) n_segs = n;
+        }
+        begin_round();
+        if (lane == 0) {
+            // ================================================================ the products
+            constexpr uint32_t kIdescS = umma_idesc_f16(N), kIdescO = umma_idesc_f16(D) | (1u << 16);   // (V is transposed)
+            const auto score = [&](int t, int stage, int slot) {
+#pragma unroll
+                for (int pn = 0; pn < NB; ++pn)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        umma_f16_lo(tmem + T::kS + N * slot, umma_desc_lo(sbase + T::kOffQ + (t * NB + pn) * T::kPanelQ) + 2 * k, umma_desc_lo(sbase + T::kOffK + stage * T::kStage + pn * T::kPanelKV) + 2 * k, kIdescS, pn + k > 0);
+                umma_commit(sf(slot));
+            };
+            const auto value = [&](int t, int stage, int slot, bool add) {
+#pragma unroll
+                for (int k = 0; k < N / 16; ++k)
+                    umma_f16_ta(tmem + T::kO + D * t, tmem + T::kS + N * slot + 8 * k, ((sbase + T::kOffV + stage * T::kStage + 2048 * k) >> 4) | ((uint32_t)(T::kPanelKV >> 4) << 16), kIdescO, add || k > 0);
+                umma_commit(of(slot));
+            };
+            uint32_t it = rd.it0;
+            bool ok = true;
+            for (int si = 0; si < rd.n && ok; ++si) {
+                const int steps = segs[si].n;
+                for (int t = 0; t < NT && ok; ++t) ok = mbar_wait(qf(t), (rd.seg0 + si) & 1, abort_flag, 0xA50 + t);
+                ok = ok && mbar_wait_hot(kf(it & 1), (it >> 1) & 1, abort_flag, 0xA60);
+                if (!ok) break;
+                if (NT == 2) {
+                    score(0, it & 1, 0);
+                    score(1, it & 1, 1);
+                } else {
+                    score(0, it & 1, it & 1);
+                }
+                umma_commit(ke(it & 1));
+                for (int j = 0; j < steps; ++j, ++it) {
+                    const bool more = j + 1 < steps;
+                    const uint32_t nx = it + 1;
+                    if (NT == 1 && more) {                               // the next scores first: the softmax has two buffers
+                        if (!(ok = mbar_wait_hot(kf(nx & 1), (nx >> 1) & 1, abort_flag, 0xA61))) break;
+                        score(0, nx & 1, nx & 1);
+                        umma_commit(ke(nx & 1));
+                    }
+                    if (!(ok = mbar_wait_hot(vf(it & 1), (it >> 1) & 1, abort_flag, 0xA70))) break;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const int slot = NT == 2 ? t : it & 1;
+                        if (!(ok = mbar_wait_hot(pf(slot), NT == 2 ? it & 1 : (it >> 1) & 1, abort_flag, 0xA80 + slot))) break;
+                        tc_fence_after();
+                        value(t, it & 1, slot, j > 0);
+                        if (t == NT - 1) umma_commit(ve(it & 1));
+                        if (NT == 2 && more) {
+                            if (t == 0 && !(ok = mbar_wait_hot(kf(nx & 1), (nx >> 1) & 1, abort_flag, 0xA62))) break;
+                            score(t, nx & 1, t);
+                            if (t == 1) umma_commit(ke(nx & 1));
+                        }
+                    }
+                    if (!ok) break;
+                }
+            }
+        }
+        end_round();
+        }
+        while (rd.on) { begin_round(); end_round(); }                    // (warps 13 to 15)
+    }
+    // every product has to be complete before the memory it reads and writes is given back
+    if (tid == 12 * 32) {
+        umma_commit(done);
+        mbar_wait(done, 0, abort_flag + 1, 0);
+    }
+    __syncthreads();
+    if (warp == 12) tmem_dealloc(tmem, 512);
+}
+
+}  // namespace ql

@@ -11,9 +11,16 @@
 
 #include "host.h"
 
+namespace ql {
+// This unit's words of the bounded waits (sm100_ptx.cuh): the host reads the pinned one, which the whole device shares.
+static __device__ unsigned int g_device_flag[2];
+static __device__ unsigned int* g_status_host;
+}  // namespace ql
+
 #include "logits.cuh"
 #include "paged.cuh"
 #include "paged_attention.cuh"
+#include "paged_tiles.cuh"
 #include "rope_tables.cuh"
 
 using namespace ql;
@@ -116,6 +123,18 @@ extern "C" ql_status qlinear_paged_create(const qlinear_paged_desc* d, void* poo
     SharedState shared;
     const ql_status st = shared_state(device, &shared);
     if (st != QL_OK) return st;
+    {
+        // this unit's kernels report an expired wait through the device's pinned word as well
+        static std::atomic<bool> linked[64];
+        DeviceGuard guard(device);
+        if (!guard.ok) { cudaGetLastError(); return QL_ERR_CUDA; }
+        unsigned int* word = nullptr;
+        if (!linked[device].load(std::memory_order_acquire)) {
+            if (cudaHostGetDevicePointer(reinterpret_cast<void**>(&word), const_cast<unsigned int*>(shared.status_host), 0) != cudaSuccess ||
+                cudaMemcpyToSymbol(g_status_host, &word, sizeof(word)) != cudaSuccess) { cudaGetLastError(); return QL_ERR_CUDA; }
+            linked[device].store(true, std::memory_order_release);
+        }
+    }
     qlinear_paged_s* h = new (std::nothrow) qlinear_paged_s();
     if (!h) return QL_ERR_ALLOC;
     h->d = *d;
@@ -180,33 +199,42 @@ extern "C" ql_status qlinear_paged_read(qlinear_paged_t h, const int32_t* table,
 
 namespace {
 
-struct AttnPlan { int32_t group, row_blocks, grid; int64_t segments; size_t parts_at, bytes; };
+struct AttnPlan { bool tiles; int32_t group, rows, row_blocks, grid; size_t split_at, bytes; };   // rows: of a segment
 // The launch of an attention call, from what the host knows of it; false for bad arguments.
 bool attn_plan(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t max_q, AttnPlan* a)
 {
     if (!h || h_q < 1 || h_q > 65536 || h_q % h->d.h_kv || B < 0 || B > QL_PAGED_MAX_SEQUENCES || max_q < 0) return false;
     a->group = h_q / h->d.h_kv;
-    const int64_t rows = (int64_t)max_q * a->group, blocks = (rows + kAttnCols - 1) / kAttnCols;
-    a->segments = blocks * h->d.h_kv * B;
-    if (rows > INT32_MAX || a->segments > INT32_MAX) return false;
-    a->row_blocks = (int32_t)blocks;
-    a->grid = 2 * h->shared.sms;
-    a->parts_at = (size_t)2 * a->grid * kAttnCols * (h->d.d_h + 2) * sizeof(float);
-    a->bytes = a->parts_at + (size_t)a->segments * sizeof(int2);
+    const int64_t rows = (int64_t)max_q * a->group;
+    if (rows > INT32_MAX / 2) return false;
+    a->tiles = rows > kAttnMaxRows;
+    a->rows = a->tiles ? (h->d.d_h == 256 ? TileShape<256>::kRows : TileShape<128>::kRows) : kAttnCols;
+    a->row_blocks = (int32_t)((rows + a->rows - 1) / a->rows);
+    a->grid = (a->tiles ? 1 : 2) * h->shared.sms;
+    a->split_at = (size_t)2 * a->grid * a->rows * (h->d.d_h + 2) * sizeof(float);
+    a->bytes = a->split_at + (size_t)a->grid * sizeof(int4);
     return true;
 }
 
 template <int D, bool CAP>
-cudaError_t launch_attention(const PagedAttnParams& p, int device, cudaStream_t st, bool pdl)
+cudaError_t launch_attention(const PagedAttnParams& p, bool tiles, int device, cudaStream_t st, bool pdl)
 {
+    using T = TileShape<D>;
     static std::atomic<bool> flags[64];
-    constexpr int kMost = AttnRing<D>::kBytes + (QL_PAGED_MAX_SEQUENCES + 1) * 4;
+    constexpr int kMost = AttnRing<D>::kBytes + (QL_PAGED_MAX_SEQUENCES + 1) * 4, kMostTiles = 1024 + T::kOffPre + (QL_PAGED_MAX_SEQUENCES + 1) * 4;
     if (!flags[device].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(paged_attention_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        cudaFuncAttributes at;
+        cudaError_t e = cudaFuncSetAttribute(paged_attention_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_tiles_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostTiles);
+        if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, paged_tiles_kernel<D, CAP>);
         if (e != cudaSuccess) return e;
+        if (at.numRegs < 128) return cudaErrorInvalidConfiguration;      // (the roles' shares are taken from what the block was launched with: a smaller sum would be waited for)
         flags[device].store(true, std::memory_order_release);
     }
-    return launch(paged_attention_kernel<D, CAP>, p, dim3(p.grid), dim3(kAttnWarps * 32), AttnRing<D>::kBytes + (p.batch.B + 1) * 4, st, 1, pdl);
+    cudaError_t e = tiles ? launch(paged_tiles_kernel<D, CAP>, p, dim3(p.grid), dim3(kTileThreads), 1024 + T::kOffPre + (p.batch.B + 1) * 4, st, 1, pdl)
+                          : launch(paged_attention_kernel<D, CAP>, p, dim3(p.grid), dim3(kAttnWarps * 32), AttnRing<D>::kBytes + (p.batch.B + 1) * 4, st, 1, pdl);
+    if (e != cudaSuccess) return e;
+    return tiles ? launch(paged_combine_kernel<D, T::kRows>, p, dim3(p.grid, T::kRows / 8), dim3(256), 0, st, 1, pdl) : launch(paged_combine_kernel<D, kAttnCols>, p, dim3(p.grid), dim3(256), 0, st, 1, pdl);
 }
 
 }  // namespace
@@ -235,21 +263,16 @@ extern "C" ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q, i
     p.q = static_cast<const __half*>(q);
     p.out = static_cast<__half*>(out);
     p.partial = static_cast<float*>(workspace);
-    p.parts = reinterpret_cast<int2*>(static_cast<char*>(workspace) + a.parts_at);
+    p.split = reinterpret_cast<int4*>(static_cast<char*>(workspace) + a.split_at);
     p.q_ld = q_ld; p.out_ld = out_ld;
     p.h_q = h_q; p.group = a.group; p.max_q = max_q; p.row_blocks = a.row_blocks; p.window = window;
     p.scale = scale; p.softcap = softcap; p.grid = a.grid;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool cap = softcap > 0.f;
     cudaError_t e;
-    if (d == 64) e = cap ? launch_attention<64, true>(p, h->device, st, h->pdl) : launch_attention<64, false>(p, h->device, st, h->pdl);
-    else if (d == 128) e = cap ? launch_attention<128, true>(p, h->device, st, h->pdl) : launch_attention<128, false>(p, h->device, st, h->pdl);
-    else e = cap ? launch_attention<256, true>(p, h->device, st, h->pdl) : launch_attention<256, false>(p, h->device, st, h->pdl);
-    if (e != cudaSuccess) return launched(e);
-    const dim3 grid((unsigned)a.segments), block(kAttnWarps * 32);
-    if (d == 64) e = launch(paged_combine_kernel<64>, p, grid, block, 0, st, 1, h->pdl);
-    else if (d == 128) e = launch(paged_combine_kernel<128>, p, grid, block, 0, st, 1, h->pdl);
-    else e = launch(paged_combine_kernel<256>, p, grid, block, 0, st, 1, h->pdl);
+    if (d == 64) e = cap ? launch_attention<64, true>(p, a.tiles, h->device, st, h->pdl) : launch_attention<64, false>(p, a.tiles, h->device, st, h->pdl);
+    else if (d == 128) e = cap ? launch_attention<128, true>(p, a.tiles, h->device, st, h->pdl) : launch_attention<128, false>(p, a.tiles, h->device, st, h->pdl);
+    else e = cap ? launch_attention<256, true>(p, a.tiles, h->device, st, h->pdl) : launch_attention<256, false>(p, a.tiles, h->device, st, h->pdl);
     return launched(e);
 }
 

@@ -82,13 +82,14 @@ def filled(P, torch, batch, h_kv, d, seed=1, k_scale=1.0):
     return cache, [(held(k[e - l:e]), held(v[e - l:e])) for e, l in zip(ends, batch.lens)]
 
 
-def attention64(q, kv, batch, scale, softcap=0.0, window=0, rows=None):
-    """(out, bound per element): the definition in 64 bits.  The kernels round the unnormalised weights to fp16 (2^-11 relative, 2^-25 absolute below 2^-14,
+def attention64(q, kv, batch, scale, softcap=0.0, window=0, rows=None, max_q=None):
+    """(out, bound per element): the definition in 64 bits.  Beyond 32 rows per KV head the keys are rounded to fp16(q s) as well: 2^-11 of each product.  The kernels round the unnormalised weights to fp16 (2^-11 relative, 2^-25 absolute below 2^-14,
     of weights whose largest is at least 1), the values q s to fp16 (2^-11) and the result (2^-11, 2^-25 absolute); scores are sums of d products in fp32 whose
     error moves a weight by exp(error) - 1."""
     T, h_q, d = q.shape
     out, tol = np.zeros((T, h_q, d)), np.zeros((T, h_q, d))
     g = h_q // kv[0][0].shape[1]
+    key = 2.0 ** -11 if (max_q or batch.max_q) * g > 32 else 0.0
     for t, b, pos in rows or batch.rows():
         k, v = kv[b]
         lo, hi = (max(0, pos - window + 1) if window else 0), min(pos + 1, len(k))
@@ -98,7 +99,7 @@ def attention64(q, kv, batch, scale, softcap=0.0, window=0, rows=None):
             kk, vv = k[lo:hi, hk], v[lo:hi, hk]
             q64 = q[t, hk * g:(hk + 1) * g].astype(np.float64)
             x = q64 @ kk.T * scale
-            dx = (d + 40) * 2.0 ** -24 * (np.abs(q64) @ np.abs(kk).T) * abs(scale)         # sums in any order, scale, scores on a base-2 scale
+            dx = (key + (d + 40) * 2.0 ** -24) * (np.abs(q64) @ np.abs(kk).T) * abs(scale)         # sums in any order, scale, scores on a base-2 scale
             if softcap:
                 x = softcap * np.tanh(x / softcap)
                 dx = dx + 16 * 2.0 ** -24 * softcap                      # (quotient, exponential and reciprocal of a few ulp on numbers up to softcap)
@@ -315,7 +316,7 @@ def test_more_rows_than_tokens(P, torch, more):
     rows = [(int(starts[b]) + i, b, lens[b] - n + i) for b, n in enumerate(new) for i in range(n)]
     seen = [r for r in rows if r[2] >= 0]
     assert not got[[r[0] for r in rows if r[2] < 0]].any() and got[[r[0] for r in seen]].any(-1).all()
-    want, tol = attention64(q.cpu().numpy(), kv, batch, 0.125, rows=seen)
+    want, tol = attention64(q.cpu().numpy(), kv, batch, 0.125, rows=seen, max_q=max(new))
     check(got, want, tol, seen)
 
 
@@ -326,7 +327,7 @@ def test_rows_behind_max_q_stay(P, torch, new, most):
     q = f16(np.random.default_rng(2), 2 * new, 2, 64)
     out = torch.full((2 * new, 2, 64), 3.0, dtype=torch.float16, device="cuda")
     got = cache.attention(torch.from_numpy(q).cuda(), *batch.args, most, out=out).cpu().numpy()
-    want, tol = attention64(q, kv, batch, 0.125)
+    want, tol = attention64(q, kv, batch, 0.125, max_q=most)
     check(got, want, tol, [r for r in batch.rows() if r[0] % new < most])
     assert (got[[t for t in range(2 * new) if t % new >= most]] == 3).all()
 
@@ -337,7 +338,7 @@ def test_rows_that_are_no_rows(P, torch, max_q):
     batch = Batch(torch, [20, 20, 20], [1, 1, 1], 16)
     cache, kv = filled(P, torch, batch, 2, 64)
     q = f16(np.random.default_rng(2), 3, 2, 64)
-    want, tol = attention64(q, kv, batch, 0.125)
+    want, tol = attention64(q, kv, batch, 0.125, max_q=max_q)
     for starts, rows in (([0, 1, 5, 6], [0]), ([0, 1, 0, 1], None), ([-1, 0, 1, 2], None)):
         st = torch.tensor(starts, dtype=torch.int32, device="cuda")
         out = torch.full((3, 2, 64), 3.0, dtype=torch.float16, device="cuda")
