@@ -38,8 +38,8 @@ struct PagedAttnParams {
     PagedBatch batch;
     const __half* q;             // row t, head h at q + t * q_ld + h * D
     __half* out;                 // the same with out_ld
-    float* partial;              // [2 * gridDim.x][rows * D of o, rows of m, rows of l]; slot 0 of a CTA: the part that its span begins with
-    int4* split;                 // per CTA: sequence (-1: none), KV head, row block of the segment that begins in its span and ends in another's, and 2 * (the last CTA that holds a part) + (the first part's slot)
+    float* partial;              // [2 * gridDim.x][rows * D of o, rows of m, rows of l]; slot 1 of a CTA: the first part of a segment, slot 0: a later one
+    int4* split;                 // per CTA: sequence (-1: none), KV head, row block of the segment that begins in its span and ends in another's, and the last CTA that holds a part
     int64_t q_ld, out_ld;
     int32_t h_q, group, max_q, row_blocks, window;
     float scale, softcap;        // (softcap 0: none)
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
         }
         __syncthreads();
         const bool whole = ua == 0 && ub == blocks;
-        float* part = p.partial + (int64_t)(2 * blockIdx.x + (w == w0 ? 0 : 1)) * (kAttnCols * (D + 2));
+        float* part = p.partial + (int64_t)(2 * blockIdx.x + (ua > 0 ? 0 : 1)) * (kAttnCols * (D + 2));
         for (int e = tid * 4; e < kAttnCols * D; e += kAttnWarps * 32 * 4) {
             const int col = e / D, d = e - col * D, r = r0 + col;
             float mm = -1e30f, l = 0.f;
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
                 *reinterpret_cast<uint2*>(p.out + (int64_t)(t0 + i) * p.out_ld + (int64_t)(head * p.group + r - i * p.group) * D + d) = *reinterpret_cast<const uint2*>(y);
             }
         }
-        if (tid == 0 && ua == 0 && !whole) p.split[blockIdx.x] = make_int4(b, head, seg - head * p.row_blocks, 2 * (int)((w + blocks - 1) / span) + (w == w0 ? 0 : 1));
+        if (tid == 0 && ua == 0 && !whole) p.split[blockIdx.x] = make_int4(b, head, seg - head * p.row_blocks, (int)((w + blocks - 1) / span));
         w += ub - ua;
         __syncthreads();                                                 // (the ring is free again)
     }
@@ -380,13 +380,13 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnParam
     constexpr int64_t kStride = ROWS * (D + 2);
     const int4 split = p.split[blockIdx.x];
     if (split.x < 0) return;
-    const int row = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, r = split.z * ROWS + row, c0 = blockIdx.x, c1 = split.w >> 1, slot = split.w & 1;
+    const int row = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, r = split.z * ROWS + row, c0 = blockIdx.x, c1 = split.w;
     int t0;
     if (r >= min(paged_rows(p.batch, split.x, &t0), p.max_q) * p.group) return;
     float m = -1e30f, l = 0.f, acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
-    const auto part_of = [&](int c) { return p.partial + (2 * c + (c == c0 ? slot : 0)) * kStride; };
+    const auto part_of = [&](int c) { return p.partial + (2 * c + (c == c0 ? 1 : 0)) * kStride; };
     for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, part_of(c)[ROWS * D + row]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));

@@ -13,8 +13,8 @@
 // Warps 0-3, 4-7: softmax of the two tiles (at d_h 256 one tile of 128 rows with two buffers of S, and warps 4-7 unpack as well); warps 8-11: unpack;
 // warp 12: issues the products.  The two tiles alternate: while one's softmax runs, the tensor core has the other's products.
 //
-// Work: the (segment, step) pairs of the whole batch, numbered through, in one span of equal length per CTA, as in paged_attention.cuh; a segment cut by a span's end
-// leaves its rows' (m, l, O) in the workspace for paged_combine_kernel.
+// Work: the segments of the whole batch, numbered through, each as long as its steps and kTileOverhead more (queries in, rows out, an empty pipeline), in one span of
+// equal length per CTA, as in paged_attention.cuh; a segment cut by a span's end leaves its rows' (m, l, O) in the workspace for paged_combine_kernel.
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -42,6 +42,7 @@ template <int D> struct TileShape {
     static constexpr uint32_t kO = NT == 2 ? 256 : 0, kS = NT == 2 ? 0 : 256;             // columns of tensor memory
 };
 constexpr int kTileThreads = 512;
+constexpr int kTileOverhead = 3;                                         // a segment without steps, in steps
 
 struct TileSegment {
     int32_t head, row0, n_rows, t0, pos0, end, step0, n, slot;           // rows of the sequence row0 .. (n_rows of it), row 0's token and position, keys [.., end), steps step0 .. + n
@@ -73,6 +74,8 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 template <int R> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
 template <int R> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
 
+__device__ __forceinline__ int tile_length(int steps) { return steps > 0 ? steps + kTileOverhead : 0; }
+
 // Steps of N keys that the rows [row0, row0 + kRows) of a sequence see: *first the first of them.  rows_all rows of len tokens, n_rows (times group) of them served.
 template <int N, int kRows>
 __device__ __forceinline__ int tile_steps(int row0, int n_rows, int rows_all, int len, int held, int group, int window, int* first)
@@ -92,10 +95,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
     constexpr int NT = T::NT, N = T::N, NB = T::NB;
     extern __shared__ __align__(128) uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    int* pre = reinterpret_cast<int*>(smem + T::kOffPre);                // [B + 1]: steps (of all row tiles, per head) before sequence b
+    int* pre = reinterpret_cast<int*>(smem + T::kOffPre);                // [B + 1]: length of the row tiles (per head) before sequence b
     __shared__ __align__(8) uint64_t bars[17];
     __shared__ TileSegment segs[T::kMaxSegments];
     __shared__ int n_segs;
+    __shared__ int64_t round_end;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t abort_flag[4];
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, c = lane & 3;
@@ -129,11 +133,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
 
     const PagedBatch& bt = p.batch;
     const int held = (int)min((int64_t)bt.table_width << (bt.log2_blocks + 4), (int64_t)INT32_MAX);
-    // ---- the plan: steps per sequence, their sums
+    // ---- the plan: the length of every sequence, their sums
     for (int b = warp; b < bt.B; b += kTileThreads / 32) {
         int t0, first, sum = 0;
         const int rows_all = paged_rows(bt, b, &t0), n_rows = min(rows_all, p.max_q) * p.group, len = bt.kv_len[b];
-        for (int r = lane; r * T::kRows < n_rows; r += 32) sum += tile_steps<N, T::kRows>(r * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &first);
+        for (int r = lane; r * T::kRows < n_rows; r += 32) sum += tile_length(tile_steps<N, T::kRows>(r * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &first));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (lane == 0) pre[b + 1] = sum;
@@ -186,7 +190,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
     const auto end_round = [&]() {
         __syncwarp();
         __syncthreads();
-        rd.w += rd.steps;
+        rd.w = round_end;
         rd.it0 += rd.steps;                                              // steps and segments before the next round
         rd.seg0 += rd.n;
         rd.on = rd.w < w_end && !abort_flag[0];
@@ -204,22 +208,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
             const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
             const auto load_q = [&](const TileSegment& s) {              // this tile's rows, 16 lanes per row of 128 elements
                 constexpr int kChunks = D / 8;
-#pragma unroll 4
-                for (int e = in_tile; e < 128 * kChunks; e += 128) {
-                    const int row = e / kChunks, ch = e - row * kChunks, rr = s.row0 + 128 * t + row;
-                    uint4 u = make_uint4(0, 0, 0, 0);
-                    if (rr < s.n_rows) {
-                        const int i = rr / p.group;
-                        u = *reinterpret_cast<const uint4*>(p.q + (int64_t)(s.t0 + i) * p.q_ld + (int64_t)(s.head * p.group + rr - i * p.group) * D + 8 * ch);
-                        u.x ^= sign; u.y ^= sign; u.z ^= sign; u.w ^= sign;
+#pragma unroll
+                for (int e0 = 0; e0 < kChunks; e0 += 16) {               // (16 loads on their way at a time)
+                    uint4 u[kChunks < 16 ? kChunks : 16];
+#pragma unroll
+                    for (int k = 0; k < (kChunks < 16 ? kChunks : 16); ++k) {
+                        const int e = in_tile + 128 * (e0 + k), row = e / kChunks, ch = e - row * kChunks, rr = s.row0 + 128 * t + row, i = rr / p.group;
+                        u[k] = rr < s.n_rows ? *reinterpret_cast<const uint4*>(p.q + (int64_t)(s.t0 + i) * p.q_ld + (int64_t)(s.head * p.group + rr - i * p.group) * D + 8 * ch) : make_uint4(0, 0, 0, 0);
                     }
-                    *reinterpret_cast<uint4*>(smem + T::kOffQ + (t * NB + (ch >> 3)) * T::kPanelQ + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = u;
+#pragma unroll
+                    for (int k = 0; k < (kChunks < 16 ? kChunks : 16); ++k) {
+                        const int e = in_tile + 128 * (e0 + k), row = e / kChunks, ch = e - row * kChunks;
+                        u[k].x ^= sign; u[k].y ^= sign; u[k].z ^= sign; u[k].w ^= sign;
+                        *reinterpret_cast<uint4*>(smem + T::kOffQ + (t * NB + (ch >> 3)) * T::kPanelQ + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = u[k];
+                    }
                 }
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(qf(t));
             };
-            load_q(segs[0]);
+            if (rd.n > 0) load_q(segs[0]);
             uint32_t it = rd.it0;
             bool ok = true;
             for (int si = 0; si < rd.n && ok; ++si) {
@@ -390,11 +398,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                 unpack_int4_word(word, h);
                 *reinterpret_cast<uint4*>(row + chunk * 16) = make_uint4(h2_mul(h[0], scale), h2_mul(h[1], scale), h2_mul(h[2], scale), h2_mul(h[3], scale));
             };
-            look_up();
-            request_k();
-            request_v();
-            look_up();
-            next(si_l, j_l);
+            if (rd.steps > 0) {
+                look_up();
+                request_k();
+                request_v();
+                look_up();
+                next(si_l, j_l);
+            }
             for (uint32_t q = 0; q < rd.steps; ++q) {
                 const uint32_t it = rd.it0 + q, st = it & 1, par = ((it >> 1) & 1) ^ 1;
                 if (!warp_wait(ke(st), par, abort_flag, 0xA30 + st)) break;
@@ -458,8 +468,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                 int64_t local = ww - (int64_t)pre[lo] * bt.h_kv;
                 int r = 0, steps = 0, first = 0;
                 for (int r0 = 0;; r0 += 32) {                            // the row tile: sums over 32 at a time
-                    int f, v = tile_steps<N, T::kRows>((r0 + lane) * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &f);
-                    const int mine = v;
+                    int f;
+                    const int mine = tile_steps<N, T::kRows>((r0 + lane) * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &f);
+                    int v = tile_length(mine);
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
                         const int u = __shfl_up_sync(0xffffffffu, v, o);
@@ -471,23 +482,27 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                         r = r0 + at;
                         steps = __shfl_sync(0xffffffffu, mine, at);
                         first = __shfl_sync(0xffffffffu, f, at);
-                        local -= (int64_t)(__shfl_sync(0xffffffffu, v, at) - steps) * bt.h_kv;
+                        local -= (int64_t)(__shfl_sync(0xffffffffu, v, at) - tile_length(steps)) * bt.h_kv;
                         break;
                     }
                     local -= (int64_t)__shfl_sync(0xffffffffu, v, 31) * bt.h_kv;
                 }
-                const int head0 = (int)(local / steps);
-                int ua = (int)(local - (int64_t)head0 * steps);
-                for (int head = head0; head < bt.h_kv && ww < w_end && n < T::kMaxSegments; ++head, ua = 0, ++n) {
-                    const int ub = (int)min((int64_t)steps, ua + (w_end - ww));
-                    const bool whole = ua == 0 && ub == steps;
-                    if (lane == 0) {
-                        segs[n] = TileSegment{head, r * T::kRows, n_rows, t0, len - rows_all, min(len, held), first + ua, ub - ua, whole ? -1 : ww == w_first ? 0 : 1, lo * bt.table_ld};
-                        if (ua == 0 && !whole) p.split[blockIdx.x] = make_int4(lo, head, r, (int)((ww + steps - 1) / span) * 2 + (ww == w_first ? 0 : 1));
+                const int length = tile_length(steps), head0 = (int)(local / length);
+                int ua = (int)(local - (int64_t)head0 * length);
+                for (int head = head0; head < bt.h_kv && ww < w_end && n < T::kMaxSegments; ++head, ua = 0) {
+                    const int ub = (int)min((int64_t)length, ua + (w_end - ww)), sa = max(ua - kTileOverhead, 0), sb = max(ub - kTileOverhead, 0);
+                    if (sb > sa) {
+                        const bool whole = sa == 0 && sb == steps;
+                        if (lane == 0) {
+                            segs[n] = TileSegment{head, r * T::kRows, n_rows, t0, len - rows_all, min(len, held), first + sa, sb - sa, whole ? -1 : sa > 0 ? 0 : 1, lo * bt.table_ld};
+                            if (sa == 0 && !whole) p.split[blockIdx.x] = make_int4(lo, head, r, (int)((ww - ua + length - 1) / span));
+                        }
+                        ++n;
                     }
                     ww += ub - ua;
                 }
             }
+            if (lane == 0) round_end = ww;
             if (lane == 0) n_segs = n;
         }
         begin_round();
