@@ -349,7 +349,7 @@ ql_status qlinear_rope_tables(float* cos_dev, float* sin_dev, int32_t first, int
  * qlinear_paged_attention: out[t, h] = sum_j softmax_j(x_j) v_j with x_j = scale q.k_j, or softcap * tanh(scale q.k_j / softcap) where softcap > 0, over the visible tokens of the
  *   row's sequence: j <= p, j < kv_len, and p - j < window where window > 0.  Query head h reads KV head h / (h_q / h_kv).  A row that sees nothing gives zeros.  max_q: no sequence has
  *   more rows (rows beyond it are left as they are); scores, softmax and sums in fp32, weights and values fp16.  out_dev must not overlap q_dev.
- *   workspace_dev: qlinear_paged_attention_workspace bytes of the caller's, 16-byte aligned, overwritten; calls that may overlap need one each.
+ *   workspace_dev: qlinear_paged_attention_workspace bytes of the caller's, 32-byte aligned, overwritten; calls that may overlap need one each.
  * Asynchronous, allocate nothing; appends must be ordered against the calls that read the same pages.
  * Errors: QL_ERR_INVALID_ARG, QL_ERR_UNSUPPORTED (create: the descriptor), QL_ERR_CUDA, QL_ERR_DEVICE_TIMEOUT (see qlinear_forward; qlinear_paged_device_status is
  * qlinear_device_status for this handle's device). */

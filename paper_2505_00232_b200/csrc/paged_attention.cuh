@@ -370,8 +370,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
     }
 }
 
-// Joins the parts of the segment that begins in a CTA's span and ends in another's, in order: CTA blockIdx.x's, rows 8 blockIdx.y and so on, a warp per row.
-template <int D, int ROWS>
+// Joins the parts of the segment that begins in a CTA's span and ends in another's, in order: CTA blockIdx.x's, ROWS / gridDim.y of its rows, R at a time per warp.
+template <int D, int ROWS, int R>
 __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnParams p)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -380,29 +380,46 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnParam
     constexpr int64_t kStride = ROWS * (D + 2);
     const int4 split = p.split[blockIdx.x];
     if (split.x < 0) return;
-    const int row = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, r = split.z * ROWS + row, c0 = blockIdx.x, c1 = split.w;
+    const int row = (blockIdx.y * 8 + (threadIdx.x >> 5)) * R, lane = threadIdx.x & 31, c0 = blockIdx.x, c1 = split.w;
     int t0;
-    if (r >= min(paged_rows(p.batch, split.x, &t0), p.max_q) * p.group) return;
-    float m = -1e30f, l = 0.f, acc[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) acc[e] = 0.f;
+    const int n_rows = min(paged_rows(p.batch, split.x, &t0), p.max_q) * p.group;
+    if (split.z * ROWS + row >= n_rows) return;
     const auto part_of = [&](int c) { return p.partial + (2 * c + (c == c0 ? 1 : 0)) * kStride; };
-    for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, part_of(c)[ROWS * D + row]);
+    float m[R], l[R], acc[R][V];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-#pragma unroll 4
+    for (int k = 0; k < R; ++k) {
+        m[k] = -1e30f;
+        l[k] = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[k][e] = 0.f;
+    }
+    for (int c = c0 + lane; c <= c1; c += 32)
+#pragma unroll
+        for (int k = 0; k < R; ++k) m[k] = fmaxf(m[k], part_of(c)[ROWS * D + row + k]);
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m[k] = fmaxf(m[k], __shfl_xor_sync(0xffffffffu, m[k], o));
+#pragma unroll 2
     for (int c = c0; c <= c1; ++c) {
         const float* part = part_of(c);
-        const float f = exp2_fast(part[ROWS * D + row] - m);
-        l += part[ROWS * D + ROWS + row] * f;
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = fmaf(part[row * D + V * lane + e], f, acc[e]);
+        for (int k = 0; k < R; ++k) {
+            const float f = exp2_fast(part[ROWS * D + row + k] - m[k]);
+            l[k] += part[ROWS * D + ROWS + row + k] * f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[k][e] = fmaf(part[(row + k) * D + V * lane + e], f, acc[k][e]);
+        }
     }
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    const int i = r / p.group;
-    __half* to = p.out + (int64_t)(t0 + i) * p.out_ld + (int64_t)(split.y * p.group + r - i * p.group) * D + V * lane;
 #pragma unroll
-    for (int e = 0; e < V; e += 2) *reinterpret_cast<__half2*>(to + e) = __floats2half2_rn(acc[e] * inv, acc[e + 1] * inv);
+    for (int k = 0; k < R; ++k) {
+        const int r = split.z * ROWS + row + k, i = r / p.group;
+        if (r >= n_rows) break;
+        const float inv = l[k] > 0.f || l[k] != l[k] ? 1.f / l[k] : 0.f;
+        __half* to = p.out + (int64_t)(t0 + i) * p.out_ld + (int64_t)(split.y * p.group + r - i * p.group) * D + V * lane;
+#pragma unroll
+        for (int e = 0; e < V; e += 2) *reinterpret_cast<__half2*>(to + e) = __floats2half2_rn(acc[k][e] * inv, acc[k][e + 1] * inv);
+    }
 }
 
 }  // namespace ql

@@ -69,6 +69,30 @@ __device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const uint32_t r
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float a0, float a1, float b, float c)                           // (a0 b + c, a1 b + c)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+// 32 bytes in one store.
+__device__ __forceinline__ void store32(void* p, const uint32_t r[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
 // A wait of a whole warp: its lanes agree on the outcome (what follows is warp-collective).
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t code) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, code)); }
 template <int R> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
@@ -96,7 +120,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
     extern __shared__ __align__(128) uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     int* pre = reinterpret_cast<int*>(smem + T::kOffPre);                // [B + 1]: length of the row tiles (per head) before sequence b
-    __shared__ __align__(8) uint64_t bars[17];
+    __shared__ __align__(8) uint64_t bars[19];
     __shared__ TileSegment segs[T::kMaxSegments];
     __shared__ int n_segs;
     __shared__ int64_t round_end;
@@ -104,13 +128,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
     __shared__ volatile uint32_t abort_flag[4];
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, c = lane & 3;
     const uint32_t bar0 = smem_u32(bars);
-    // barriers: K, V full and empty (two stages), S, P and O per buffer, Q per tile, the end
+    // barriers: K, V full and empty (two stages), S, the halves of P and O per buffer, Q per tile, the end
     const auto kf = [&](int s) { return bar0 + 8 * s; };
     const auto ke = [&](int s) { return bar0 + 8 * (2 + s); };
     const auto vf = [&](int s) { return bar0 + 8 * (4 + s); };
     const auto ve = [&](int s) { return bar0 + 8 * (6 + s); };
     const auto sf = [&](int s) { return bar0 + 8 * (8 + s); };
-    const auto pf = [&](int s) { return bar0 + 8 * (10 + s); };
+    const auto pf = [&](int s, int half) { return bar0 + 8 * (half ? 17 + s : 10 + s); };
     const auto of = [&](int s) { return bar0 + 8 * (12 + s); };
     const auto qf = [&](int t) { return bar0 + 8 * (14 + t); };
     const uint32_t done = bar0 + 8 * 16;
@@ -119,7 +143,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
         for (int s = 0; s < 2; ++s) {
             mbar_init(kf(s), T::kUnpackWarps); mbar_init(vf(s), T::kUnpackWarps);
             mbar_init(ke(s), 1); mbar_init(ve(s), 1);
-            mbar_init(sf(s), 1); mbar_init(pf(s), 4);
+            mbar_init(sf(s), 1); mbar_init(pf(s, 0), 4); mbar_init(pf(s, 1), 4);
             mbar_init(of(s), 1); mbar_init(qf(s), 4);
         }
         mbar_init(done, 1);
@@ -206,21 +230,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
             constexpr float kLog2e = 1.4426950408889634f;
             const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * kLog2e, 1e-30f);   // (never 0: hidden scores are -infinity)
             const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
-            const auto load_q = [&](const TileSegment& s) {              // this tile's rows, 16 lanes per row of 128 elements
-                constexpr int kChunks = D / 8;
+            // this warp's 32 rows of the tile, D / 8 lanes' worth of a row side by side; a lane knows where its own row lies
+            const auto load_q = [&](const TileSegment& s) {
+                constexpr int kChunks = D / 8, kRowsAt = 32 / kChunks > 0 ? 32 / kChunks : 1;   // rows of a load
+                const int mine = s.row0 + 128 * t + in_tile, i = mine / p.group;
+                const int64_t at = mine < s.n_rows ? (int64_t)(s.t0 + i) * p.q_ld + (int64_t)(s.head * p.group + mine - i * p.group) * D : -1;
+                const int sub = lane / kChunks, ch = lane - sub * kChunks;
 #pragma unroll
-                for (int e0 = 0; e0 < kChunks; e0 += 16) {               // (16 loads on their way at a time)
-                    uint4 u[kChunks < 16 ? kChunks : 16];
+                for (int r0 = 0; r0 < 32; r0 += 16 * kRowsAt) {          // (16 loads on their way at a time)
+                    uint4 u[16];
 #pragma unroll
-                    for (int k = 0; k < (kChunks < 16 ? kChunks : 16); ++k) {
-                        const int e = in_tile + 128 * (e0 + k), row = e / kChunks, ch = e - row * kChunks, rr = s.row0 + 128 * t + row, i = rr / p.group;
-                        u[k] = rr < s.n_rows ? *reinterpret_cast<const uint4*>(p.q + (int64_t)(s.t0 + i) * p.q_ld + (int64_t)(s.head * p.group + rr - i * p.group) * D + 8 * ch) : make_uint4(0, 0, 0, 0);
+                    for (int k = 0; k < 16; ++k) {
+                        const int r = r0 + k * kRowsAt + sub;
+                        const int64_t from = __shfl_sync(0xffffffffu, at, r & 31);
+                        u[k] = r < 32 && from >= 0 ? *reinterpret_cast<const uint4*>(p.q + from + 8 * ch) : make_uint4(0, 0, 0, 0);
                     }
 #pragma unroll
-                    for (int k = 0; k < (kChunks < 16 ? kChunks : 16); ++k) {
-                        const int e = in_tile + 128 * (e0 + k), row = e / kChunks, ch = e - row * kChunks;
+                    for (int k = 0; k < 16; ++k) {
+                        const int r = r0 + k * kRowsAt + sub, row = 32 * wq + r;
                         u[k].x ^= sign; u[k].y ^= sign; u[k].z ^= sign; u[k].w ^= sign;
-                        *reinterpret_cast<uint4*>(smem + T::kOffQ + (t * NB + (ch >> 3)) * T::kPanelQ + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = u[k];
+                        if (r < 32) *reinterpret_cast<uint4*>(smem + T::kOffQ + (t * NB + (ch >> 3)) * T::kPanelQ + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = u[k];
                     }
                 }
                 fence_async_smem();
@@ -228,13 +257,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                 if (lane == 0) mbar_arrive(qf(t));
             };
             if (rd.n > 0) load_q(segs[0]);
+            const bool wide_out = ((reinterpret_cast<uintptr_t>(p.out) | (uintptr_t)(p.out_ld * 2)) & 31) == 0;
             uint32_t it = rd.it0;
             bool ok = true;
             for (int si = 0; si < rd.n && ok; ++si) {
                 const TileSegment s = segs[si];
                 const int rr = s.row0 + 128 * t + in_tile, i = rr / p.group, pos = s.pos0 + i;
                 const int last = rr < s.n_rows ? min(pos, s.end - 1) : -1, lowest = p.window > 0 ? pos - p.window : -1;
-                float m = -1e30f, l[4] = {0.f, 0.f, 0.f, 0.f};
+                float m = -1e30f;
+                float2 l[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 const int32_t* table = bt.table + s.table;
                 const auto page_of = [&](int step) {                     // (lane: the page of the block `lane` from that step on)
                     const int at = (step * T::kBlocks + lane) >> bt.log2_blocks;
@@ -276,8 +307,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     if (__any_sync(0xffffffffu, top > m + 8.f)) {        // the maximum is raised, and with it the scale of the sums
                         const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
                         m = mn;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) l[e] *= f;
+                        l[0].x *= f; l[0].y *= f; l[1].x *= f; l[1].y *= f;
                         if (j > 0) {
                             if (NT == 1) {                               // (S of this step may be complete before the values of the one before)
                                 if (!warp_wait(of((it - 1) & 1), ((it - 1) >> 1) & 1, abort_flag, 0xA10)) { ok = false; break; }
@@ -293,29 +323,34 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                             }
                         }
                     }
+                    // weights: in halves, so that the product with the values begins with the first
 #pragma unroll
-                    for (int e = 0; e < N; e += 32) {
-                        uint32_t h[16];
+                    for (int half = 0; half < 2; ++half) {
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const float a = exp2_fast(fmaf(x[e + 2 * k], cc, -m)), b = exp2_fast(fmaf(x[e + 2 * k + 1], cc, -m));
-                            l[2 * (k & 1)] += a;
-                            l[2 * (k & 1) + 1] += b;
-                            const __half2 ab = __floats2half2_rn(a, b);
-                            h[k] = *reinterpret_cast<const uint32_t*>(&ab);
+                        for (int e = half * (N / 2); e < (half + 1) * (N / 2); e += 32) {
+                            uint32_t h[16];
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                float2 y = fma2(x[e + 2 * k], x[e + 2 * k + 1], cc, -m);
+                                y.x = exp2_fast(y.x);
+                                y.y = exp2_fast(y.y);
+                                l[k & 1] = add2(l[k & 1], y);
+                                const __half2 ab = __floats2half2_rn(y.x, y.y);
+                                h[k] = *reinterpret_cast<const uint32_t*>(&ab);
+                            }
+                            tmem_st16_async(ts + e / 2, h);
                         }
-                        tmem_st16_async(ts + e / 2, h);
+                        tmem_st_wait();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(pf(slot, half));
                     }
-                    tmem_st_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(pf(slot));
                 }
                 if (!ok) break;
                 if (si + 1 < rd.n) load_q(segs[si + 1]);                    // (every product with this segment's queries is complete)
                 if (!warp_wait(of(NT == 2 ? t : (it - 1) & 1), NT == 2 ? (it - 1) & 1 : ((it - 1) >> 1) & 1, abort_flag, 0xA20 + t)) { ok = false; break; }
                 tc_fence_after();
-                const float sum = (l[0] + l[1]) + (l[2] + l[3]);
+                const float sum = (l[0].x + l[0].y) + (l[1].x + l[1].y);
                 if (s.slot < 0) {
                     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
                     __half* dst = p.out + (int64_t)(s.t0 + i) * p.out_ld + (int64_t)(s.head * p.group + rr - i * p.group) * D;
@@ -331,7 +366,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                         }
                         if (rr < s.n_rows) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(dst + d + 8 * e) = make_uint4(h[4 * e], h[4 * e + 1], h[4 * e + 2], h[4 * e + 3]);
+                            for (int e = 0; e < 4; e += 2) {
+                                if (wide_out) store32(dst + d + 8 * e, h + 4 * e);
+                                else {
+                                    *reinterpret_cast<uint4*>(dst + d + 8 * e) = make_uint4(h[4 * e], h[4 * e + 1], h[4 * e + 2], h[4 * e + 3]);
+                                    *reinterpret_cast<uint4*>(dst + d + 8 * e + 8) = make_uint4(h[4 * e + 4], h[4 * e + 5], h[4 * e + 6], h[4 * e + 7]);
+                                }
+                            }
                         }
                     }
                 } else {
@@ -342,7 +383,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                         uint32_t o[32];
                         tmem_ld32(to + d, o);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4*>(part + row * D + d + 4 * e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        for (int e = 0; e < 4; ++e) store32(part + row * D + d + 8 * e, o + 8 * e);
                     }
                     part[T::kRows * D + row] = m;
                     part[T::kRows * D + T::kRows + row] = sum;
@@ -517,11 +558,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                         umma_f16_lo(tmem + T::kS + N * slot, umma_desc_lo(sbase + T::kOffQ + (t * NB + pn) * T::kPanelQ) + 2 * k, umma_desc_lo(sbase + T::kOffK + stage * T::kStage + pn * T::kPanelKV) + 2 * k, kIdescS, pn + k > 0);
                 umma_commit(sf(slot));
             };
-            const auto value = [&](int t, int stage, int slot, bool add) {
+            const auto value = [&](int t, int stage, int slot, bool add, int half) {
 #pragma unroll
-                for (int k = 0; k < N / 16; ++k)
+                for (int k = half * (N / 32); k < (half + 1) * (N / 32); ++k)
                     umma_f16_ta(tmem + T::kO + D * t, tmem + T::kS + N * slot + 8 * k, ((sbase + T::kOffV + stage * T::kStage + 2048 * k) >> 4) | ((uint32_t)(T::kPanelKV >> 4) << 16), kIdescO, add || k > 0);
-                umma_commit(of(slot));
+                if (half) umma_commit(of(slot));
             };
             uint32_t it = rd.it0;
             bool ok = true;
@@ -549,9 +590,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         const int slot = NT == 2 ? t : it & 1;
-                        if (!(ok = mbar_wait_hot(pf(slot), NT == 2 ? it & 1 : (it >> 1) & 1, abort_flag, 0xA80 + slot))) break;
-                        tc_fence_after();
-                        value(t, it & 1, slot, j > 0);
+                        for (int half = 0; half < 2; ++half) {
+                            if (!(ok = mbar_wait_hot(pf(slot, half), NT == 2 ? it & 1 : (it >> 1) & 1, abort_flag, 0xA80 + 2 * slot + half))) break;
+                            tc_fence_after();
+                            value(t, it & 1, slot, j > 0, half);
+                        }
+                        if (!ok) break;
                         if (t == NT - 1) umma_commit(ve(it & 1));
                         if (NT == 2 && more) {
                             if (t == 0 && !(ok = mbar_wait_hot(kf(nx & 1), (nx >> 1) & 1, abort_flag, 0xA62))) break;

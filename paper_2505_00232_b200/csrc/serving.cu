@@ -234,7 +234,7 @@ cudaError_t launch_attention(const PagedAttnParams& p, bool tiles, int device, c
     cudaError_t e = tiles ? launch(paged_tiles_kernel<D, CAP>, p, dim3(p.grid), dim3(kTileThreads), 1024 + T::kOffPre + (p.batch.B + 1) * 4, st, 1, pdl)
                           : launch(paged_attention_kernel<D, CAP>, p, dim3(p.grid), dim3(kAttnWarps * 32), AttnRing<D>::kBytes + (p.batch.B + 1) * 4, st, 1, pdl);
     if (e != cudaSuccess) return e;
-    return tiles ? launch(paged_combine_kernel<D, T::kRows>, p, dim3(p.grid, T::kRows / 8), dim3(256), 0, st, 1, pdl) : launch(paged_combine_kernel<D, kAttnCols>, p, dim3(p.grid), dim3(256), 0, st, 1, pdl);
+    return tiles ? launch(paged_combine_kernel<D, T::kRows, 4>, p, dim3(p.grid, T::kRows / 32), dim3(256), 0, st, 1, pdl) : launch(paged_combine_kernel<D, kAttnCols, 1>, p, dim3(p.grid), dim3(256), 0, st, 1, pdl);
 }
 
 }  // namespace
@@ -256,7 +256,7 @@ extern "C" ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q, i
     if (B == 0 || T == 0 || max_q == 0) return QL_OK;
     const int32_t d = h->d.d_h;
     if (!rows_ok(q, q_ld, (int64_t)h_q * d) || !rows_ok(out, out_ld, (int64_t)h_q * d) || q == out) return QL_ERR_INVALID_ARG;
-    if (!workspace || !aligned(workspace, 16) || workspace_bytes < a.bytes) return QL_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 32) || workspace_bytes < a.bytes) return QL_ERR_INVALID_ARG;
     if (timed_out(h)) return QL_ERR_DEVICE_TIMEOUT;
     DeviceGuard guard(h->device);
     if (!guard.ok) { cudaGetLastError(); return QL_ERR_CUDA; }
