@@ -353,7 +353,7 @@ ql_status qlinear_rope_tables(float* cos_dev, float* sin_dev, int32_t first, int
  * Asynchronous, allocate nothing; appends must be ordered against the calls that read the same pages.
  * Errors: QL_ERR_INVALID_ARG, QL_ERR_UNSUPPORTED (create: the descriptor), QL_ERR_CUDA, QL_ERR_DEVICE_TIMEOUT (see qlinear_forward; qlinear_paged_device_status is
  * qlinear_device_status for this handle's device). */
-#define QL_PAGED_MAX_SEQUENCES 4096
+#define QL_PAGED_MAX_SEQUENCES 2048
 typedef struct qlinear_paged_s* qlinear_paged_t;
 typedef struct {
     int32_t n_pages, page_size, h_kv, d_h;

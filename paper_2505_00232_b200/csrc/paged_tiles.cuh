@@ -2,16 +2,17 @@
 // products on the 5th-generation tensor cores.
 //
 // A CTA works on a segment: 256 query rows (row = token * group + head of the group; 128 rows at d_h 256) of one KV head, and steps through the keys that any of
-// them sees, 128 (64) at a time.  Per step and tile of 128 rows:
+// them sees, 64 at a time.  Per step and tile of 128 rows:
 //     S = Q K^T      tcgen05.mma, both operands in shared memory, S in tensor memory (fp32)
 //     P = exp2(S c - m) as fp16, written over S in tensor memory by the softmax warps, a thread per row
 //     O += P V       tcgen05.mma with P from tensor memory, O in tensor memory (fp32)
-// so the scores never leave the SM and no thread needs another's row.  The maximum m of a row is raised, and O rescaled, only when it is passed by 2^8; O is
-// free for that when S is complete (the products of a CTA are complete in order).  Keys and values are unpacked from the cache's integers by warps of their own
+// so the scores never leave the SM and no thread needs another's row.  A tile has two buffers of S: the scores of the next step are computed while the softmax has
+// the last ones, which never waits for the tensor core then (steps of 128 keys with one buffer per tile: 1073 TFLOP/s, a chunk of 4096 at 16384; the two tiles ran in
+// step, softmax and products in turn).  The maximum m of a row is raised, and O rescaled, only when it is passed by 2^8.  Keys and values are unpacked from the cache's integers by warps of their own
 // to fp16(q s), which go to shared memory in the operands' swizzled layout: K as rows of elements, V as rows of elements too, read transposed.
 //
-// Warps 0-3, 4-7: softmax of the two tiles (at d_h 256 one tile of 128 rows with two buffers of S, and warps 4-7 unpack as well); warps 8-11: unpack;
-// warp 12: issues the products.  The two tiles alternate: while one's softmax runs, the tensor core has the other's products.
+// Warps 0-3, 4-7: softmax of the two tiles (at d_h 256 there is one); warps 8-15: unpack; warps 16 and 17 issue the two products; warp 18 looks up the pages and
+// requests the blocks of 16 tokens (bulk copies to a ring of raw steps in shared memory), so that nothing else waits for global memory between two segments.
 //
 // Work: the segments of the whole batch, numbered through, each as long as its steps and kTileOverhead more (queries in, rows out, an empty pipeline), in one span of
 // equal length per CTA, as in paged_attention.cuh; a segment cut by a span's end leaves its rows' (m, l, O) in the workspace for paged_combine_kernel.
@@ -29,20 +30,25 @@ namespace ql {
 
 template <int D> struct TileShape {
     static constexpr int NT = D == 256 ? 1 : 2;                          // tiles of 128 rows
-    static constexpr int N = D == 256 ? 64 : 128;                        // keys of a step
+    static constexpr int N = 64;                                         // keys of a step
+    static constexpr int kSlots = D == 256 ? 3 : D == 128 ? 6 : 8;       // operands in shared memory: K and V of the steps in turn
+    static constexpr int kRaw = D == 256 ? 3 : 4;                        // raw steps
     static constexpr int NB = D / 64;                                    // panels of 64 elements
     static constexpr int kRows = 128 * NT;
     static constexpr int kBlocks = N / kPagedBlock;                      // blocks of 16 tokens of a step
-    static constexpr int kUnpackWarps = NT == 2 ? 4 : 8;
+    static constexpr int kUnpackWarps = kBlocks * NB < 8 ? kBlocks * NB : 8;
     static constexpr int kItems = kBlocks * NB / kUnpackWarps;           // (block, panel) pairs of a warp and step
     static constexpr int kPanelQ = 128 * 128, kPanelKV = N * 128;        // bytes
-    static constexpr int kQ = NT * NB * kPanelQ, kStage = NB * kPanelKV;
+    static constexpr int kQ = NT * NB * kPanelQ, kSlot = NB * kPanelKV, kRawStep = kBlocks * paged_block_bytes(D);
     static constexpr int kMaxSegments = 64;                              // of a CTA between two meetings
-    static constexpr int kOffQ = 0, kOffK = kQ, kOffV = kOffK + 2 * kStage, kOffPre = kOffV + 2 * kStage;
-    static constexpr uint32_t kO = NT == 2 ? 256 : 0, kS = NT == 2 ? 0 : 256;             // columns of tensor memory
+    static constexpr int kOffQ = 0, kOffKV = kQ, kOffRaw = kOffKV + kSlots * kSlot, kOffPre = kOffRaw + kRaw * kRawStep;
+    static constexpr uint32_t kS = 0, kO = NT * 2 * N;                   // columns of tensor memory: two buffers of S per tile, O
 };
-constexpr int kTileThreads = 512;
-constexpr int kTileOverhead = 3;                                         // a segment without steps, in steps
+constexpr int kTileThreads = 640;
+#ifndef TOV
+#define TOV 8
+#endif
+constexpr int kTileOverhead = TOV;                                         // a segment without steps, in steps
 
 struct TileSegment {
     int32_t head, row0, n_rows, t0, pos0, end, step0, n, slot;           // rows of the sequence row0 .. (n_rows of it), row 0's token and position, keys [.., end), steps step0 .. + n
@@ -93,10 +99,11 @@ __device__ __forceinline__ void store32(void* p, const uint32_t r[8])
 {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
-// A wait of a whole warp: its lanes agree on the outcome (what follows is warp-collective).
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t code) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, code)); }
 template <int R> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
 template <int R> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+constexpr int kTileRegisters = 96;                                       // of a thread at launch: 5 x 96 = 2 x 128 + 2 x 80 + 64 per four warps
+// A wait of a whole warp: its lanes agree on the outcome (what follows is warp-collective).
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t code) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, code)); }
 
 __device__ __forceinline__ int tile_length(int steps) { return steps > 0 ? steps + kTileOverhead : 0; }
 
@@ -120,7 +127,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
     extern __shared__ __align__(128) uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     int* pre = reinterpret_cast<int*>(smem + T::kOffPre);                // [B + 1]: length of the row tiles (per head) before sequence b
-    __shared__ __align__(8) uint64_t bars[19];
+    __shared__ __align__(8) uint64_t bars[2 * T::kSlots + 2 * T::kRaw + 15];
     __shared__ TileSegment segs[T::kMaxSegments];
     __shared__ int n_segs;
     __shared__ int64_t round_end;
@@ -128,29 +135,29 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
     __shared__ volatile uint32_t abort_flag[4];
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, c = lane & 3;
     const uint32_t bar0 = smem_u32(bars);
-    // barriers: K, V full and empty (two stages), S, the halves of P and O per buffer, Q per tile, the end
-    const auto kf = [&](int s) { return bar0 + 8 * s; };
-    const auto ke = [&](int s) { return bar0 + 8 * (2 + s); };
-    const auto vf = [&](int s) { return bar0 + 8 * (4 + s); };
-    const auto ve = [&](int s) { return bar0 + 8 * (6 + s); };
-    const auto sf = [&](int s) { return bar0 + 8 * (8 + s); };
-    const auto pf = [&](int s, int half) { return bar0 + 8 * (half ? 17 + s : 10 + s); };
-    const auto of = [&](int s) { return bar0 + 8 * (12 + s); };
-    const auto qf = [&](int t) { return bar0 + 8 * (14 + t); };
-    const uint32_t done = bar0 + 8 * 16;
+    // barriers: operand slots and raw steps full and empty; S, P and O per buffer (2 t + slot); Q per tile; the end
+    constexpr int NS = T::kSlots, NR = T::kRaw;
+    const auto full = [&](uint32_t s) { return bar0 + 8 * s; };
+    const auto empty = [&](uint32_t s) { return bar0 + 8 * (NS + s); };
+    const auto rf = [&](uint32_t s) { return bar0 + 8 * (2 * NS + s); };
+    const auto re = [&](uint32_t s) { return bar0 + 8 * (2 * NS + NR + s); };
+    const uint32_t bar1 = bar0 + 8 * (2 * NS + 2 * NR);
+    const auto sf = [&](int s) { return bar1 + 8 * s; };
+    const auto pf = [&](int s) { return bar1 + 8 * (4 + s); };
+    const auto of = [&](int s) { return bar1 + 8 * (8 + s); };
+    const auto qf = [&](int t) { return bar1 + 8 * (12 + t); };
+    const uint32_t done = bar1 + 8 * 14;
     const uint32_t sbase = smem_u32(smem);
     if (tid == 0) {
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(kf(s), T::kUnpackWarps); mbar_init(vf(s), T::kUnpackWarps);
-            mbar_init(ke(s), 1); mbar_init(ve(s), 1);
-            mbar_init(sf(s), 1); mbar_init(pf(s, 0), 4); mbar_init(pf(s, 1), 4);
-            mbar_init(of(s), 1); mbar_init(qf(s), 4);
-        }
-        mbar_init(done, 1);
+        for (int s = 0; s < NS; ++s) { mbar_init(full(s), T::kUnpackWarps); mbar_init(empty(s), 1); }
+        for (int s = 0; s < NR; ++s) { mbar_init(rf(s), 1); mbar_init(re(s), T::kUnpackWarps); }
+        for (int s = 0; s < 4; ++s) { mbar_init(sf(s), 1); mbar_init(pf(s), 4); mbar_init(of(s), 1); }
+        mbar_init(qf(0), 4); mbar_init(qf(1), 4);
+        mbar_init(done, 2);
         abort_flag[0] = abort_flag[1] = abort_flag[2] = abort_flag[3] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) tmem_alloc(smem_u32(&tmem_slot), 512);
+    if (warp == 16) tmem_alloc(smem_u32(&tmem_slot), 512);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (tid == 0) abort_flag[2] = abort_flag[3] = 1;                     // (from here on, waiting counts against the time limit)
@@ -200,9 +207,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
     const int64_t total = (int64_t)pre[bt.B] * bt.h_kv, span = max((total + p.grid - 1) / p.grid, (int64_t)1);
     const int64_t w_first = (int64_t)blockIdx.x * span, w_end = min(total, w_first + span);
-    if (tid == 12 * 32) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    if (tid == 16 * 32) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
 
-    // Rounds of at most kMaxSegments segments; every role has a loop of its own (its share of the registers).
+    // Rounds of at most kMaxSegments segments; every role has a loop of its own.
     struct Round { int64_t w; uint32_t it0, seg0, steps; int n; bool on; } rd{w_first, 0, 0, 0, 0, w_first < w_end};
     const auto begin_round = [&]() {                                     // (the list is complete)
         __syncwarp();
@@ -220,8 +227,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
         rd.on = rd.w < w_end && !abort_flag[0];
         __syncthreads();                                                 // (the list may be written again)
     };
-    if (warp < 4 * NT) {
-        more_registers<192>();
+    if (warp < 8) {
+        more_registers<128>();
+        while (rd.on && warp >= 4 * NT) { begin_round(); end_round(); }
         while (rd.on) {
         begin_round();
             // ================================================================ softmax: thread = row
@@ -280,8 +288,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                         pg = page_of(s.step0 + j + kAhead);
                     }
                     const uint32_t blocks = (held_blocks >> (T::kBlocks * (j % kAhead))) & ((1u << T::kBlocks) - 1);
-                    const int slot = NT == 2 ? t : it & 1;
-                    if (!warp_wait(sf(slot), NT == 2 ? it & 1 : (it >> 1) & 1, abort_flag, 0xA00 + slot)) { ok = false; break; }
+                    const int slot = 2 * t + (it & 1);
+                    if (!warp_wait(sf(slot), (it >> 1) & 1, abort_flag, 0xA00 + slot)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t ts = tmem + lanes + T::kS + N * slot;
                     float x[N];
@@ -309,10 +317,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                         m = mn;
                         l[0].x *= f; l[0].y *= f; l[1].x *= f; l[1].y *= f;
                         if (j > 0) {
-                            if (NT == 1) {                               // (S of this step may be complete before the values of the one before)
-                                if (!warp_wait(of((it - 1) & 1), ((it - 1) >> 1) & 1, abort_flag, 0xA10)) { ok = false; break; }
-                                tc_fence_after();
-                            }
+                            // (S of this step is complete before the values of the one before)
+                            if (!warp_wait(of(2 * t + ((it - 1) & 1)), ((it - 1) >> 1) & 1, abort_flag, 0xA10 + t)) { ok = false; break; }
+                            tc_fence_after();
 #pragma unroll 1
                             for (int d = 0; d < D; d += 16) {
                                 uint32_t o[16];
@@ -323,32 +330,28 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                             }
                         }
                     }
-                    // weights: in halves, so that the product with the values begins with the first
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
+                    for (int e = 0; e < N; e += 32) {
+                        uint32_t h[16];
 #pragma unroll
-                        for (int e = half * (N / 2); e < (half + 1) * (N / 2); e += 32) {
-                            uint32_t h[16];
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) {
-                                float2 y = fma2(x[e + 2 * k], x[e + 2 * k + 1], cc, -m);
-                                y.x = exp2_fast(y.x);
-                                y.y = exp2_fast(y.y);
-                                l[k & 1] = add2(l[k & 1], y);
-                                const __half2 ab = __floats2half2_rn(y.x, y.y);
-                                h[k] = *reinterpret_cast<const uint32_t*>(&ab);
-                            }
-                            tmem_st16_async(ts + e / 2, h);
+                        for (int k = 0; k < 16; ++k) {
+                            float2 y = fma2(x[e + 2 * k], x[e + 2 * k + 1], cc, -m);
+                            y.x = exp2_fast(y.x);
+                            y.y = exp2_fast(y.y);
+                            l[k & 1] = add2(l[k & 1], y);
+                            const __half2 ab = __floats2half2_rn(y.x, y.y);
+                            h[k] = *reinterpret_cast<const uint32_t*>(&ab);
                         }
-                        tmem_st_wait();
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(pf(slot, half));
+                        tmem_st16_async(ts + e / 2, h);
                     }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(pf(slot));
                 }
                 if (!ok) break;
                 if (si + 1 < rd.n) load_q(segs[si + 1]);                    // (every product with this segment's queries is complete)
-                if (!warp_wait(of(NT == 2 ? t : (it - 1) & 1), NT == 2 ? (it - 1) & 1 : ((it - 1) >> 1) & 1, abort_flag, 0xA20 + t)) { ok = false; break; }
+                if (!warp_wait(of(2 * t + ((it - 1) & 1)), ((it - 1) >> 1) & 1, abort_flag, 0xA20 + t)) { ok = false; break; }
                 tc_fence_after();
                 const float sum = (l[0].x + l[0].y) + (l[1].x + l[1].y);
                 if (s.slot < 0) {
@@ -392,67 +395,39 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
             }
         end_round();
         }
-    } else if (warp < 12) {
-        fewer_registers<88>();
+    } else if (warp < 16) {
+        fewer_registers<80>();
+        while (rd.on && warp >= 8 + T::kUnpackWarps) { begin_round(); end_round(); }
         while (rd.on) {
         begin_round();
-            // ================================================================ unpack: K and V of every step to shared memory
-            const int uw = warp - 4 * NT;
-            // this warp's (block, panel) pairs: pair kItems * uw + i, panels innermost
-            uint4 kw[T::kItems], vw[T::kItems];
-            uint2 ks[T::kItems], vs[T::kItems];
-            int si_l = 0, j_l = 0;                                       // the step whose integers are requested next
-            int si_p = 0, j_p = 0, pg = -1;                              // the step whose pages are looked up next; the pages of the one before (lane: block)
-            const auto next = [&](int& si, int& j) { if (++j == segs[si].n) { j = 0; ++si; } };
-            const auto look_up = [&]() {
-                if (si_p >= rd.n) return;
-                const int at = ((segs[si_p].step0 + j_p) * T::kBlocks + (lane & (T::kBlocks - 1))) >> bt.log2_blocks;
-                const int v = at < bt.table_width ? bt.table[segs[si_p].table + at] : -1;
-                pg = v >= 0 && v < bt.n_pages ? v : 0;                   // (scores of blocks without a page are hidden: any page will do)
-                next(si_p, j_p);
-            };
-            const auto block_of = [&](int i, int step, int head) {
-                const int blk = (T::kItems * uw + i) / NB, u = step * T::kBlocks + blk;
-                const int page = __shfl_sync(0xffffffffu, pg, blk);
-                return bt.pool + ((((int64_t)page * bt.h_kv + head) << bt.log2_blocks) + (u & ((1 << bt.log2_blocks) - 1))) * paged_block_bytes(D);
-            };
-            const uint8_t* src[T::kItems];
-            const auto request_k = [&]() {
-#pragma unroll
-                for (int i = 0; i < T::kItems; ++i) {
-                    const int pn = (T::kItems * uw + i) % NB;
-                    src[i] = block_of(i, segs[si_l].step0 + j_l, segs[si_l].head);
-                    kw[i] = *reinterpret_cast<const uint4*>(src[i] + 512 * pn + 16 * lane);
-                    ks[i] = *reinterpret_cast<const uint2*>(src[i] + paged_k_scales(D) + g * (8 * NB) + 8 * pn);
-                }
-            };
-            const auto request_v = [&]() {
-#pragma unroll
-                for (int i = 0; i < T::kItems; ++i) {
-                    const int pn = (T::kItems * uw + i) % NB;
-                    vw[i] = *reinterpret_cast<const uint4*>(src[i] + paged_v_data(D) + 512 * pn + 16 * lane);
-                    vs[i] = *reinterpret_cast<const uint2*>(src[i] + paged_v_scales(D) + (2 * pn + (g >> 2)) * 32 + 8 * c);
-                }
-            };
+            // ================================================================ unpack: K and V of every step from the raw blocks to the operands' layout
+            const int uw = warp - 8;                                     // this warp's (block, panel) pairs: pair kItems * uw + i, panels innermost
             const auto put = [&](uint8_t* row, int chunk, uint32_t word, uint32_t scale) {
                 uint32_t h[4];
                 unpack_int4_word(word, h);
                 *reinterpret_cast<uint4*>(row + chunk * 16) = make_uint4(h2_mul(h[0], scale), h2_mul(h[1], scale), h2_mul(h[2], scale), h2_mul(h[3], scale));
             };
-            if (rd.steps > 0) {
-                look_up();
-                request_k();
-                request_v();
-                look_up();
-                next(si_l, j_l);
-            }
             for (uint32_t q = 0; q < rd.steps; ++q) {
-                const uint32_t it = rd.it0 + q, st = it & 1, par = ((it >> 1) & 1) ^ 1;
-                if (!warp_wait(ke(st), par, abort_flag, 0xA30 + st)) break;
+                const uint32_t it = rd.it0 + q, rs = it % NR, nk = 2 * it, nv = 2 * it + 1, sk = nk % NS, sv = nv % NS;
+                if (!warp_wait(rf(rs), (it / NR) & 1, abort_flag, 0xA30 + rs)) break;
+                uint4 kw[T::kItems], vw[T::kItems];
+                uint2 ks[T::kItems], vs[T::kItems];
 #pragma unroll
                 for (int i = 0; i < T::kItems; ++i) {
                     const int item = T::kItems * uw + i, blk = item / NB, pn = item % NB;
-                    uint8_t* panel = smem + T::kOffK + st * T::kStage + pn * T::kPanelKV + (16 * blk + g) * 128;
+                    const uint8_t* src = smem + T::kOffRaw + rs * T::kRawStep + blk * paged_block_bytes(D);
+                    kw[i] = *reinterpret_cast<const uint4*>(src + 512 * pn + 16 * lane);
+                    ks[i] = *reinterpret_cast<const uint2*>(src + paged_k_scales(D) + g * (8 * NB) + 8 * pn);
+                    vw[i] = *reinterpret_cast<const uint4*>(src + paged_v_data(D) + 512 * pn + 16 * lane);
+                    vs[i] = *reinterpret_cast<const uint2*>(src + paged_v_scales(D) + (2 * pn + (g >> 2)) * 32 + 8 * c);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(re(rs));
+                if (!warp_wait(empty(sk), ((nk / NS) & 1) ^ 1, abort_flag, 0xA40)) break;
+#pragma unroll
+                for (int i = 0; i < T::kItems; ++i) {
+                    const int item = T::kItems * uw + i, blk = item / NB, pn = item % NB;
+                    uint8_t* panel = smem + T::kOffKV + sk * T::kSlot + pn * T::kPanelKV + (16 * blk + g) * 128;
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {                        // (the group by the row's parity: 8 lanes of a store have 8 chunks)
                         const bool second = (k ^ g) & 1;
@@ -464,14 +439,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                 }
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(kf(st));
-                const bool more = q + 1 < rd.steps;
-                if (more) request_k();
-                if (!warp_wait(ve(st), par, abort_flag, 0xA40 + st)) break;
+                if (lane == 0) mbar_arrive(full(sk));
+                if (!warp_wait(empty(sv), ((nv / NS) & 1) ^ 1, abort_flag, 0xA41)) break;
 #pragma unroll
                 for (int i = 0; i < T::kItems; ++i) {
                     const int item = T::kItems * uw + i, blk = item / NB, pn = item % NB;
-                    uint8_t* panel = smem + T::kOffV + st * T::kStage + pn * T::kPanelKV;
+                    uint8_t* panel = smem + T::kOffKV + sv * T::kSlot + pn * T::kPanelKV;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int row = 2 * c + (k & 1) + 8 * (k >> 1);
@@ -481,18 +454,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                 }
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(vf(st));
-                if (more) {
-                    request_v();
-                    look_up();
-                    next(si_l, j_l);
-                }
+                if (lane == 0) mbar_arrive(full(sv));
             }
         end_round();
         }
     } else {
-        fewer_registers<40>();                                           // (one instruction for the four warps)
-        while (rd.on && warp == 12) {
+        fewer_registers<64>();                                           // (one instruction for the four warps)
+        while (rd.on && warp == 16) {
         // ---- the next segments: (sequence, row tile, KV head), and the part of the steps that lies in the span
         {
             int n = 0;
@@ -547,77 +515,118 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
             if (lane == 0) n_segs = n;
         }
         begin_round();
-        if (lane == 0) {
-            // ================================================================ the products
-            constexpr uint32_t kIdescS = umma_idesc_f16(N), kIdescO = umma_idesc_f16(D) | (1u << 16);   // (V is transposed)
-            const auto score = [&](int t, int stage, int slot) {
-#pragma unroll
-                for (int pn = 0; pn < NB; ++pn)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        umma_f16_lo(tmem + T::kS + N * slot, umma_desc_lo(sbase + T::kOffQ + (t * NB + pn) * T::kPanelQ) + 2 * k, umma_desc_lo(sbase + T::kOffK + stage * T::kStage + pn * T::kPanelKV) + 2 * k, kIdescS, pn + k > 0);
-                umma_commit(sf(slot));
-            };
-            const auto value = [&](int t, int stage, int slot, bool add, int half) {
-#pragma unroll
-                for (int k = half * (N / 32); k < (half + 1) * (N / 32); ++k)
-                    umma_f16_ta(tmem + T::kO + D * t, tmem + T::kS + N * slot + 8 * k, ((sbase + T::kOffV + stage * T::kStage + 2048 * k) >> 4) | ((uint32_t)(T::kPanelKV >> 4) << 16), kIdescO, add || k > 0);
-                if (half) umma_commit(of(slot));
-            };
+        {
+            // ================================================================ S = Q K^T: the warp runs the loop together, one lane issues
+            constexpr uint32_t kIdesc = umma_idesc_f16(N);
+            const uint32_t q_lo = umma_desc_lo(sbase + T::kOffQ), k_lo = umma_desc_lo(sbase + T::kOffKV);
             uint32_t it = rd.it0;
             bool ok = true;
             for (int si = 0; si < rd.n && ok; ++si) {
                 const int steps = segs[si].n;
-                for (int t = 0; t < NT && ok; ++t) ok = mbar_wait(qf(t), (rd.seg0 + si) & 1, abort_flag, 0xA50 + t);
-                ok = ok && mbar_wait_hot(kf(it & 1), (it >> 1) & 1, abort_flag, 0xA60);
-                if (!ok) break;
-                if (NT == 2) {
-                    score(0, it & 1, 0);
-                    score(1, it & 1, 1);
-                } else {
-                    score(0, it & 1, it & 1);
-                }
-                umma_commit(ke(it & 1));
-                for (int j = 0; j < steps; ++j, ++it) {
-                    const bool more = j + 1 < steps;
-                    const uint32_t nx = it + 1;
-                    if (NT == 1 && more) {                               // the next scores first: the softmax has two buffers
-                        if (!(ok = mbar_wait_hot(kf(nx & 1), (nx >> 1) & 1, abort_flag, 0xA61))) break;
-                        score(0, nx & 1, nx & 1);
-                        umma_commit(ke(nx & 1));
-                    }
-                    if (!(ok = mbar_wait_hot(vf(it & 1), (it >> 1) & 1, abort_flag, 0xA70))) break;
+                for (int t = 0; t < NT && ok; ++t) ok = warp_wait(qf(t), (rd.seg0 + si) & 1, abort_flag, 0xA50 + t);
+                for (int j = 0; j < steps && ok; ++j, ++it) {
+                    const uint32_t n = 2 * it, at = n % NS, kd = k_lo + at * (T::kSlot >> 4), sd = tmem + T::kS + N * (it & 1);
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait_hot(full(at), (n / NS) & 1, abort_flag, 0xA60)))) break;
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        const int slot = NT == 2 ? t : it & 1;
-                        for (int half = 0; half < 2; ++half) {
-                            if (!(ok = mbar_wait_hot(pf(slot, half), NT == 2 ? it & 1 : (it >> 1) & 1, abort_flag, 0xA80 + 2 * slot + half))) break;
-                            tc_fence_after();
-                            value(t, it & 1, slot, j > 0, half);
+                        const int slot = 2 * t + (it & 1);
+                        // (the weights of step it - 2 lay in this buffer)
+                        if (it >= 2 && !(ok = __all_sync(0xffffffffu, mbar_wait_hot(of(slot), ((it >> 1) & 1) ^ 1, abort_flag, 0xA64 + slot)))) break;
+                        if (elect_one()) {
+#pragma unroll
+                            for (int pn = 0; pn < NB; ++pn)
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    umma_f16_lo(sd + 2 * N * t, q_lo + (t * NB + pn) * (T::kPanelQ >> 4) + 2 * k, kd + pn * (T::kPanelKV >> 4) + 2 * k, kIdesc, pn + k > 0);
+                            umma_commit(sf(slot));
+                            if (t == NT - 1) umma_commit(empty(at));
                         }
-                        if (!ok) break;
-                        if (t == NT - 1) umma_commit(ve(it & 1));
-                        if (NT == 2 && more) {
-                            if (t == 0 && !(ok = mbar_wait_hot(kf(nx & 1), (nx >> 1) & 1, abort_flag, 0xA62))) break;
-                            score(t, nx & 1, t);
-                            if (t == 1) umma_commit(ke(nx & 1));
-                        }
+                        __syncwarp();
                     }
-                    if (!ok) break;
                 }
             }
         }
         end_round();
         }
-        while (rd.on) { begin_round(); end_round(); }                    // (warps 13 to 15)
+        while (rd.on && warp == 17) {
+        begin_round();
+        {
+            // ================================================================ O += P V
+            constexpr uint32_t kIdesc = umma_idesc_f16(D) | (1u << 16);  // (V is transposed)
+            const uint32_t v_lo = ((sbase + T::kOffKV) >> 4) | ((uint32_t)(T::kPanelKV >> 4) << 16);
+            uint32_t it = rd.it0;
+            bool ok = true;
+            for (int si = 0; si < rd.n && ok; ++si) {
+                const int steps = segs[si].n;
+                for (int j = 0; j < steps && ok; ++j, ++it) {
+                    const uint32_t n = 2 * it + 1, at = n % NS, vd = v_lo + at * (T::kSlot >> 4), pd = tmem + T::kS + N * (it & 1), add = j > 0;
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait_hot(full(at), (n / NS) & 1, abort_flag, 0xA70)))) break;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const int slot = 2 * t + (it & 1);
+                        if (!(ok = __all_sync(0xffffffffu, mbar_wait_hot(pf(slot), (it >> 1) & 1, abort_flag, 0xA80 + slot)))) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < N / 16; ++k) umma_f16_ta(tmem + T::kO + D * t, pd + 2 * N * t + 8 * k, vd + (2048 >> 4) * k, kIdesc, k > 0 ? 1u : add);
+                            umma_commit(of(slot));
+                            if (t == NT - 1) umma_commit(empty(at));
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+        }
+        end_round();
+        }
+        while (rd.on && warp == 18) {
+        begin_round();
+        {
+            // ================================================================ the raw blocks: pages of eight steps looked up at once (lane kBlocks * step + block), eight steps ahead
+            constexpr uint32_t kWindow = 32 / T::kBlocks;
+            int si = 0, j = 0, si_w = 0, j_w = 0, pages = 0, pages_next = -1;
+            const auto look_up = [&]() {
+                int sl = si_w, jl = j_w + lane / T::kBlocks;
+                while (sl < rd.n && jl >= segs[sl].n) jl -= segs[sl++].n;
+                pages_next = -1;
+                if (sl < rd.n) {
+                    const int at = ((segs[sl].step0 + jl) * T::kBlocks + (lane & (T::kBlocks - 1))) >> bt.log2_blocks;
+                    if (at < bt.table_width) pages_next = bt.table[segs[sl].table + at];
+                }
+                j_w += kWindow;
+                while (si_w < rd.n && j_w >= segs[si_w].n) j_w -= segs[si_w++].n;
+            };
+            look_up();
+            uint32_t q = 0;
+            for (; q < rd.steps; ++q) {
+                const uint32_t it = rd.it0 + q, rs = it % NR;
+                if (q % kWindow == 0) {
+                    pages = pages_next >= 0 && pages_next < bt.n_pages ? pages_next : 0;   // (scores of blocks without a page are hidden: any page will do)
+                    look_up();
+                }
+                const int page = __shfl_sync(0xffffffffu, pages, (q % kWindow) * T::kBlocks + (lane & (T::kBlocks - 1))), at = (segs[si].step0 + j) * T::kBlocks + lane;
+                const uint8_t* src = bt.pool + ((((int64_t)page * bt.h_kv + segs[si].head) << bt.log2_blocks) + (at & ((1 << bt.log2_blocks) - 1))) * paged_block_bytes(D);
+                if (++j == segs[si].n) { j = 0; ++si; }
+                if (!warp_wait(re(rs), ((it / NR) & 1) ^ 1, abort_flag, 0xA90 + rs)) break;
+                if (lane == 0) mbar_expect_tx(rf(rs), T::kRawStep);
+                __syncwarp();
+                if (lane < T::kBlocks) bulk_copy_g2s(sbase + T::kOffRaw + rs * T::kRawStep + lane * paged_block_bytes(D), src, paged_block_bytes(D), rf(rs));
+            }
+            if (abort_flag[0])                                           // (let the copies on their way arrive before the CTA leaves)
+                for (uint32_t k = q > NR ? q - NR : 0; k < q; ++k) mbar_wait(rf((rd.it0 + k) % NR), ((rd.it0 + k) / NR) & 1, abort_flag + 1, 0);
+        }
+        end_round();
+        }
+        while (rd.on) { begin_round(); end_round(); }                    // (warp 19)
     }
     // every product has to be complete before the memory it reads and writes is given back
-    if (tid == 12 * 32) {
-        umma_commit(done);
+    if (warp == 16 || warp == 17) {
+        if (elect_one()) umma_commit(done);
+        __syncwarp();
         mbar_wait(done, 0, abort_flag + 1, 0);
     }
     __syncthreads();
-    if (warp == 12) tmem_dealloc(tmem, 512);
+    if (warp == 16) tmem_dealloc(tmem, 512);
 }
 
 }  // namespace ql

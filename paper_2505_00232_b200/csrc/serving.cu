@@ -223,12 +223,12 @@ cudaError_t launch_attention(const PagedAttnParams& p, bool tiles, int device, c
     static std::atomic<bool> flags[64];
     constexpr int kMost = AttnRing<D>::kBytes + (QL_PAGED_MAX_SEQUENCES + 1) * 4, kMostTiles = 1024 + T::kOffPre + (QL_PAGED_MAX_SEQUENCES + 1) * 4;
     if (!flags[device].load(std::memory_order_acquire)) {
-        cudaFuncAttributes at;
         cudaError_t e = cudaFuncSetAttribute(paged_attention_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_tiles_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostTiles);
+        cudaFuncAttributes at;
         if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, paged_tiles_kernel<D, CAP>);
         if (e != cudaSuccess) return e;
-        if (at.numRegs < 128) return cudaErrorInvalidConfiguration;      // (the roles' shares are taken from what the block was launched with: a smaller sum would be waited for)
+        if (at.numRegs < kTileRegisters) return cudaErrorInvalidConfiguration;   // (the roles' shares come from what the block was launched with: they would be waited for)
         flags[device].store(true, std::memory_order_release);
     }
     cudaError_t e = tiles ? launch(paged_tiles_kernel<D, CAP>, p, dim3(p.grid), dim3(kTileThreads), 1024 + T::kOffPre + (p.batch.B + 1) * 4, st, 1, pdl)
