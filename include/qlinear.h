@@ -379,7 +379,7 @@ ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q_dev, int64_t 
  *     listed in the row's biases:        x = x + bias_values[i], i the last entry of v among bias_ids[bias_start[r]] .. bias_ids[bias_start[r + 1] - 1]
  *     bit v % 32 of mask[r, v / 32] 0:   x = -infinity (whatever the logit was, NaN too)
  * and out[r, v] = x in the logits' type (fp16, or fp32 with is_fp32).  tokens (with start), bias_ids (with values and start) and mask may be NULL: nothing of the kind; repetition NULL: 1,
- * presence, frequency NULL: 0.  Tokens and ids outside [0, vocab) are passed over.  logits_dev, out_dev: rows of leading dimension ld, out_ld >= vocab, any alignment; out_dev may be
+ * presence, frequency NULL: 0.  Tokens and ids outside [0, vocab) are passed over; of more than 65535 bias entries a row the last 65535 count.  logits_dev, out_dev: rows of leading dimension ld, out_ld >= vocab, any alignment; out_dev may be
  * logits_dev with ld == out_ld, and must not overlap it otherwise.  mask int32 words, mask_ld >= ceil(vocab / 32) of them a row.  rows <= 65535.
  * Asynchronous, allocates nothing.  Errors: QL_ERR_INVALID_ARG, QL_ERR_ARCH, QL_ERR_CUDA. */
 ql_status qlinear_adjust_logits(const void* logits_dev, int64_t ld, void* out_dev, int64_t out_ld, int32_t rows, int32_t vocab, int32_t is_fp32,

@@ -63,25 +63,22 @@ __device__ __forceinline__ uint8_t* paged_block(const PagedBatch& p, int b, int 
 }
 
 constexpr int kPagedThreads = 256;
+constexpr int kPagedMostRows = 8;                                        // rows of the call that a CTA takes
 
-// Which sequence row t of the call belongs to, and its position there; false for a row of none.  Every thread of the CTA takes part.
-__device__ __forceinline__ bool paged_locate(const PagedBatch& p, int t, int* seq, int* position)
+// Which sequences the rows t0 .. t0 + n - 1 (n <= kPagedMostRows) of the call belong to (seq[i], -1: none), and their positions there.  Every thread of the CTA takes part.
+__device__ __forceinline__ void paged_locate(const PagedBatch& p, int t0, int n, int* seq, int* position)
 {
-    __shared__ int found[2];
-    if (threadIdx.x == 0) found[0] = -1;
+    if (threadIdx.x < n) seq[threadIdx.x] = -1;
     __syncthreads();
     for (int b = threadIdx.x; b < p.B; b += blockDim.x) {
         int first;
-        const int n = paged_rows(p, b, &first);
-        if (t >= first && t - first < n) {
-            found[0] = b;
-            found[1] = p.kv_len[b] - n + (t - first);
+        const int rows = paged_rows(p, b, &first);
+        for (int t = max(first, t0); t < min(first + rows, t0 + n); ++t) {
+            seq[t - t0] = b;
+            position[t - t0] = p.kv_len[b] - rows + (t - first);
         }
     }
     __syncthreads();
-    *seq = found[0];
-    *position = found[1];
-    return found[0] >= 0;
 }
 
 struct PagedAppendParams {
@@ -108,99 +105,118 @@ __device__ __forceinline__ void paged_unpack8(const uint4& u, float f[8])
 }
 
 // 8 elements of a group that 4 neighbouring lanes hold: the word, and the group's scale.
+// The integers are those of round-half-even of the IEEE quotient, without dividing: for fp16 numbers x and s, x / s below 7.01 is a tie (a whole number and a half) or at
+// least 2^-14 away from one (2 x and an odd multiple of s are multiples of a unit that is at least 2^-12 of the larger), so a product with the reciprocal, off by less than
+// 2^-18, is right once it has been rounded to a multiple of 2^-15 (the sum with 384), which makes the ties exact again.
 __device__ __forceinline__ uint32_t paged_quantise(const uint4& u, __half* scale)
 {
-    float f[8];
-    paged_unpack8(u, f);
-    float amax = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(f[i]));
+    const __half2* h2 = reinterpret_cast<const __half2*>(&u);
+    const __half2 top = __hmax2(__hmax2(__habs2(h2[0]), __habs2(h2[1])), __hmax2(__habs2(h2[2]), __habs2(h2[3])));
+    float amax = fmaxf(__low2float(top), __high2float(top));
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
     const float s = fminf(__half2float(__float2half_rn(__fdiv_rn(amax, 7.f))), 9352.f);
     *scale = __float2half_rn(s);
+    const float r = s > 0.f ? __frcp_rn(s) : 0.f;
+    float f[8];
+    paged_unpack8(u, f);
     uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int q = s > 0.f ? __float2int_rn(fminf(fmaxf(__fdiv_rn(f[i], s), -7.f), 7.f)) : 0;   // (clamped, then rounded: the same, 7 is a whole number)
-        w |= (uint32_t)(q + 8) << (4 * ((i >> 1) + 4 * (i & 1)));
+        const float t = __fsub_rn(__fadd_rn(fminf(fmaxf(f[i] * r, -7.f), 7.f), 384.f), 384.f);
+        // (the low bits of 1.5 * 2^23 + 8 + a whole number are 8 and that number)
+        w |= (__float_as_uint(__fadd_rn(t, 12582920.f)) & 15u) << (4 * ((i >> 1) + 4 * (i & 1)));
     }
     return w;
 }
 
-// One CTA per row of the call (and, for few rows, per piece of its heads); d / 8 lanes per head, 8 elements each: one 16-byte load, the partner of the
-// two-halves layout by a shuffle, the group's maximum by two.  Every product and sum of the rotation is one rounded fp32 operation, the result is
+// ROWS rows of the call per CTA, one after the other (and, for few rows, a CTA per piece of the heads); d / 8 lanes per head, 8 elements each: one 16-byte load, the partner of
+// the two-halves layout by a shuffle, the group's maximum by two.  A thread has the same elements of several heads: it requests up to kHeads of them at once
+// and reads the angles, the same for all heads, once per row.  Every product and sum of the rotation is one rounded fp32 operation, the result is
 // rounded to fp16 (what the calls that it stands for write), and that is quantised: the integers do not depend on the compiler's contractions.
-__global__ void __launch_bounds__(kPagedThreads) paged_append_kernel(const PagedAppendParams p)
+// Bound: HBM.
+template <int ROWS>
+__global__ void __launch_bounds__(kPagedThreads, ROWS > 1 ? 4 : 1) paged_append_kernel(const PagedAppendParams p)
 {
+    constexpr int kHeads = 3;
+    __shared__ int seq[kPagedMostRows], position[kPagedMostRows];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int t = blockIdx.x, d = p.d;
-    int b, pos;
-    if (!paged_locate(p.batch, t, &b, &pos) || pos < 0) return;
+    const int d = p.d, n = min(ROWS, p.batch.T - (int)blockIdx.x * ROWS);
+    paged_locate(p.batch, blockIdx.x * ROWS, n, seq, position);
     const int log2_lanes = 31 - __clz(d >> 3), lane = threadIdx.x & 31, m = lane & ((1 << log2_lanes) - 1);
     const int h_kv = p.batch.h_kv, rows = p.h_q + 2 * h_kv, per_pass = kPagedThreads >> log2_lanes;
     const int half = p.rot >> 1, hl = half >> 3;                         // the lanes of the first half's elements
-    const int64_t at = (int64_t)min(pos, p.n_pos - 1) * half;
     const int block_bytes = paged_block_bytes(d);
+    const bool turned = p.cos_t && 8 * m < p.rot, low = m < hl;
+    const int partner = p.interleaved ? lane : lane - m + (low ? m + hl : m < 2 * hl ? m - hl : m);
+    const int angle = p.interleaved ? 4 * m : 8 * (low ? m : m - hl);
 
-    for (int base = blockIdx.y * per_pass; base < rows; base += gridDim.y * per_pass) {
-        const int r = base + (threadIdx.x >> log2_lanes);
-        const int kind = r < p.h_q ? 0 : r < p.h_q + h_kv ? 1 : 2, head = kind == 0 ? r : kind == 1 ? r - p.h_q : r - p.h_q - h_kv;
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (r < rows) {
-            const __half* src = kind == 0 ? p.q + t * p.q_ld : kind == 1 ? p.k + t * p.k_ld : p.v + t * p.v_ld;
-            u = *reinterpret_cast<const uint4*>(src + (int64_t)head * d + 8 * m);
-        }
-        if (p.cos_t) {
-            float x[8], y[8], o[8];
-            paged_unpack8(u, x);
-            if (p.interleaved) {
-                if (kind < 2 && 8 * m < p.rot) {
-                    const float4 c = __ldg(reinterpret_cast<const float4*>(p.cos_t + at + 4 * m)), s = __ldg(reinterpret_cast<const float4*>(p.sin_t + at + 4 * m));
-                    const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        o[2 * i] = __fsub_rn(__fmul_rn(x[2 * i], cc[i]), __fmul_rn(x[2 * i + 1], ss[i]));
-                        o[2 * i + 1] = __fadd_rn(__fmul_rn(x[2 * i + 1], cc[i]), __fmul_rn(x[2 * i], ss[i]));
-                    }
-                }
-            } else {
-                const int partner = lane - m + (m < hl ? m + hl : m < 2 * hl ? m - hl : m);
-                uint4 w;
-                w.x = __shfl_sync(0xffffffffu, u.x, partner);
-                w.y = __shfl_sync(0xffffffffu, u.y, partner);
-                w.z = __shfl_sync(0xffffffffu, u.z, partner);
-                w.w = __shfl_sync(0xffffffffu, u.w, partner);
-                paged_unpack8(w, y);
-                if (kind < 2 && 8 * m < p.rot) {
-                    const bool low = m < hl;
-                    const int i0 = 8 * (low ? m : m - hl);
-                    float c[8], s[8];
-#pragma unroll
-                    for (int i = 0; i < 8; i += 4) {
-                        *reinterpret_cast<float4*>(c + i) = __ldg(reinterpret_cast<const float4*>(p.cos_t + at + i0 + i));
-                        *reinterpret_cast<float4*>(s + i) = __ldg(reinterpret_cast<const float4*>(p.sin_t + at + i0 + i));
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] = __fadd_rn(__fmul_rn(x[i], c[i]), __fmul_rn(low ? -y[i] : y[i], s[i]));
-                }
-            }
-            if (kind < 2 && 8 * m < p.rot) {
-                __half2* h = reinterpret_cast<__half2*>(&u);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(o[2 * i], o[2 * i + 1]);
+    for (int i = 0; i < n; ++i) {
+        const int b = seq[i], pos = position[i];
+        if (b < 0 || pos < 0) continue;
+        const int64_t t = (int64_t)blockIdx.x * ROWS + i;
+        float c[8], sn[8];
+        if (turned) {
+            const int64_t at = (int64_t)min(pos, p.n_pos - 1) * half + angle;
+            *reinterpret_cast<float4*>(c) = __ldg(reinterpret_cast<const float4*>(p.cos_t + at));
+            *reinterpret_cast<float4*>(sn) = __ldg(reinterpret_cast<const float4*>(p.sin_t + at));
+            if (!p.interleaved) {
+                *reinterpret_cast<float4*>(c + 4) = __ldg(reinterpret_cast<const float4*>(p.cos_t + at + 4));
+                *reinterpret_cast<float4*>(sn + 4) = __ldg(reinterpret_cast<const float4*>(p.sin_t + at + 4));
             }
         }
-        __half scale;
-        const uint32_t word = paged_quantise(u, &scale);                 // (every lane: it shuffles)
-        if (r >= rows) continue;
-        if (kind == 0) {
-            *reinterpret_cast<uint4*>(p.q_out + t * p.q_out_ld + (int64_t)head * d + 8 * m) = u;
-        } else if (uint8_t* block = paged_block(p.batch, b, pos, head, block_bytes)) {
-            const int tt = pos & 15;
-            *reinterpret_cast<uint32_t*>(block + (kind == 1 ? paged_k_word(m, tt) : paged_v_word(m, tt, d))) = word;
-            if ((m & 3) == 0) *reinterpret_cast<__half*>(block + (kind == 1 ? paged_k_scale(m, tt, d) : paged_v_scale(m, tt, d))) = scale;
+        uint8_t* blocks = paged_block(p.batch, b, pos, 0, block_bytes);  // of head 0; the others' lie a head of the page further each
+        for (int base = blockIdx.y * per_pass; base < rows; base += gridDim.y * per_pass * kHeads) {
+            uint4 u[kHeads];
+#pragma unroll
+            for (int k = 0; k < kHeads; ++k) {
+                const int r = base + k * gridDim.y * per_pass + (threadIdx.x >> log2_lanes);
+                const __half* src = r < p.h_q ? p.q + t * p.q_ld + (int64_t)r * d : r < p.h_q + h_kv ? p.k + t * p.k_ld + (int64_t)(r - p.h_q) * d : p.v + t * p.v_ld + (int64_t)(r - p.h_q - h_kv) * d;
+                u[k] = r < rows ? *reinterpret_cast<const uint4*>(src + 8 * m) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < kHeads; ++k) {
+                const int r0 = base + k * gridDim.y * per_pass + (int)((threadIdx.x & ~31u) >> log2_lanes), r = r0 + (lane >> log2_lanes);   // r0: the warp's first head
+                if (r0 >= rows) break;
+                const bool is_value = r >= p.h_q + h_kv;
+                if (p.cos_t && r0 < p.h_q + h_kv) {
+                    uint4 w;
+                    w.x = __shfl_sync(0xffffffffu, u[k].x, partner);
+                    w.y = __shfl_sync(0xffffffffu, u[k].y, partner);
+                    w.z = __shfl_sync(0xffffffffu, u[k].z, partner);
+                    w.w = __shfl_sync(0xffffffffu, u[k].w, partner);
+                    if (turned && !is_value) {
+                        float x[8], o[8];
+                        paged_unpack8(u[k], x);
+                        if (p.interleaved) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                o[2 * e] = __fsub_rn(__fmul_rn(x[2 * e], c[e]), __fmul_rn(x[2 * e + 1], sn[e]));
+                                o[2 * e + 1] = __fadd_rn(__fmul_rn(x[2 * e + 1], c[e]), __fmul_rn(x[2 * e], sn[e]));
+                            }
+                        } else {
+                            float y[8];
+                            paged_unpack8(w, y);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) o[e] = __fadd_rn(__fmul_rn(x[e], c[e]), __fmul_rn(low ? -y[e] : y[e], sn[e]));
+                        }
+                        __half2* h = reinterpret_cast<__half2*>(&u[k]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) h[e] = __floats2half2_rn(o[2 * e], o[2 * e + 1]);
+                    }
+                }
+                if (r < p.h_q) *reinterpret_cast<uint4*>(p.q_out + t * p.q_out_ld + (int64_t)r * d + 8 * m) = u[k];
+                if (!blocks || r0 + (31 >> log2_lanes) < p.h_q) continue;   // (a warp of queries only)
+                __half scale;
+                const uint32_t word = paged_quantise(u[k], &scale);      // (every lane: it shuffles)
+                if (r >= p.h_q && r < rows) {
+                    const int head = is_value ? r - p.h_q - h_kv : r - p.h_q, tt = pos & 15;
+                    uint8_t* block = blocks + ((int64_t)head << p.batch.log2_blocks) * block_bytes;
+                    *reinterpret_cast<uint32_t*>(block + (is_value ? paged_v_word(m, tt, d) : paged_k_word(m, tt))) = word;
+                    if ((m & 3) == 0) *reinterpret_cast<__half*>(block + (is_value ? paged_v_scale(m, tt, d) : paged_k_scale(m, tt, d))) = scale;
+                }
+            }
         }
     }
 }
@@ -212,28 +228,45 @@ struct PagedReadParams {
     int32_t d;
 };
 
-// fp16(q * s) of the tokens of a call, zeros where the table gives them no page: one CTA per row, 8 elements per lane.
+__device__ __forceinline__ uint4 paged_values(uint32_t w, __half scale)
+{
+    uint4 u;
+    __half2* h = reinterpret_cast<__half2*>(&u);
+    const float s = __half2float(scale);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = __floats2half2_rn((float)((int)((w >> (4 * e)) & 15) - 8) * s, (float)((int)((w >> (4 * e + 16)) & 15) - 8) * s);
+    return u;
+}
+
+// fp16(q * s) of the tokens of a call, zeros where the table gives them no page: ROWS rows per CTA, 8 elements of the key and of the value per lane.
+template <int ROWS>
 __global__ void __launch_bounds__(kPagedThreads) paged_read_kernel(const PagedReadParams p)
 {
+    __shared__ int seq[kPagedMostRows], position[kPagedMostRows];
+    __shared__ const uint8_t* first_head[kPagedMostRows];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int t = blockIdx.x, d = p.d;
-    int b, pos;
-    if (!paged_locate(p.batch, t, &b, &pos)) return;
-    const int lanes = d >> 3, n = p.batch.h_kv * lanes;
-    for (int i = threadIdx.x; i < 2 * n; i += kPagedThreads) {
-        const bool value = i >= n;
-        const int r = value ? i - n : i, head = r / lanes, m = r - head * lanes, tt = pos & 15;
-        const uint8_t* block = paged_block(p.batch, b, pos, head, paged_block_bytes(d));
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (block) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(block + (value ? paged_v_word(m, tt, d) : paged_k_word(m, tt)));
-            const float s = __half2float(*reinterpret_cast<const __half*>(block + (value ? paged_v_scale(m, tt, d) : paged_k_scale(m, tt, d))));
-            __half2* h = reinterpret_cast<__half2*>(&u);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = __floats2half2_rn((float)((int)((w >> (4 * e)) & 15) - 8) * s, (float)((int)((w >> (4 * e + 16)) & 15) - 8) * s);
+    const int d = p.d, n = min(ROWS, p.batch.T - (int)blockIdx.x * ROWS), bytes = paged_block_bytes(d);
+    paged_locate(p.batch, blockIdx.x * ROWS, n, seq, position);
+    if (threadIdx.x < n && seq[threadIdx.x] >= 0) first_head[threadIdx.x] = paged_block(p.batch, seq[threadIdx.x], position[threadIdx.x], 0, bytes);
+    __syncthreads();
+    const int lanes = d >> 3, per = p.batch.h_kv * lanes;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < n * per; i += kPagedThreads) {
+        const int row = i / per, r = i - row * per, head = r / lanes, m = r - head * lanes;
+        if (seq[row] < 0) continue;
+        const int tt = position[row] & 15;
+        uint4 k = make_uint4(0, 0, 0, 0), v = k;
+        if (const uint8_t* block = first_head[row]) {
+            block += ((int64_t)head << p.batch.log2_blocks) * bytes;
+            const uint32_t kw = *reinterpret_cast<const uint32_t*>(block + paged_k_word(m, tt)), vw = *reinterpret_cast<const uint32_t*>(block + paged_v_word(m, tt, d));
+            const __half ks = *reinterpret_cast<const __half*>(block + paged_k_scale(m, tt, d)), vs = *reinterpret_cast<const __half*>(block + paged_v_scale(m, tt, d));
+            k = paged_values(kw, ks);
+            v = paged_values(vw, vs);
         }
-        *reinterpret_cast<uint4*>((value ? p.v : p.k) + ((int64_t)t * p.batch.h_kv + head) * d + 8 * m) = u;
+        const int64_t to = (((int64_t)blockIdx.x * ROWS + row) * p.batch.h_kv + head) * d + 8 * m;
+        *reinterpret_cast<uint4*>(p.k + to) = k;
+        *reinterpret_cast<uint4*>(p.v + to) = v;
     }
 }
 

@@ -100,15 +100,16 @@ extern "C" ql_status qlinear_rope_tables(float* cos_dev, float* sin_dev, int32_t
             const double slowed = std::min(1.0, std::max(0.0, (i - low) / std::max(high - low, 0.001)));
             f = f / s->factor * slowed + f * (1.0 - slowed);
         }
-        p.turns[i] = f / kTwoPi;
+        const double turns = f / kTwoPi;
+        p.turns[i] = (uint64_t)std::ldexp(turns - std::floor(turns), 64);   // (below one turn: base > 1)
     }
     int sms;
     const ql_status ready = device_sms(device, &sms);
     if (ready != QL_OK) return ready;
     DeviceGuard guard(device);
     if (!guard.ok) { cudaGetLastError(); return QL_ERR_CUDA; }
-    const int64_t items = (int64_t)n_pos * (p.pairs / 4);
-    return launched(launch(rope_tables_kernel, p, dim3((unsigned)std::min<int64_t>((items + 255) / 256, 8 * sms)), dim3(256), 0, static_cast<cudaStream_t>(stream), 1, pdl_enabled()));
+    const int per_block = 256 / (p.pairs / 4);
+    return launched(launch(rope_tables_kernel, p, dim3((unsigned)std::min((n_pos + per_block - 1) / per_block, 8 * sms)), dim3(256), 0, static_cast<cudaStream_t>(stream), 1, pdl_enabled()));
 }
 
 // ---------------------------------------------------------------------------------------------------- paged cache
@@ -179,8 +180,11 @@ extern "C" ql_status qlinear_paged_append(qlinear_paged_t h, const void* q, int6
     p.q_ld = q_ld; p.k_ld = k_ld; p.v_ld = v_ld; p.q_out_ld = q_out_ld;
     p.cos_t = cos_dev; p.sin_t = sin_dev; p.n_pos = cos_dev ? n_pos : 1; p.rot = cos_dev ? rot : 0; p.interleaved = interleaved;
     p.h_q = q ? h_q : 0; p.d = d;
-    const int passes = ((p.h_q + 2 * h_kv) * (d / 8) + kPagedThreads - 1) / kPagedThreads;
-    return launched(launch(paged_append_kernel, p, dim3(T, T <= 2 * h->shared.sms ? std::min(passes, 64) : 1), dim3(kPagedThreads), 0, static_cast<cudaStream_t>(stream), 1, h->pdl));
+    const int passes = ((p.h_q + 2 * h_kv) * (d / 8) + kPagedThreads - 1) / kPagedThreads, sms = h->shared.sms;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // few rows: the passes over the heads as CTAs of their own; many: several rows to a CTA, which looks its sequences up once
+    if (T <= 16 * sms) return launched(launch(paged_append_kernel<1>, p, dim3(T, T <= 2 * sms ? std::min(passes, 64) : 1), dim3(kPagedThreads), 0, st, 1, h->pdl));
+    return launched(launch(paged_append_kernel<4>, p, dim3((T + 3) / 4), dim3(kPagedThreads), 0, st, 1, h->pdl));
 }
 
 extern "C" ql_status qlinear_paged_read(qlinear_paged_t h, const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T,
@@ -194,7 +198,9 @@ extern "C" ql_status qlinear_paged_read(qlinear_paged_t h, const int32_t* table,
     DeviceGuard guard(h->device);
     if (!guard.ok) { cudaGetLastError(); return QL_ERR_CUDA; }
     p.k = static_cast<__half*>(k_out); p.v = static_cast<__half*>(v_out); p.d = h->d.d_h;
-    return launched(launch(paged_read_kernel, p, dim3(T), dim3(kPagedThreads), 0, static_cast<cudaStream_t>(stream), 1, h->pdl));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T <= 16 * h->shared.sms) return launched(launch(paged_read_kernel<1>, p, dim3(T), dim3(kPagedThreads), 0, st, 1, h->pdl));
+    return launched(launch(paged_read_kernel<8>, p, dim3((T + 7) / 8), dim3(kPagedThreads), 0, st, 1, h->pdl));
 }
 
 namespace {
@@ -280,15 +286,10 @@ extern "C" ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q, i
 namespace {
 
 template <typename T, int TILE>
-cudaError_t launch_logits(const LogitsParams& p, int device, cudaStream_t st)
+cudaError_t launch_logits(const LogitsParams& p, cudaStream_t st)
 {
-    static std::atomic<bool> flags[64];
-    if (!flags[device].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(adjust_logits_kernel<T, TILE>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * TILE * 4);
-        if (e != cudaSuccess) return e;
-        flags[device].store(true, std::memory_order_release);
-    }
-    const size_t smem = p.bias_ids ? 2 * TILE * 4 : p.tokens ? TILE * 4 : 0;
+    static_assert(TILE * 8 <= 48 * 1024, "within what a kernel may have without asking");
+    const size_t smem = p.tokens || p.bias_ids ? TILE * 8 : 0;
     return launch(adjust_logits_kernel<T, TILE>, p, dim3((p.vocab + TILE - 1) / TILE, p.rows), dim3(kLogitsThreads), smem, st, 1, pdl_enabled());
 }
 
@@ -322,7 +323,7 @@ extern "C" ql_status qlinear_adjust_logits(const void* logits, int64_t ld, void*
     p.rows = rows; p.vocab = vocab; p.n_tokens = n_tokens; p.n_biases = n_biases;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     // small tiles until the large ones fill the SMs
-    const bool small = (int64_t)rows * ((vocab + 8191) / 8192) < 2 * sms;
-    if (is_fp32) return launched(small ? launch_logits<float, 2048>(p, device, st) : launch_logits<float, 8192>(p, device, st));
-    return launched(small ? launch_logits<__half, 2048>(p, device, st) : launch_logits<__half, 8192>(p, device, st));
+    const bool small = (int64_t)rows * ((vocab + kLogitsTile - 1) / kLogitsTile) < 2 * sms;
+    if (is_fp32) return launched(small ? launch_logits<float, 1024>(p, st) : launch_logits<float, kLogitsTile>(p, st));
+    return launched(small ? launch_logits<__half, 2048>(p, st) : launch_logits<__half, kLogitsTile>(p, st));
 }
