@@ -105,9 +105,9 @@ __device__ __forceinline__ void paged_unpack8(const uint4& u, float f[8])
 }
 
 // 8 elements of a group that 4 neighbouring lanes hold: the word, and the group's scale.
-// The integers are those of round-half-even of the IEEE quotient, without dividing: for fp16 numbers x and s, x / s below 7.01 is a tie (a whole number and a half) or at
-// least 2^-14 away from one (2 x and an odd multiple of s are multiples of a unit that is at least 2^-12 of the larger), so a product with the reciprocal, off by less than
-// 2^-18, is right once it has been rounded to a multiple of 2^-15 (the sum with 384), which makes the ties exact again.
+// The integers are those of round-half-even of the IEEE quotient, without dividing: for fp16 numbers x and s, x / s below 16 is a tie (a whole number and a half) or at
+// least 2^-14 away from one (2 x and an odd multiple of s are multiples of a unit that is at least 2^-12 of the larger), so x r + 384 with the reciprocal r, off by less than
+// 2^-18 before it is rounded, once, to a multiple of 2^-15, has the ties exact again.  The scale: fp16(amax * (1 / 7)) is fp16(amax / 7) for every fp16 number.
 __device__ __forceinline__ uint32_t paged_quantise(const uint4& u, __half* scale)
 {
     const __half2* h2 = reinterpret_cast<const __half2*>(&u);
@@ -115,19 +115,19 @@ __device__ __forceinline__ uint32_t paged_quantise(const uint4& u, __half* scale
     float amax = fmaxf(__low2float(top), __high2float(top));
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-    const float s = fminf(__half2float(__float2half_rn(__fdiv_rn(amax, 7.f))), 9352.f);
+    const float s = fminf(__half2float(__float2half_rn(__fmul_rn(amax, 1.f / 7))), 9352.f);
     *scale = __float2half_rn(s);
     const float r = s > 0.f ? __frcp_rn(s) : 0.f;
     float f[8];
     paged_unpack8(u, f);
-    uint32_t w = 0;
+    uint32_t b[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float t = __fsub_rn(__fadd_rn(fminf(fmaxf(f[i] * r, -7.f), 7.f), 384.f), 384.f);
-        // (the low bits of 1.5 * 2^23 + 8 + a whole number are 8 and that number)
-        w |= (__float_as_uint(__fadd_rn(t, 12582920.f)) & 15u) << (4 * ((i >> 1) + 4 * (i & 1)));
-    }
-    return w;
+    for (int i = 0; i < 8; ++i)                                          // the bits of 1.5 * 2^23 and the integer + 8 as the low ones
+        b[i] = __float_as_uint(__fadd_rn(fminf(fmaxf(__fmaf_rn(f[i], r, 384.f), 377.f), 391.f), 12582536.f));
+    uint32_t w = b[7];                                                   // nibble 7 first; what the upper bits add up to is taken off at the end
+    w = w * 16 + b[5]; w = w * 16 + b[3]; w = w * 16 + b[1];
+    w = w * 16 + b[6]; w = w * 16 + b[4]; w = w * 16 + b[2]; w = w * 16 + b[0];
+    return w - 0x3f400000u;
 }
 
 // ROWS rows of the call per CTA, one after the other (and, for few rows, a CTA per piece of the heads); d / 8 lanes per head, 8 elements each: one 16-byte load, the partner of
@@ -166,14 +166,17 @@ __global__ void __launch_bounds__(kPagedThreads, ROWS > 1 ? 4 : 1) paged_append_
                 *reinterpret_cast<float4*>(sn + 4) = __ldg(reinterpret_cast<const float4*>(p.sin_t + at + 4));
             }
         }
+        const __half *q_row = p.q + t * p.q_ld + 8 * m, *k_row = p.k + t * p.k_ld + 8 * m, *v_row = p.v + t * p.v_ld + 8 * m;
+        __half* q_to = p.q_out + t * p.q_out_ld + 8 * m;
         uint8_t* blocks = paged_block(p.batch, b, pos, 0, block_bytes);  // of head 0; the others' lie a head of the page further each
         for (int base = blockIdx.y * per_pass; base < rows; base += gridDim.y * per_pass * kHeads) {
             uint4 u[kHeads];
 #pragma unroll
             for (int k = 0; k < kHeads; ++k) {
                 const int r = base + k * gridDim.y * per_pass + (threadIdx.x >> log2_lanes);
-                const __half* src = r < p.h_q ? p.q + t * p.q_ld + (int64_t)r * d : r < p.h_q + h_kv ? p.k + t * p.k_ld + (int64_t)(r - p.h_q) * d : p.v + t * p.v_ld + (int64_t)(r - p.h_q - h_kv) * d;
-                u[k] = r < rows ? *reinterpret_cast<const uint4*>(src + 8 * m) : make_uint4(0, 0, 0, 0);
+                const __half* src = r < p.h_q ? q_row : r < p.h_q + h_kv ? k_row : v_row;
+                const int head = r < p.h_q ? r : r < p.h_q + h_kv ? r - p.h_q : r - p.h_q - h_kv;
+                u[k] = r < rows ? *reinterpret_cast<const uint4*>(src + head * d) : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
             for (int k = 0; k < kHeads; ++k) {
@@ -206,7 +209,7 @@ __global__ void __launch_bounds__(kPagedThreads, ROWS > 1 ? 4 : 1) paged_append_
                         for (int e = 0; e < 4; ++e) h[e] = __floats2half2_rn(o[2 * e], o[2 * e + 1]);
                     }
                 }
-                if (r < p.h_q) *reinterpret_cast<uint4*>(p.q_out + t * p.q_out_ld + (int64_t)r * d + 8 * m) = u[k];
+                if (r < p.h_q) *reinterpret_cast<uint4*>(q_to + r * d) = u[k];
                 if (!blocks || r0 + (31 >> log2_lanes) < p.h_q) continue;   // (a warp of queries only)
                 __half scale;
                 const uint32_t word = paged_quantise(u[k], &scale);      // (every lane: it shuffles)

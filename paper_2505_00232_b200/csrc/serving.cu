@@ -285,12 +285,27 @@ extern "C" ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q, i
 // ---------------------------------------------------------------------------------------------------- logits
 namespace {
 
-template <typename T, int TILE>
-cudaError_t launch_logits(const LogitsParams& p, cudaStream_t st)
+template <typename T>
+cudaError_t launch_logits(LogitsParams p, int device, int sms, cudaStream_t st)
 {
-    static_assert(TILE * 8 <= 48 * 1024, "within what a kernel may have without asking");
-    const size_t smem = p.tokens || p.bias_ids ? TILE * 8 : 0;
-    return launch(adjust_logits_kernel<T, TILE>, p, dim3((p.vocab + TILE - 1) / TILE, p.rows), dim3(kLogitsThreads), smem, st, 1, pdl_enabled());
+    constexpr int TILE = sizeof(T) == 2 ? 2048 : 1024, kPiece = 4 * kLogitsThreads * 16 / (int)sizeof(T);
+    static std::atomic<bool> flags[64];
+    if (!flags[device].load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(adjust_seen_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSeenBytes);
+        if (e != cudaSuccess) return e;
+        flags[device].store(true, std::memory_order_release);
+    }
+    const bool pdl = pdl_enabled(), some = p.tokens || p.bias_ids;
+    const int tiles = (p.vocab + TILE - 1) / TILE;
+    // one launch until its CTAs fill the SMs a few times over: each goes through its row's whole history (rows of 128256, history of 1280, one launch / two: 1 row 5.6 / 7.4 us,
+    // 8 rows 6.4 / 7.4, 16 rows 7.8 / 8.2, 256 rows 79 / 29)
+    if (some && (int64_t)p.rows * tiles <= 4 * sms)
+        return launch(adjust_logits_kernel<T, TILE>, p, dim3(tiles, p.rows), dim3(kLogitsThreads), TILE * 8, st, 1, pdl);
+    p.masked = p.mask || p.x != p.y;
+    cudaError_t e = cudaSuccess;
+    if (p.masked) e = launch(mask_logits_kernel<T>, p, dim3((p.vocab + kPiece - 1) / kPiece, p.rows), dim3(kLogitsThreads), 0, st, 1, pdl);
+    if (e == cudaSuccess && some) e = launch(adjust_seen_kernel<T>, p, dim3((p.vocab + kSeenTokens - 1) / kSeenTokens, p.rows), dim3(kSeenThreads), kSeenBytes, st, 1, pdl);
+    return e;
 }
 
 }  // namespace
@@ -322,8 +337,5 @@ extern "C" ql_status qlinear_adjust_logits(const void* logits, int64_t ld, void*
     p.mask = static_cast<const uint32_t*>(mask);
     p.rows = rows; p.vocab = vocab; p.n_tokens = n_tokens; p.n_biases = n_biases;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // small tiles until the large ones fill the SMs
-    const bool small = (int64_t)rows * ((vocab + kLogitsTile - 1) / kLogitsTile) < 2 * sms;
-    if (is_fp32) return launched(small ? launch_logits<float, 1024>(p, st) : launch_logits<float, kLogitsTile>(p, st));
-    return launched(small ? launch_logits<__half, 2048>(p, st) : launch_logits<__half, kLogitsTile>(p, st));
+    return launched(is_fp32 ? launch_logits<float>(p, device, sms, st) : launch_logits<__half>(p, device, sms, st));
 }
