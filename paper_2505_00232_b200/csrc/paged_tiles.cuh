@@ -30,7 +30,7 @@ namespace ql {
 
 template <int D> struct TileShape {
     static constexpr int NT = D == 256 ? 1 : 2;                          // tiles of 128 rows
-    static constexpr int N = 64;                                         // keys of a step
+    static constexpr int N = 64;                                         // keys of a step (a bit each of 64 in the softmax)
     static constexpr int kSlots = D == 256 ? 3 : D == 128 ? 6 : 8;       // operands in shared memory: K and V of the steps in turn
     static constexpr int kRaw = D == 256 ? 3 : 4;                        // raw steps
     static constexpr int NB = D / 64;                                    // panels of 64 elements
@@ -268,7 +268,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
             for (int si = 0; si < rd.n && ok; ++si) {
                 const TileSegment s = segs[si];
                 const int rr = s.row0 + 128 * t + in_tile, i = rr / p.group, pos = s.pos0 + i;
-                const int last = rr < s.n_rows ? min(pos, s.end - 1) : -1, lowest = p.window > 0 ? pos - p.window : -1;
+                // (a row behind the sequence's last, whose result nobody looks at, sees all: it does not send its warp through the hiding below)
+                const int last = rr < s.n_rows ? min(pos, s.end - 1) : INT32_MAX, lowest = p.window > 0 && rr < s.n_rows ? pos - p.window : -1;
                 float m = -1e30f;
                 float2 l[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 const int32_t* table = bt.table + s.table;
@@ -298,9 +299,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     }
                     const int hi = last - (s.step0 + j) * N, lo = lowest - (s.step0 + j) * N;
                     if (__any_sync(0xffffffffu, hi < N - 1 || lo >= 0) || blocks != (1u << T::kBlocks) - 1) {
+                        // one bit per key: up to hi, above lo, of blocks with a page
+                        uint64_t see = hi < 0 ? 0 : hi >= 63 ? ~0ull : (2ull << hi) - 1;
+                        if (lo >= 0) see &= lo >= 63 ? 0 : ~0ull << (lo + 1);
+#pragma unroll
+                        for (int k = 0; k < T::kBlocks; ++k)
+                            if (!(blocks >> k & 1)) see &= ~(0xffffull << (16 * k));
+                        const uint32_t half[2] = {(uint32_t)see, (uint32_t)(see >> 32)};
 #pragma unroll
                         for (int e = 0; e < N; ++e)
-                            if (e > hi || e <= lo || !(blocks >> (e >> 4) & 1)) x[e] = -INFINITY;
+                            if (!(half[e >> 5] & 1u << (e & 31))) x[e] = -INFINITY;
                     }
                     float mx[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
