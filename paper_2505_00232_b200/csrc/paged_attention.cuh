@@ -7,12 +7,18 @@
 // columns; the weights become the second product's operand by two 8 x 8 transpositions in registers, the values, unpacked and scaled to
 // fp16(q s), its rows.  So no lane ever needs another's bytes but through the tensor core.
 //
-// Work: the blocks of all (sequence, KV head, 8 query rows) segments, numbered through, are cut into one span of equal length per CTA, whatever the
-// lengths: a ragged batch and a single long sequence load the SMs alike.  The plan is made by every CTA from the lengths on the device
-// (a scan), so a captured launch follows them.  A CTA's 8 warps take the blocks of a segment in turn, each through a ring of its own in shared
-// memory (cp.async), and meet at the segment's end; a segment cut by a span's end leaves (m, l, o) in the workspace, which paged_combine_kernel
-// joins in order.  Weights are fp16 relative to a maximum that is raised only when it is passed by 2^8 (sums are fp32; at most 2^8 of
-// 2^16 are used).
+// Work: the segments (sequence, KV head, 8 query rows) of the batch, numbered through, each as long as its blocks and kAttnOverhead more
+// (what a segment costs besides its blocks: an empty pipeline, the warps' meeting), are cut into one span of equal length per CTA, whatever the
+// lengths: a ragged batch and a single long sequence load the SMs alike (64 sequences of 128 .. 8192 tokens, 194618 in all, 8 KV heads of 128:
+// 81.7 us with spans of blocks alone, 72.3, 68.1, 64.1, 66.0 with 8, 16, 32, 48 more; of equal lengths 63).  The plan is made by every CTA
+// from the lengths on the device (a scan), so a captured launch follows them.  A CTA's 8 warps take the blocks of a segment in turn, each
+// through a ring of its own in shared memory that goes on from segment to segment (bulk copies, requested by the lane that looked up the page), and
+// meet at the segment's end, when the first blocks of the next one are on their way.  A segment cut by a span's end leaves (m, l, o) in the
+// workspace, which paged_combine_kernel joins in order.  Weights are fp16 relative to a maximum that is raised only when it is passed by 2^8
+// (sums are fp32; at most 2^8 of 2^16 are used).
+//
+// Bound: the instructions that unpack, not the memory.  About 430 warp instructions per block of 16 tokens and 128 elements give 4.5 TB/s of cache
+// in the loop; 131071 tokens of one sequence take 53 us (151 MB, 23 us at the copy rate), of which 8 are the two launches' fixed part.
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -20,18 +26,23 @@
 
 #include "dequant.cuh"
 #include "paged.cuh"
+#include "sm100_ptx.cuh"
 
 namespace ql {
 
 constexpr int kAttnWarps = 8;
 constexpr int kAttnCols = 8;
 constexpr int kAttnMaxRows = 32;                                         // query rows per KV head that this kernel takes (8 at a time); more: paged_tiles.cuh
+constexpr int kAttnOverhead = 32;                                         // a segment without blocks, in blocks
 template <int D> struct AttnRing {
     static constexpr int kBlock = paged_block_bytes(D);
     static constexpr int kStages = D == 64 ? 6 : D == 128 ? 4 : 3;
-    static constexpr int kBytes = kAttnWarps * kStages * kBlock;
-    static constexpr int kMergeStride = D + 4;                           // floats of a column in the warps' meeting (the ring's memory)
-    static_assert(kAttnWarps * kAttnCols * kMergeStride * 4 <= kBytes, "the warps meet in the ring's memory");
+    static constexpr int kRing = kAttnWarps * kStages * kBlock;
+    static constexpr int kMergeStride = D + 4;                           // floats of a column in the warps' meeting
+    static constexpr bool kMeetApart = D < 256;                          // a buffer of its own for it: the ring already has the next segment's blocks
+    static constexpr int kMeet = kAttnWarps * kAttnCols * kMergeStride * 4;
+    static constexpr int kBytes = kRing + (kMeetApart ? kMeet : 0);
+    static_assert(kMeet <= kRing, "or the ring's memory");
 };
 
 struct PagedAttnParams {
@@ -66,10 +77,6 @@ __device__ __forceinline__ uint32_t move_matrix(uint32_t a)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
     return r;
 }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
 __device__ __forceinline__ float exp2_fast(float x)                      // (2 ulp; subnormal results are zero)
 {
     float r;
@@ -77,23 +84,27 @@ __device__ __forceinline__ float exp2_fast(float x)                      // (2 u
     return r;
 }
 
-// The score of a key on a base-2 scale, after the soft cap.  tanh(y) = 1 - 2 / (exp(2 y) + 1).
-template <bool CAP>
-__device__ __forceinline__ float attn_score(float dot, float scale, float softcap)
+__device__ __forceinline__ float rcp_fast(float x)                       // (1 ulp; 0 of infinity)
 {
-    constexpr float kLog2e = 1.4426950408889634f;
-    if (!CAP) return dot * (scale * kLog2e);
-    return softcap * kLog2e * (1.f - __fdividef(2.f, exp2_fast(2.f * kLog2e * fminf(dot * scale / softcap, 40.f)) + 1.f));
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
+// The soft cap of scores on a base-2 scale: cap log2(e) tanh(scale dot / cap), tanh(y) = 1 - 2 / (exp(2 y) + 1).
+struct SoftCap {
+    float in, out;
+    __device__ SoftCap(float scale, float cap) : in(cap > 0.f ? 2.f * 1.4426950408889634f * scale / cap : 0.f), out(cap * 1.4426950408889634f) {}
+    __device__ __forceinline__ float operator()(float dot) const { return fmaf(-2.f * out, rcp_fast(exp2_fast(dot * in) + 1.f), out); }
+};
 
-// Sums over a scan of the sequences' block counts: pre[b] blocks before sequence b (per head and row block).  Every thread takes part.
+// Sums over a scan of the sequences' lengths: pre[b] before sequence b (per head and row block).  Every thread takes part.
 __device__ __forceinline__ void attn_scan(const PagedAttnParams& p, int* pre)
 {
     __shared__ int warp_sum[kAttnWarps];
     const int B = p.batch.B, tid = threadIdx.x, per = (B + 255) / 256, lo = min(B, tid * per), hi = min(B, lo + per);
     int sum = 0, first;
     for (int b = lo; b < hi; ++b) {
-        const int n = attn_blocks(p, b, &first);
+        const int blocks = attn_blocks(p, b, &first), n = blocks > 0 ? blocks + kAttnOverhead : 0;
         pre[b + 1] = n;
         sum += n;
     }
@@ -112,24 +123,40 @@ __device__ __forceinline__ void attn_scan(const PagedAttnParams& p, int* pre)
     __syncthreads();
 }
 
+// What a CTA does of a segment: blocks first .. first + n - 1 of its sequence.
+struct AttnSegment {
+    int32_t head, row0, n_rows, t0, pos0, first, n, slot;                // rows of the sequence row0 .. (n_rows of it), row 0's token and position; slot -1: the whole segment
+    int64_t table, next;                                                 // offset of the sequence's row of the page table; where the next segment begins in the numbering
+};
+
 template <int D, bool CAP>
 __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(const PagedAttnParams p)
 {
     constexpr int NB = D / 64, kBlock = AttnRing<D>::kBlock, S = AttnRing<D>::kStages, kStride = AttnRing<D>::kMergeStride;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float meet_m[kAttnWarps][kAttnCols], meet_l[kAttnWarps][kAttnCols];
+    __shared__ float meet_m[2][kAttnWarps][kAttnCols], meet_l[2][kAttnWarps][kAttnCols];
+    __shared__ __align__(8) uint64_t bars[kAttnWarps * S];
+    __shared__ AttnSegment segs[4];                                      // in turn: the last one (slow warps still look at it), this, the next, the one after it
+    __shared__ volatile uint32_t abort_flag[4];
+    // (at d_h 256 the queries lie in shared memory, read for every block: with 128 registers they would be spilled)
+    constexpr bool kQueriesApart = D == 256;
+    __shared__ __align__(16) uint4 queries[kQueriesApart ? 2 * NB * 32 : 1];
     int* pre = reinterpret_cast<int*>(smem + AttnRing<D>::kBytes);       // [B + 1]
+    float* meet = reinterpret_cast<float*>(smem + (AttnRing<D>::kMeetApart ? AttnRing<D>::kRing : 0));
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    const uint32_t bar0 = smem_u32(bars) + warp * (S * 8), ring_u32 = smem_u32(smem) + warp * (S * kBlock);
+    const uint8_t* ring = smem + warp * (S * kBlock);
+    if (lane < S) mbar_init(bar0 + 8 * lane, 1);
+    if (tid == 0) { abort_flag[0] = abort_flag[1] = 0; abort_flag[2] = abort_flag[3] = 1; }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     attn_scan(p, pre);
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
-    const int h_kv = p.batch.h_kv, segs = h_kv * p.row_blocks;
-    const int64_t total = (int64_t)pre[p.batch.B] * segs;
+    const int h_kv = p.batch.h_kv, per_head = h_kv * p.row_blocks;
+    const int64_t total = (int64_t)pre[p.batch.B] * per_head;
     const int64_t span = max((int64_t)kAttnWarps, (total + p.grid - 1) / p.grid);
     const int64_t w0 = (int64_t)blockIdx.x * span, w1 = min(total, w0 + span);
-    uint8_t* ring = smem + warp * (S * kBlock);
-    const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
     if (tid == 0) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
     for (int b = blockIdx.x; b < p.batch.B; b += p.grid) {               // rows of sequences that see nothing: zeros
         int t0;
@@ -138,57 +165,117 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
         for (int64_t e = tid; e < (int64_t)rows * p.h_q * (D / 8); e += kAttnWarps * 32)
             *reinterpret_cast<uint4*>(p.out + (t0 + e / (p.h_q * (D / 8))) * p.out_ld + 8 * (e % (p.h_q * (D / 8)))) = make_uint4(0, 0, 0, 0);
     }
-
-    for (int64_t w = w0; w < w1;) {
-        // the segment (sequence, KV head, 8 rows) and the part [ua, ub) of its blocks
-        int b;
-        {
-            const int x = (int)(w / segs);
+    // The first segment from place w of the numbering on of which this CTA has blocks (n 0: none).  (by the warp with the fewest blocks; every lane computes it)
+    const auto describe = [&](int64_t w, AttnSegment* to) {
+        AttnSegment s{};
+        while (w < w1) {
+            const int x = (int)(w / per_head);
             int lo = 0, hi = p.batch.B;                                  // pre[lo] <= x < pre[hi]
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (pre[mid] <= x) lo = mid;
                 else hi = mid;
             }
-            b = lo;
+            const int b = lo, length = pre[b + 1] - pre[b], blocks = length - kAttnOverhead;
+            const int64_t local = w - (int64_t)pre[b] * per_head;
+            const int seg = (int)(local / length), ua = (int)(local - (int64_t)seg * length), ub = (int)min((int64_t)length, ua + (w1 - w));
+            const int sa = max(ua - kAttnOverhead, 0), sb = max(ub - kAttnOverhead, 0);
+            const int64_t begin = w - ua;
+            w += ub - ua;
+            if (sb <= sa) continue;
+            int first;
+            attn_blocks(p, b, &first);
+            const int rows_all = paged_rows(p.batch, b, &s.t0);
+            s.head = seg / p.row_blocks;
+            s.row0 = (seg - s.head * p.row_blocks) * kAttnCols;
+            s.n_rows = min(rows_all, p.max_q) * p.group;
+            s.pos0 = p.batch.kv_len[b] - rows_all;
+            s.first = first + sa;
+            s.n = sb - sa;
+            const bool whole = sa == 0 && sb == blocks;
+            s.slot = whole ? -1 : sa > 0 ? 0 : 1;
+            s.table = b * p.batch.table_ld;
+            if (sa == 0 && !whole && lane == 0) p.split[blockIdx.x] = make_int4(b, s.head, s.row0 / kAttnCols, (int)((begin + length - 1) / span));
+            break;
         }
-        const int blocks = pre[b + 1] - pre[b];
-        const int64_t local = w - (int64_t)pre[b] * segs;
-        const int seg = (int)(local / blocks), ua = (int)(local - (int64_t)seg * blocks), ub = (int)min((int64_t)blocks, ua + (w1 - w));
-        const int head = seg / p.row_blocks, r0 = (seg - head * p.row_blocks) * kAttnCols;
-        int first_block, t0;
-        attn_blocks(p, b, &first_block);
-        const int rows_all = paged_rows(p.batch, b, &t0), n_rows = min(rows_all, p.max_q) * p.group;
-        const int len = p.batch.kv_len[b];
-        const int32_t* table = p.batch.table + b * p.batch.table_ld;
+        s.next = w;
+        if (lane == 0) *to = s;
+        return s.next;
+    };
+    __syncthreads();                                                     // (p.split)
+    if (warp == kAttnWarps - 1) describe(w0, &segs[0]);
+    __syncthreads();
 
-        // the queries: column g of the second operand
-        uint32_t qf[NB][2][4];
-        {
-            const int r = r0 + g, i = r / p.group;
-            const __half* src = p.q + (int64_t)(t0 + i) * p.q_ld + (int64_t)(head * p.group + r - i * p.group) * D + 8 * c;
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint4 u = r < n_rows ? *reinterpret_cast<const uint4*>(src + 64 * j + 32 * e) : make_uint4(0, 0, 0, 0);
-                    qf[j][e][0] = u.x; qf[j][e][1] = u.y; qf[j][e][2] = u.z; qf[j][e][3] = u.w;
-                }
+    // Blocks warp, warp + 8, ... of a segment are this warp's; the ring goes on from segment to segment.  Their places are found 32 at a time: `src` in lane k is that of block k
+    // of a window, page_next the page of a block of the window after it, and none_even, none_odd tell which blocks of an even or odd window have no page (none_after: of the next segment's first).
+    const uint8_t* src = nullptr;
+    int page_next = -1, stage = 0, parity = 0, to = 0;                   // the stage (and its phase) that is read next, the one that is filled next
+    uint32_t none_even = 0, none_odd = 0, none_after = 0;
+    const auto mine_of = [&](const AttnSegment& s) { return s.n > warp ? (s.n - warp + kAttnWarps - 1) / kAttnWarps : 0; };
+    const auto look_up = [&](const AttnSegment& s, int i) {              // the page of block i + lane
+        const int at = (s.first + warp + (i + lane) * kAttnWarps) >> p.batch.log2_blocks;
+        page_next = i + lane < mine_of(s) && at < p.batch.table_width ? p.batch.table[s.table + at] : -1;
+    };
+    const auto place = [&](const AttnSegment& s, int i) {                // of block i + lane, from the page that has been looked up; which have none
+        const bool ok = page_next >= 0 && page_next < p.batch.n_pages;
+        const int u = s.first + warp + (i + lane) * kAttnWarps;
+        src = p.batch.pool + ((((int64_t)(ok ? page_next : 0) * h_kv + s.head) << p.batch.log2_blocks) + (u & ((1 << p.batch.log2_blocks) - 1))) * kBlock;
+        return ~__ballot_sync(0xffffffffu, ok);
+    };
+    const auto request = [&](int i) {                                    // (block i lies in the window of `src`)
+        if (lane == (i & 31)) {
+            mbar_expect_tx(bar0 + 8 * to, kBlock);
+            bulk_copy_g2s(ring_u32 + to * kBlock, src, kBlock, bar0 + 8 * to);
         }
-        // what this lane's two columns see: tokens (lowest, last]
+        to = to + 1 == S ? 0 : to + 1;
+    };
+    int requested = 0;                                                   // blocks of the segment, and on into the next one
+    const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * 1.4426950408889634f, 1e-30f), margin = 8.f / cc;   // weights exp2(cc (x - m)); (cc never 0: hidden scores are -infinity)
+    const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
+    const SoftCap cap(mag, p.softcap);
+
+    uint32_t qf[kQueriesApart ? 1 : NB][2][4];
+    const auto load_queries = [&](const AttnSegment& s) {                // column g of the second operand
+        const int r = s.row0 + g, i = r / p.group;
+        const __half* from = p.q + (int64_t)(s.t0 + i) * p.q_ld + (int64_t)(s.head * p.group + r - i * p.group) * D + 8 * c;
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if (kQueriesApart && (2 * j + e) % kAttnWarps != warp) continue;
+                uint4 u = r < s.n_rows ? *reinterpret_cast<const uint4*>(from + 64 * j + 32 * e) : make_uint4(0, 0, 0, 0);
+                u.x ^= sign; u.y ^= sign; u.z ^= sign; u.w ^= sign;
+                if (kQueriesApart) queries[(2 * j + e) * 32 + lane] = u;
+                else { qf[j % (kQueriesApart ? 1 : NB)][e][0] = u.x; qf[j % (kQueriesApart ? 1 : NB)][e][1] = u.y; qf[j % (kQueriesApart ? 1 : NB)][e][2] = u.z; qf[j % (kQueriesApart ? 1 : NB)][e][3] = u.w; }
+            }
+    };
+
+    look_up(segs[0], 0);
+    if (segs[0].n > 0) load_queries(segs[0]);
+    if (warp == kAttnWarps - 1) describe(segs[0].next, &segs[1]);
+    __syncthreads();
+    bool ok = true;
+    int meeting = 0;
+    for (int it = 0; segs[it].n > 0; it = (it + 1) & 3) {
+        const AttnSegment &s = segs[it], &nx = segs[(it + 1) & 3];
+        const int n_mine = mine_of(s), n_next = mine_of(nx);
+        if (n_mine == 0 || (requested > 0 && n_mine <= 32)) look_up(nx, 0);
+        if (warp == kAttnWarps - 1) describe(nx.next, &segs[(it + 2) & 3]);
+        // what this lane's two columns see: tokens (lowest, last]; every column of the tile sees the blocks `seen` on, n_seen of them
         int last[2], lowest[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int r = r0 + 2 * c + e, pos = len - rows_all + r / p.group;
-            last[e] = r < n_rows ? pos : -1;
-            lowest[e] = p.window > 0 ? pos - p.window : -1;
+            const int r = s.row0 + 2 * c + e, pos = s.pos0 + r / p.group;
+            last[e] = r < s.n_rows ? pos : INT32_MAX;                    // (a column behind the last row: its result is not looked at)
+            lowest[e] = p.window > 0 && r < s.n_rows ? pos - p.window : -1;
         }
-        int all_last = min(last[0], last[1]), all_lowest = max(lowest[0], lowest[1]);      // every column of the tile sees the tokens between
+        int all_last = min(last[0], last[1]), all_lowest = max(lowest[0], lowest[1]);
 #pragma unroll
         for (int o = 1; o < 4; o <<= 1) {
             all_last = min(all_last, __shfl_xor_sync(0xffffffffu, all_last, o));
             all_lowest = max(all_lowest, __shfl_xor_sync(0xffffffffu, all_lowest, o));
         }
+        const int seen = (all_lowest + 16) >> 4, n_seen = max(((int)min((int64_t)all_last + 1, (int64_t)INT32_MAX) >> 4) - seen, 0);
 
         float o[NB][4][4];
 #pragma unroll
@@ -198,139 +285,130 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[j][h][e] = 0.f;
         float m0 = -1e30f, m1 = -1e30f, l0 = 0.f, l1 = 0.f;
-
-        // this warp's blocks ua + warp, + 8, ...: their pages are looked up 32 at a time
-        const int n_mine = ub - ua > warp ? (ub - ua - warp + kAttnWarps - 1) / kAttnWarps : 0;
-        const int u_first = first_block + ua + warp;
-        int page = -1, page_next = -1;
-        auto look_up = [&](int i) {                                      // the page of block i + lane of this warp's
-            const int at = (u_first + (i + lane) * kAttnWarps) >> p.batch.log2_blocks;
-            const int pg = i + lane < n_mine && at < p.batch.table_width ? table[at] : -1;
-            return pg < p.batch.n_pages ? pg : -1;
-        };
-        page_next = look_up(0);
-        // requests block i (a commit group in any case)
-        auto request = [&](int i) {
-            if ((i & 31) == 0) { page = page_next; page_next = look_up(i + 32); }
-            const int pg = __shfl_sync(0xffffffffu, page, i & 31);
-            if (i < n_mine) {
-                const int u = u_first + i * kAttnWarps;
-                const uint8_t* src = p.batch.pool + ((((int64_t)max(pg, 0) * h_kv + head) << p.batch.log2_blocks) + (u & ((1 << p.batch.log2_blocks) - 1))) * kBlock;
-                const uint32_t dst = ring_u32 + (i % S) * kBlock;
-#pragma unroll
-                for (int k = 0; k < (kBlock + 511) / 512; ++k)
-                    if ((k + 1) * 512 <= kBlock || k * 512 + lane * 16 < kBlock) cp_async16(dst + k * 512 + lane * 16, src + k * 512 + lane * 16);
+        int u = s.first + warp;
+#pragma unroll 1
+        for (int i = 0; i < n_mine; ++i, u += kAttnWarps) {
+            __syncwarp();                                                // (no lane still reads the block before)
+            while (requested < min(i + S, AttnRing<D>::kMeetApart ? n_mine + n_next : n_mine)) {
+                const bool here = requested < n_mine;
+                const int k = here ? requested : requested - n_mine;
+                if ((k & 31) == 0) {
+                    const AttnSegment& of = here ? s : nx;
+                    const uint32_t none = place(of, k);
+                    if (!here) none_after = none;
+                    else if (k & 32) none_odd = none;
+                    else none_even = none;
+                    if (k + 32 < (here ? n_mine : n_next)) look_up(of, k + 32);
+                    else if (here) look_up(nx, 0);
+                }
+                request(k);
+                ++requested;
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            return pg;
-        };
-        int pages_ok[S];                                                 // (of the blocks in the ring: whether the table gave them a page)
-#pragma unroll
-        for (int i = 0; i < S - 1; ++i) pages_ok[i] = request(i);
+            if (!__all_sync(0xffffffffu, mbar_wait_hot(bar0 + 8 * stage, parity, abort_flag, 0xA00))) {
+                ok = false;
+                requested -= i;
+                break;
+            }
+            const bool no_page = (i & 32 ? none_odd : none_even) >> (i & 31) & 1;
+            const uint8_t* blk = ring + stage * kBlock;
+            if (++stage == S) { stage = 0; parity ^= 1; }
 
-        for (int i0 = 0; i0 < n_mine; i0 += S) {
+            // scores
+            float x[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t ks[2 * NB];                                         // scales: (token g, token g + 8) per group
 #pragma unroll
-            for (int s = 0; s < S; ++s) {
-                const int i = i0 + s;
-                if (i >= n_mine) break;
-                asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
-                __syncwarp();                                            // (this block has arrived for every lane, and no lane still reads the one before)
-                pages_ok[(s + S - 1) % S] = request(i + S - 1);
-                const uint8_t* blk = ring + s * kBlock;
-                const int u = u_first + i * kAttnWarps;
-
-                // scores
-                float x[4] = {0.f, 0.f, 0.f, 0.f};
-                uint32_t ks[2 * NB];                                     // (token g, token g + 8) per group
+            for (int e = 0; e < NB; ++e)
+                *reinterpret_cast<uint2*>(ks + 2 * e) = *reinterpret_cast<const uint2*>(blk + paged_k_scales(D) + g * (8 * NB) + 8 * e);
 #pragma unroll
-                for (int e = 0; e < NB; ++e)
-                    *reinterpret_cast<uint2*>(ks + 2 * e) = *reinterpret_cast<const uint2*>(blk + paged_k_scales(D) + g * (8 * NB) + 8 * e);
+            for (int j = 0; j < NB; ++j) {
+                const uint4 kw = *reinterpret_cast<const uint4*>(blk + 512 * j + 16 * lane);
 #pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    const uint4 kw = *reinterpret_cast<const uint4*>(blk + 512 * j + 16 * lane);
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        uint32_t lo[4], hi[4];
-                        unpack_int4_word(e ? kw.y : kw.x, lo);
-                        unpack_int4_word(e ? kw.w : kw.z, hi);
-                        float t[4];
-                        const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
-                        mma_16816_zero(t, a0, qf[j][e][0], qf[j][e][1]);
-                        mma_16816_pure(t, a1, qf[j][e][2], qf[j][e][3]);
-                        const float2 sc = __half22float2(*reinterpret_cast<const __half2*>(&ks[2 * j + e]));
-                        x[0] = fmaf(t[0], sc.x, x[0]); x[1] = fmaf(t[1], sc.x, x[1]);
-                        x[2] = fmaf(t[2], sc.y, x[2]); x[3] = fmaf(t[3], sc.y, x[3]);
-                    }
+                for (int e = 0; e < 2; ++e) {
+                    uint32_t lo[4], hi[4];
+                    unpack_int4_word(e ? kw.y : kw.x, lo);
+                    unpack_int4_word(e ? kw.w : kw.z, hi);
+                    float t[4];
+                    const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+                    uint4 q;
+                    if (kQueriesApart) q = queries[(2 * j + e) * 32 + lane];
+                    else q = make_uint4(qf[j % (kQueriesApart ? 1 : NB)][e][0], qf[j % (kQueriesApart ? 1 : NB)][e][1], qf[j % (kQueriesApart ? 1 : NB)][e][2], qf[j % (kQueriesApart ? 1 : NB)][e][3]);
+                    mma_16816_zero(t, a0, q.x, q.y);
+                    mma_16816_pure(t, a1, q.z, q.w);
+                    const float2 sc = __half22float2(*reinterpret_cast<const __half2*>(&ks[2 * j + e]));
+                    x[0] = fmaf(t[0], sc.x, x[0]); x[1] = fmaf(t[1], sc.x, x[1]);
+                    x[2] = fmaf(t[2], sc.y, x[2]); x[3] = fmaf(t[3], sc.y, x[3]);
                 }
+            }
+            if (CAP) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = attn_score<CAP>(x[e], p.scale, p.softcap);
-                // hidden tokens (only blocks that some column does not see whole, or without a page)
+                for (int e = 0; e < 4; ++e) x[e] = cap(x[e]);
+            }
+            // hidden tokens (only blocks that some column does not see whole, or without a page)
+            if ((uint32_t)(u - seen) >= (uint32_t)n_seen || no_page) {
                 const int j0 = u * 16;
-                if (j0 + 15 > all_last || j0 <= all_lowest || pages_ok[s] < 0) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int j = j0 + g + 8 * (e >> 1);
-                        if (j > last[e & 1] || j <= lowest[e & 1] || pages_ok[s] < 0) x[e] = -INFINITY;
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const int j = j0 + g + 8 * (e >> 1);
+                    if (j > last[e & 1] || j <= lowest[e & 1] || no_page) x[e] = -INFINITY;
                 }
-                // the maximum is raised when it is passed by 2^8
-                if (__any_sync(0xffffffffu, fmaxf(x[0], x[2]) > m0 + 8.f || fmaxf(x[1], x[3]) > m1 + 8.f)) {
-                    float n0 = fmaxf(x[0], x[2]), n1 = fmaxf(x[1], x[3]);
+            }
+            // the maximum is raised when it is passed by 2^8
+            if (__any_sync(0xffffffffu, fmaxf(x[0], x[2]) > m0 + margin || fmaxf(x[1], x[3]) > m1 + margin)) {
+                float n0 = fmaxf(x[0], x[2]), n1 = fmaxf(x[1], x[3]);
 #pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) {
-                        n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, d));
-                        n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, d));
-                    }
-                    n0 = fmaxf(n0, m0); n1 = fmaxf(n1, m1);
-                    const float f0 = exp2_fast(m0 - n0), f1 = exp2_fast(m1 - n1);
-                    m0 = n0; m1 = n1; l0 *= f0; l1 *= f1;
-#pragma unroll
-                    for (int j = 0; j < NB; ++j)
-#pragma unroll
-                        for (int h = 0; h < 4; ++h) { o[j][h][0] *= f0; o[j][h][1] *= f1; o[j][h][2] *= f0; o[j][h][3] *= f1; }
+                for (int d = 4; d < 32; d <<= 1) {
+                    n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, d));
+                    n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, d));
                 }
-                x[0] = exp2_fast(x[0] - m0); x[1] = exp2_fast(x[1] - m1); x[2] = exp2_fast(x[2] - m0); x[3] = exp2_fast(x[3] - m1);
-                l0 += x[0] + x[2];
-                l1 += x[1] + x[3];
-                const __half2 p01 = __floats2half2_rn(x[0], x[1]), p23 = __floats2half2_rn(x[2], x[3]);
-                const uint32_t b0 = move_matrix(*reinterpret_cast<const uint32_t*>(&p01)), b1 = move_matrix(*reinterpret_cast<const uint32_t*>(&p23));
+                n0 = fmaxf(n0, m0); n1 = fmaxf(n1, m1);
+                const float f0 = exp2_fast((m0 - n0) * cc), f1 = exp2_fast((m1 - n1) * cc);
+                m0 = n0; m1 = n1; l0 *= f0; l1 *= f1;
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) { o[j][h][0] *= f0; o[j][h][1] *= f1; o[j][h][2] *= f0; o[j][h][3] *= f1; }
+            }
+            x[0] = exp2_fast((x[0] - m0) * cc); x[1] = exp2_fast((x[1] - m1) * cc); x[2] = exp2_fast((x[2] - m0) * cc); x[3] = exp2_fast((x[3] - m1) * cc);
+            l0 += x[0] + x[2];
+            l1 += x[1] + x[3];
+            const __half2 p01 = __floats2half2_rn(x[0], x[1]), p23 = __floats2half2_rn(x[2], x[3]);
+            const uint32_t b0 = move_matrix(*reinterpret_cast<const uint32_t*>(&p01)), b1 = move_matrix(*reinterpret_cast<const uint32_t*>(&p23));
 
-                // values
+            // values
 #pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    const uint4 vw = *reinterpret_cast<const uint4*>(blk + paged_v_data(D) + 512 * j + 16 * lane);
-                    const uint2 vs = *reinterpret_cast<const uint2*>(blk + paged_v_scales(D) + (2 * j + (g >> 2)) * 32 + 8 * c);
-                    uint32_t lo01[4], hi01[4], lo23[4], hi23[4];
-                    unpack_int4_word(__byte_perm(vw.x, vw.y, 0x5410), lo01);
-                    unpack_int4_word(__byte_perm(vw.x, vw.y, 0x7632), hi01);
-                    unpack_int4_word(__byte_perm(vw.z, vw.w, 0x5410), lo23);
-                    unpack_int4_word(__byte_perm(vw.z, vw.w, 0x7632), hi23);
+            for (int j = 0; j < NB; ++j) {
+                const uint4 vw = *reinterpret_cast<const uint4*>(blk + paged_v_data(D) + 512 * j + 16 * lane);
+                const uint2 vs = *reinterpret_cast<const uint2*>(blk + paged_v_scales(D) + (2 * j + (g >> 2)) * 32 + 8 * c);
+                uint32_t lo01[4], hi01[4], lo23[4], hi23[4];
+                unpack_int4_word(__byte_perm(vw.x, vw.y, 0x5410), lo01);
+                unpack_int4_word(__byte_perm(vw.x, vw.y, 0x7632), hi01);
+                unpack_int4_word(__byte_perm(vw.z, vw.w, 0x5410), lo23);
+                unpack_int4_word(__byte_perm(vw.z, vw.w, 0x7632), hi23);
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const uint32_t a[4] = {h2_mul(lo01[h], vs.x), h2_mul(hi01[h], vs.x), h2_mul(lo23[h], vs.y), h2_mul(hi23[h], vs.y)};
-                        mma_16816_pure(o[j][h], a, b0, b1);
-                    }
+                for (int h = 0; h < 4; ++h) {
+                    const uint32_t a[4] = {h2_mul(lo01[h], vs.x), h2_mul(hi01[h], vs.x), h2_mul(lo23[h], vs.y), h2_mul(hi23[h], vs.y)};
+                    mma_16816_pure(o[j][h], a, b0, b1);
                 }
             }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-
-        // the warps meet: o of column col in meet[warp][col][*], in the ring's memory
+        if (ok) requested -= n_mine;
+        // the warps meet: o of column col in meet[warp][col][*]
+        float (*mm)[kAttnCols] = meet_m[meeting], (*ml)[kAttnCols] = meet_l[meeting];
+        meeting ^= 1;
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
             l0 += __shfl_xor_sync(0xffffffffu, l0, d);
             l1 += __shfl_xor_sync(0xffffffffu, l1, d);
         }
         if (g == 0) {
-            meet_m[warp][2 * c] = m0; meet_m[warp][2 * c + 1] = m1;
-            meet_l[warp][2 * c] = l0; meet_l[warp][2 * c + 1] = l1;
+            mm[warp][2 * c] = m0; mm[warp][2 * c + 1] = m1;
+            ml[warp][2 * c] = l0; ml[warp][2 * c + 1] = l1;
         }
         __syncthreads();
         float M0 = -1e30f, M1 = -1e30f;
 #pragma unroll
-        for (int k = 0; k < kAttnWarps; ++k) { M0 = fmaxf(M0, meet_m[k][2 * c]); M1 = fmaxf(M1, meet_m[k][2 * c + 1]); }
-        const float f0 = exp2_fast(m0 - M0), f1 = exp2_fast(m1 - M1);
-        float* meet = reinterpret_cast<float*>(smem);
+        for (int k = 0; k < kAttnWarps; ++k) { M0 = fmaxf(M0, mm[k][2 * c]); M1 = fmaxf(M1, mm[k][2 * c + 1]); }
+        const float f0 = exp2_fast((m0 - M0) * cc), f1 = exp2_fast((m1 - M1) * cc);
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             float* to = meet + (warp * kAttnCols + 2 * c) * kStride + 64 * j + 8 * g;
@@ -339,34 +417,43 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
             *reinterpret_cast<float4*>(to + kStride) = make_float4(o[j][0][1] * f1, o[j][0][3] * f1, o[j][1][1] * f1, o[j][1][3] * f1);
             *reinterpret_cast<float4*>(to + kStride + 4) = make_float4(o[j][2][1] * f1, o[j][2][3] * f1, o[j][3][1] * f1, o[j][3][3] * f1);
         }
+        if (nx.n > 0) load_queries(nx);
         __syncthreads();
-        const bool whole = ua == 0 && ub == blocks;
-        float* part = p.partial + (int64_t)(2 * blockIdx.x + (ua > 0 ? 0 : 1)) * (kAttnCols * (D + 2));
+        float* part = p.partial + (int64_t)(2 * blockIdx.x + max(s.slot, 0)) * (kAttnCols * (D + 2));
         for (int e = tid * 4; e < kAttnCols * D; e += kAttnWarps * 32 * 4) {
-            const int col = e / D, d = e - col * D, r = r0 + col;
-            float mm = -1e30f, l = 0.f;
+            const int col = e / D, d = e - col * D, r = s.row0 + col;
+            float top = -1e30f, l = 0.f;
 #pragma unroll
-            for (int k = 0; k < kAttnWarps; ++k) mm = fmaxf(mm, meet_m[k][col]);
-            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < kAttnWarps; ++k) top = fmaxf(top, mm[k][col]);
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int k = 0; k < kAttnWarps; ++k) {
                 const float4 v = *reinterpret_cast<const float4*>(meet + (k * kAttnCols + col) * kStride + d);
-                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-                l += meet_l[k][col] * exp2_fast(meet_m[k][col] - mm);
+                sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+                l += ml[k][col] * exp2_fast((mm[k][col] - top) * cc);
             }
-            if (!whole) {
-                *reinterpret_cast<float4*>(part + e) = s;
-                if (d == 0) { part[kAttnCols * D + col] = mm; part[kAttnCols * D + kAttnCols + col] = l; }
-            } else if (r < n_rows) {
+            if (s.slot >= 0) {
+                *reinterpret_cast<float4*>(part + e) = sum;
+                if (d == 0) { part[kAttnCols * D + col] = top * cc; part[kAttnCols * D + kAttnCols + col] = l; }
+            } else if (r < s.n_rows) {
                 const float inv = l > 0.f || l != l ? 1.f / l : 0.f;     // (no visible token: zeros)
                 const int i = r / p.group;
-                const __half2 y[2] = {__floats2half2_rn(s.x * inv, s.y * inv), __floats2half2_rn(s.z * inv, s.w * inv)};
-                *reinterpret_cast<uint2*>(p.out + (int64_t)(t0 + i) * p.out_ld + (int64_t)(head * p.group + r - i * p.group) * D + d) = *reinterpret_cast<const uint2*>(y);
+                const __half2 y[2] = {__floats2half2_rn(sum.x * inv, sum.y * inv), __floats2half2_rn(sum.z * inv, sum.w * inv)};
+                *reinterpret_cast<uint2*>(p.out + (int64_t)(s.t0 + i) * p.out_ld + (int64_t)(s.head * p.group + r - i * p.group) * D + d) = *reinterpret_cast<const uint2*>(y);
             }
         }
-        if (tid == 0 && ua == 0 && !whole) p.split[blockIdx.x] = make_int4(b, head, seg - head * p.row_blocks, (int)((w + blocks - 1) / span));
-        w += ub - ua;
-        __syncthreads();                                                 // (the ring is free again)
+        if (abort_flag[0]) {                                             // a wait ran out (every warp is past this segment's): the copies in flight land first
+            for (; requested > 0; --requested) {
+                mbar_wait(bar0 + 8 * stage, parity, abort_flag + 1, 0);
+                if (++stage == S) { stage = 0; parity ^= 1; }
+            }
+            break;
+        }
+        if (!AttnRing<D>::kMeetApart) {                                  // (the sums have been read: the ring's memory is free)
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncthreads();
+        }
+        none_even = none_after;
     }
 }
 

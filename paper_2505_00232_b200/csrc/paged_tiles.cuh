@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
             constexpr float kLog2e = 1.4426950408889634f;
             const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * kLog2e, 1e-30f);   // (never 0: hidden scores are -infinity)
             const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
+            const SoftCap cap(mag, p.softcap);
             // this warp's 32 rows of the tile, D / 8 lanes' worth of a row side by side; a lane knows where its own row lies
             const auto load_q = [&](const TileSegment& s) {
                 constexpr int kChunks = D / 8, kRowsAt = 32 / kChunks > 0 ? 32 / kChunks : 1;   // rows of a load
@@ -295,7 +296,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     for (int e = 0; e < N; e += 64) tmem_ld64(ts + e, x + e);
                     if (CAP) {
 #pragma unroll
-                        for (int e = 0; e < N; ++e) x[e] = attn_score<true>(x[e], mag, p.softcap);
+                        for (int e = 0; e < N; ++e) x[e] = cap(x[e]);
                     }
                     const int hi = last - (s.step0 + j) * N, lo = lowest - (s.step0 + j) * N;
                     if (__any_sync(0xffffffffu, hi < N - 1 || lo >= 0) || blocks != (1u << T::kBlocks) - 1) {
