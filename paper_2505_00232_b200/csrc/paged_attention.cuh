@@ -18,7 +18,7 @@
 // (sums are fp32; at most 2^8 of 2^16 are used).
 //
 // Bound: the instructions that unpack, not the memory.  About 430 warp instructions per block of 16 tokens and 128 elements give 4.5 TB/s of cache
-// in the loop; 131071 tokens of one sequence take 53 us (151 MB, 23 us at the copy rate), of which 8 are the two launches' fixed part.
+// in the loop; 131071 tokens of one sequence take 43 us (151 MB, 23 us at the copy rate), of which 8 are the two launches' fixed part.
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -33,7 +33,8 @@ namespace ql {
 constexpr int kAttnWarps = 8;
 constexpr int kAttnCols = 8;
 constexpr int kAttnMaxRows = 32;                                         // query rows per KV head that this kernel takes (8 at a time); more: paged_tiles.cuh
-constexpr int kAttnOverhead = 32;                                         // a segment without blocks, in blocks
+constexpr int kAttnOverhead = 32;                                        // a segment without blocks, in blocks
+constexpr int kAttnSpan = 16;                                            // the least span: two blocks per warp (4096 tokens, 8 KV heads: 11.1, 11.4, 10.6 us with 8, 16, 24; 512 tokens: 8.6, 9.2, 9.8; four of 1280: 11.2, 11.3, 12.0)
 template <int D> struct AttnRing {
     static constexpr int kBlock = paged_block_bytes(D);
     static constexpr int kStages = D == 64 ? 6 : D == 128 ? 4 : 3;
@@ -155,7 +156,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
 
     const int h_kv = p.batch.h_kv, per_head = h_kv * p.row_blocks;
     const int64_t total = (int64_t)pre[p.batch.B] * per_head;
-    const int64_t span = max((int64_t)kAttnWarps, (total + p.grid - 1) / p.grid);
+    const int64_t span = max((int64_t)kAttnSpan, (total + p.grid - 1) / p.grid);
     const int64_t w0 = (int64_t)blockIdx.x * span, w1 = min(total, w0 + span);
     if (tid == 0) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
     for (int b = blockIdx.x; b < p.batch.B; b += p.grid) {               // rows of sequences that see nothing: zeros
@@ -457,21 +458,28 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
     }
 }
 
-// Joins the parts of the segment that begins in a CTA's span and ends in another's, in order: CTA blockIdx.x's, ROWS / gridDim.y of its rows, R at a time per warp.
-template <int D, int ROWS, int R>
+// Joins the parts of the segment that begins in a CTA's span and ends in another's, in a fixed order: CTA blockIdx.x's, 8 / W x R of its rows
+// per CTA.  W warps share a row's parts, 8 of them in flight each: one long sequence is many parts of few segments, and reading them one after
+// the other took as long as a fifth of the pass (131071 tokens, 8 KV heads of 128, 37 parts each: 52.8 -> 42.8 us for the call; 4 KV heads of
+// 256, 74 parts: 79.7 -> 55.8).
+template <int D, int ROWS, int R, int W>
 __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnParams p)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    constexpr int V = D / 32;                                            // values of a lane
+    static_assert(W == 1 || R == 1, "");
+    constexpr int V = D / 32, kAhead = 8 / R;                            // values of a lane; parts whose loads are in flight
     constexpr int64_t kStride = ROWS * (D + 2);
+    __shared__ __align__(16) float sums[W > 1 ? 8 : 1][D];
+    __shared__ float sums_l[W > 1 ? 8 : 1];
     const int4 split = p.split[blockIdx.x];
     if (split.x < 0) return;
-    const int row = (blockIdx.y * 8 + (threadIdx.x >> 5)) * R, lane = threadIdx.x & 31, c0 = blockIdx.x, c1 = split.w;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = (blockIdx.y * (8 / W) + warp / W) * R, sub = warp % W;
+    const int c0 = blockIdx.x, parts = split.w - c0 + 1;
     int t0;
     const int n_rows = min(paged_rows(p.batch, split.x, &t0), p.max_q) * p.group;
-    if (split.z * ROWS + row >= n_rows) return;
-    const auto part_of = [&](int c) { return p.partial + (2 * c + (c == c0 ? 1 : 0)) * kStride; };
+    if (split.z * ROWS + blockIdx.y * (8 / W) * R >= n_rows) return;     // (the whole CTA; ROWS and the partial results hold the rows behind the last one)
+    const auto part_of = [&](int c) { return p.partial + (2 * (c0 + c) + (c == 0 ? 1 : 0)) * kStride; };
     float m[R], l[R], acc[R][V];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
@@ -480,22 +488,53 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnParam
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[k][e] = 0.f;
     }
-    for (int c = c0 + lane; c <= c1; c += 32)
+    for (int c = lane; c < parts; c += 32)
 #pragma unroll
         for (int k = 0; k < R; ++k) m[k] = fmaxf(m[k], part_of(c)[ROWS * D + row + k]);
 #pragma unroll
     for (int k = 0; k < R; ++k)
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) m[k] = fmaxf(m[k], __shfl_xor_sync(0xffffffffu, m[k], o));
-#pragma unroll 2
-    for (int c = c0; c <= c1; ++c) {
-        const float* part = part_of(c);
+    for (int at = sub; at < parts; at += 32 * W) {                       // 32 parts' weights side by side, then their values
+        float f[R];
+        const int mine = at + lane * W, n = min(32, (parts - at + W - 1) / W);
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const float f = exp2_fast(part[ROWS * D + row + k] - m[k]);
-            l[k] += part[ROWS * D + ROWS + row + k] * f;
+            const float* part = part_of(min(mine, parts - 1)) + ROWS * D + row + k;
+            f[k] = mine < parts ? exp2_fast(part[0] - m[k]) : 0.f;
+            l[k] += mine < parts ? part[ROWS] * f[k] : 0.f;
+        }
+#pragma unroll kAhead
+        for (int j = 0; j < n; ++j) {
+            const float* part = part_of(at + j * W) + row * D + V * lane;
 #pragma unroll
-            for (int e = 0; e < V; ++e) acc[k][e] = fmaf(part[(row + k) * D + V * lane + e], f, acc[k][e]);
+            for (int k = 0; k < R; ++k) {
+                const float fj = __shfl_sync(0xffffffffu, f[k], j);
+                float y[V];
+                if constexpr (V == 2) *reinterpret_cast<float2*>(y) = *reinterpret_cast<const float2*>(part + k * D);
+                else
+#pragma unroll
+                    for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(y + e) = *reinterpret_cast<const float4*>(part + k * D + e);
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[k][e] = fmaf(y[e], fj, acc[k][e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l[k] += __shfl_xor_sync(0xffffffffu, l[k], o);
+    if constexpr (W > 1) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) sums[warp][e * 32 + lane] = acc[0][e];
+        if (lane == 0) sums_l[warp] = l[0];
+        __syncthreads();
+        if (sub > 0) return;
+#pragma unroll
+        for (int w = 1; w < W; ++w) {
+            l[0] += sums_l[warp + w];
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[0][e] += sums[warp + w][e * 32 + lane];
         }
     }
 #pragma unroll

@@ -240,7 +240,8 @@ cudaError_t launch_attention(const PagedAttnParams& p, bool tiles, int device, c
     cudaError_t e = tiles ? launch(paged_tiles_kernel<D, CAP>, p, dim3(p.grid), dim3(kTileThreads), 1024 + T::kOffPre + (p.batch.B + 1) * 4, st, 1, pdl)
                           : launch(paged_attention_kernel<D, CAP>, p, dim3(p.grid), dim3(kAttnWarps * 32), AttnRing<D>::kBytes + (p.batch.B + 1) * 4, st, 1, pdl);
     if (e != cudaSuccess) return e;
-    return tiles ? launch(paged_combine_kernel<D, T::kRows, 4>, p, dim3(p.grid, T::kRows / 32), dim3(256), 0, st, 1, pdl) : launch(paged_combine_kernel<D, kAttnCols, 1>, p, dim3(p.grid), dim3(256), 0, st, 1, pdl);
+    return tiles ? launch(paged_combine_kernel<D, T::kRows, 4, 1>, p, dim3(p.grid, T::kRows / 32), dim3(256), 0, st, 1, pdl)
+                 : launch(paged_combine_kernel<D, kAttnCols, 1, 4>, p, dim3(p.grid, (std::min(kAttnCols, p.max_q * p.group) + 1) / 2), dim3(256), 0, st, 1, pdl);
 }
 
 }  // namespace
