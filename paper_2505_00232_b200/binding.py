@@ -215,7 +215,7 @@ def qlinear_unpack(desc: Desc, packed: np.ndarray):
 _half = _raw_stream = _device = _native = _serving = None
 _NATIVE_API = ("qlinear_forward", "qlinear_forward_a8", "qlinear_forward_group", "qlinear_forward_gated", "qlinear_residual_rmsnorm", "qlinear_rope_qkv", "qlinear_embed",
                "qlinear_kv_append_heads", "qlinear_kv_scores_heads", "qlinear_kv_output_heads", "qlinear_kv_output", "qlinear_kv_output_uses_tmp")
-_SERVING_API = ("qlinear_paged_append", "qlinear_paged_read", "qlinear_paged_attention_workspace", "qlinear_paged_attention", "qlinear_adjust_logits")
+_SERVING_API = ("qlinear_paged_append", "qlinear_paged_read", "qlinear_paged_attention_workspace", "qlinear_paged_attention", "qlinear_adjust_logits", "qlinear_rope_tables")
 
 
 def _bind_torch():
@@ -451,11 +451,16 @@ def qlinear_rope_tables(n_pos: int, rot: int, base: float = 10000.0, scaling=Non
     if kind is None or n_pos < 0 or rot < 0:
         raise QLinearError(QL_ERR_INVALID_ARG, "qlinear_rope_tables (unknown scaling or negative size)")
     turns = _ROPE_TURNS.get(kind, (1.0, 2.0))
-    s = qlinear_rope_scaling(kind, original, factor, turns[0] if slow is None else slow, turns[1] if fast is None else fast)
-    device = torch.device("cuda" if device is None else device)
-    if device.type != "cuda":
-        raise QLinearError(QL_ERR_INVALID_ARG, "qlinear_rope_tables (device must be a CUDA device)")
-    if device.index is None:
+    slow, fast = turns[0] if slow is None else slow, turns[1] if fast is None else fast
+    if device is not None:
+        device = torch.device(device)
+        if device.type != "cuda":
+            raise QLinearError(QL_ERR_INVALID_ARG, "qlinear_rope_tables (device must be a CUDA device)")
+    y = (_serving or _bind_torch()._serving).rope_tables(n_pos, rot, base, kind, factor, original, slow, fast, first, None if device is None else device.index, _raw(stream))
+    if y is not None:
+        return y
+    s = qlinear_rope_scaling(kind, original, factor, slow, fast)
+    if device is None or device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())
     st, where = _on_stream(device, stream)
     with where:

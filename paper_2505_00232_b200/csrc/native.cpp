@@ -366,6 +366,7 @@ struct ServingApi {
     decltype(&qlinear_paged_attention_workspace) workspace;
     decltype(&qlinear_paged_attention) attention;
     decltype(&qlinear_adjust_logits) adjust_logits;
+    decltype(&qlinear_rope_tables) rope_tables;
 } serving;
 
 bool small_int(PyObject* o, int64_t* v)                                  // a Python int from 0 to INT_MAX
@@ -557,6 +558,36 @@ PyObject* adjust_logits(PyObject*, PyObject* const* a, Py_ssize_t)
     });
 }
 
+// (n_pos, rot, base, kind, factor, original, slow, fast, first, device, stream): device None (the current one) or its index
+PyObject* rope_tables(PyObject*, PyObject* const* a, Py_ssize_t)
+{
+    return guarded([&]() -> PyObject* {
+        int64_t n_pos, rot, kind, original, first, device = -1;
+        double real[4];                                                  // base, factor, slow, fast
+        if (a[10] != Py_None || !small_int(a[0], &n_pos) || !small_int(a[1], &rot) || !small_int(a[3], &kind) || !small_int(a[5], &original) || !small_int(a[8], &first)) Py_RETURN_NONE;
+        for (int i = 0; i < 4; ++i) {
+            real[i] = PyFloat_AsDouble(a[i == 0 ? 2 : i == 1 ? 4 : 4 + i]);
+            if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+        }
+        if (a[9] == Py_None) device = c10::cuda::current_device();
+        else if (!small_int(a[9], &device) || device >= c10::cuda::device_count()) Py_RETURN_NONE;
+        void* st = stream_on((int)device);
+        const qlinear_rope_scaling s = {(int32_t)kind, (int32_t)original, real[1], real[2], real[3]};
+        at::Tensor cos, sin;
+        if (!done([&] {
+                const at::Device on(at::kCUDA, (at::DeviceIndex)device);
+                cos = at::detail::empty_cuda({n_pos, rot / 2}, at::kFloat, on, std::nullopt);
+                sin = at::detail::empty_cuda({n_pos, rot / 2}, at::kFloat, on, std::nullopt);
+                return serving.rope_tables(cos.data_ptr<float>(), sin.data_ptr<float>(), (int32_t)first, (int32_t)n_pos, (int32_t)rot, real[0], &s, (int32_t)device, st);
+            }, "qlinear_rope_tables")) return nullptr;
+        PyObject* y = PyTuple_New(2);
+        if (!y) return nullptr;
+        PyTuple_SET_ITEM(y, 0, THPVariable_Wrap(std::move(cos)));
+        PyTuple_SET_ITEM(y, 1, THPVariable_Wrap(std::move(sin)));
+        return y;
+    });
+}
+
 template <typename A>
 PyObject* take_entry_points(A* to, PyObject* const* a, Py_ssize_t n)
 {
@@ -578,7 +609,7 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n)
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(init), FAST(forward), FAST(forward_a8), FAST(forward_group), FAST(forward_gated), FAST(residual_rmsnorm), FAST(rope_qkv), FAST(embed),
                          FAST(kv_append), FAST(kv_scores), FAST(kv_scores_one), FAST(kv_output_heads), FAST(kv_output), {nullptr, nullptr, 0, nullptr}};
-PyMethodDef serving_methods[] = {{"init", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(init_serving)), METH_FASTCALL, nullptr}, FAST(paged_append), FAST(paged_read), FAST(paged_attention), FAST(adjust_logits),
+PyMethodDef serving_methods[] = {{"init", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(init_serving)), METH_FASTCALL, nullptr}, FAST(paged_append), FAST(paged_read), FAST(paged_attention), FAST(adjust_logits), FAST(rope_tables),
                                  {nullptr, nullptr, 0, nullptr}};
 PyModuleDef serving_module = {PyModuleDef_HEAD_INIT, "_native._serving", nullptr, -1, serving_methods, nullptr, nullptr, nullptr, nullptr};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

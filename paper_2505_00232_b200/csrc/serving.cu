@@ -87,6 +87,12 @@ extern "C" ql_status qlinear_rope_tables(float* cos_dev, float* sin_dev, int32_t
     p.magnitude = kind == QL_ROPE_YARN ? (float)(0.1 * std::log(s->factor) + 1.0) : 1.f;
     constexpr double kTwoPi = 6.283185307179586476925286766559;
     if (kind == QL_ROPE_NTK) base *= std::pow(s->factor, rot / (rot - 2.0));
+    double low = 0.0, high = 0.0;
+    if (kind == QL_ROPE_YARN) {
+        const auto pair_of = [&](double turns) { return rot * std::log(s->original / (turns * kTwoPi)) / (2.0 * std::log(base)); };
+        low = std::max(std::floor(pair_of(s->fast)), 0.0);
+        high = std::min(std::ceil(pair_of(s->slow)), rot - 1.0);
+    }
     for (int i = 0; i < rot / 2; ++i) {
         double f = std::pow(base, -2.0 * i / rot);
         if (kind == QL_ROPE_LINEAR) f /= s->factor;
@@ -95,8 +101,6 @@ extern "C" ql_status qlinear_rope_tables(float* cos_dev, float* sin_dev, int32_t
             f = f / s->factor * (1.0 - keep) + f * keep;
         }
         if (kind == QL_ROPE_YARN) {                                      // the same over the pairs' numbers
-            const auto pair_of = [&](double turns) { return rot * std::log(s->original / (turns * kTwoPi)) / (2.0 * std::log(base)); };
-            const double low = std::max(std::floor(pair_of(s->fast)), 0.0), high = std::min(std::ceil(pair_of(s->slow)), rot - 1.0);
             const double slowed = std::min(1.0, std::max(0.0, (i - low) / std::max(high - low, 0.001)));
             f = f / s->factor * slowed + f * (1.0 - slowed);
         }
