@@ -240,8 +240,8 @@ __global__ void __launch_bounds__(kSeenThreads) adjust_seen_kernel(const LogitsP
         if (p.frequency) freq = p.frequency[row];
     }
     if (p.bias_ids) {
-        b0 = max(p.bias_start[row], 0);
         b1 = min(p.bias_start[row + 1], p.n_biases);
+        b0 = max(max(p.bias_start[row], 0), b1 - 65535);                 // (as for few rows)
     }
     for (int i = tid; i < kSeenWords / 4; i += kSeenThreads) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();

@@ -265,6 +265,11 @@ extern "C" ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q, i
     if (!batch_of(h, table, table_ld, table_width, kv_len, q_start, B, T, &p.batch) || !attn_plan(h, h_q, B, max_q, &a)) return QL_ERR_INVALID_ARG;
     if (!std::isfinite(scale) || !(softcap >= 0.f) || !std::isfinite(softcap) || window < 0) return QL_ERR_INVALID_ARG;
     if (B == 0 || T == 0 || max_q == 0) return QL_OK;
+    {   // the kernels number the steps of a KV head's segments in 32 bits
+        const int64_t held = std::min((int64_t)table_width * h->d.page_size, (int64_t)INT32_MAX);
+        const int64_t segments = a.tiles ? std::min((int64_t)B * a.row_blocks, (int64_t)T * a.group / a.rows + B) : B;
+        if (segments * (a.tiles ? held / TileShape<128>::N + 1 + kTileOverhead : held / kPagedBlock + 1 + kAttnOverhead) > INT32_MAX) return QL_ERR_INVALID_ARG;
+    }
     const int32_t d = h->d.d_h;
     if (!rows_ok(q, q_ld, (int64_t)h_q * d) || !rows_ok(out, out_ld, (int64_t)h_q * d) || q == out) return QL_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 32) || workspace_bytes < a.bytes) return QL_ERR_INVALID_ARG;

@@ -119,6 +119,21 @@ def test_what_is_not_finite(P, dtype):
     assert (got[2, ~allowed] == -np.inf).all() and got[2, 1] == np.inf and (got[2, [33, 35, 65, 67, 97, 99]] == 0).all()
 
 
+@pytest.mark.parametrize("R", [2, 40])
+def test_more_biases_than_count(P, R):
+    """The last 65535 biases of a row count, for few rows and for many."""
+    import torch
+    V, n = 70003, 70000
+    ids = torch.arange(n, dtype=torch.int32, device="cuda")
+    values = torch.rand(n, device="cuda") + 1
+    start = torch.full((R + 1,), n, dtype=torch.int32, device="cuda")
+    start[:R // 2] = 0                                                   # (one row has them all)
+    y = P.qlinear_adjust_logits(torch.zeros((R, V), device="cuda"), bias_ids=ids, bias_values=values, bias_start=start)
+    want = torch.zeros((R, V), device="cuda")
+    want[R // 2 - 1, n - 65535:n] = values[n - 65535:]
+    assert torch.equal(y, want)
+
+
 def test_capture_streams_and_halves(P, monkeypatch):
     import torch
     a = inputs(np.random.default_rng(3), 7, 5000, 90, np.float16)

@@ -487,6 +487,24 @@ def test_refusals(P, torch):
     refused(lambda: cache.read(*batch.args, 2))
 
 
+@pytest.mark.parametrize("max_q,width,taken", [(1, 1 << 19, True), (1, 1 << 20, False), (64, 1 << 21, True), (64, 1 << 22, False)])
+def test_work_that_32_bits_do_not_count(P, torch, max_q, width, taken):
+    """2048 sequences whose table has room for `width` pages of 16 tokens and no page in it: the steps of a KV head are width + 33 a sequence, width / 4 + 9 with
+    many rows.  No sequence has a token or a row, so none of the table is read (it is shorter than it says)."""
+    B = 2048
+    cache = P.PagedKV(1, 16, 1, 64)
+    kv_len, q_start = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    q = torch.zeros((2, 1, 64), dtype=torch.float16, device="cuda")
+    need = P.binding.lib.qlinear_paged_attention_workspace(cache._h, 1, B, max_q)
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, 7)
+    table = torch.full((1 << 10,), -1, dtype=torch.int32, device="cuda")
+    status = P.binding.lib.qlinear_paged_attention(cache._h, q.data_ptr(), 64, out.data_ptr(), 64, 1, table.data_ptr(), width, width, kv_len.data_ptr(), q_start.data_ptr(), B, 2,
+                                                   max_q, 1.0, 0.0, 0, work.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert status == (P.binding.QL_OK if taken else P.QL_ERR_INVALID_ARG) and (out == 7).all()
+
+
 def test_empty_calls(P, torch):
     batch = Batch(torch, [20], [1], 16)
     cache, _ = filled(P, torch, batch, 2, 64)
