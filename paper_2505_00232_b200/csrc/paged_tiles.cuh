@@ -12,7 +12,9 @@
 // to fp16(q s), which go to shared memory in the operands' swizzled layout: K as rows of elements, V as rows of elements too, read transposed.
 //
 // Warps 0-3, 4-7: softmax of the two tiles (at d_h 256 there is one); warps 8-15: unpack; warps 16 and 17 issue the two products; warp 18 looks up the pages and
-// requests the blocks of 16 tokens (bulk copies to a ring of raw steps in shared memory), so that nothing else waits for global memory between two segments.
+// requests the blocks of 16 tokens (bulk copies to a ring of raw steps in shared memory), so that nothing else waits for global memory between two
+// segments but the softmax warps for the next queries, which they have copied (without passing through registers) while the last product runs.
+// Bound: the softmax (64 exponentials, conversions and a maximum per row and step) and the shared memory's ports; a chunk of 4096 at 16384 runs at 1120 TFLOP/s.
 //
 // Work: the segments of the whole batch, numbered through, each as long as its steps and kTileOverhead more (queries in, rows out, an empty pipeline), in one span of
 // equal length per CTA, as in paged_attention.cuh; a segment cut by a span's end leaves its rows' (m, l, O) in the workspace for paged_combine_kernel.
@@ -45,13 +47,17 @@ template <int D> struct TileShape {
     static constexpr uint32_t kS = 0, kO = NT * 2 * N;                   // columns of tensor memory: two buffers of S per tile, O
 };
 constexpr int kTileThreads = 640;
-constexpr int kTileOverhead = 8;                                         // a segment without steps, in steps (a prompt of 4096: 262 us with 4, 239 with 6, 233 with 9, 236 with 13)
+constexpr int kTileOverhead = 6;                                         // a segment without steps, in steps (three ragged prompts of up to 4096: 444 us with 5, 447 with 6, 450 with 7, 455 with 8; a prompt of 4096: 166, 168, 168, 169)
 
 struct TileSegment {
     int32_t head, row0, n_rows, t0, pos0, end, step0, n, slot;           // rows of the sequence row0 .. (n_rows of it), row 0's token and position, keys [.., end), steps step0 .. + n
     int64_t table;                                                       // (offset of the sequence's row of the page table)
 };
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes)   // (the rest of the 16: zeros)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void tmem_ld64(uint32_t taddr, float* r)
 {
     // the load and its wait form one statement so that no use of r[] can be scheduled between them
@@ -234,35 +240,27 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
             const uint32_t lanes = (uint32_t)(32 * wq) << 16, to = tmem + lanes + T::kO + D * t;
             constexpr float kLog2e = 1.4426950408889634f;
             const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * kLog2e, 1e-30f);   // (never 0: hidden scores are -infinity)
-            const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
             const SoftCap cap(mag, p.softcap);
-            // this warp's 32 rows of the tile, D / 8 lanes' worth of a row side by side; a lane knows where its own row lies
-            const auto load_q = [&](const TileSegment& s) {
-                constexpr int kChunks = D / 8, kRowsAt = 32 / kChunks > 0 ? 32 / kChunks : 1;   // rows of a load
+            // this warp's 32 rows of the tile, copied without waiting, D / 8 lanes' worth of a row side by side; a lane knows where its own row lies
+            const auto request_q = [&](const TileSegment& s) {
+                constexpr int kChunks = D / 8, kRowsAt = 32 / kChunks, kUnroll = D == 256 ? 4 : 32;   // (whole at d_h <= 128: rolled, the loop below it got 5 % slower)
                 const int mine = s.row0 + 128 * t + in_tile, i = mine / p.group;
                 const int64_t at = mine < s.n_rows ? (int64_t)(s.t0 + i) * p.q_ld + (int64_t)(s.head * p.group + mine - i * p.group) * D : -1;
                 const int sub = lane / kChunks, ch = lane - sub * kChunks;
-#pragma unroll
-                for (int r0 = 0; r0 < 32; r0 += 16 * kRowsAt) {          // (16 loads on their way at a time)
-                    uint4 u[16];
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const int r = r0 + k * kRowsAt + sub;
-                        const int64_t from = __shfl_sync(0xffffffffu, at, r & 31);
-                        u[k] = r < 32 && from >= 0 ? *reinterpret_cast<const uint4*>(p.q + from + 8 * ch) : make_uint4(0, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const int r = r0 + k * kRowsAt + sub, row = 32 * wq + r;
-                        u[k].x ^= sign; u[k].y ^= sign; u[k].z ^= sign; u[k].w ^= sign;
-                        if (r < 32) *reinterpret_cast<uint4*>(smem + T::kOffQ + (t * NB + (ch >> 3)) * T::kPanelQ + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = u[k];
-                    }
+#pragma unroll kUnroll
+                for (int r0 = 0; r0 < 32; r0 += kRowsAt) {
+                    const int row = 32 * wq + r0 + sub;
+                    const int64_t from = __shfl_sync(0xffffffffu, at, r0 + sub);
+                    cp_async16(sbase + T::kOffQ + (t * NB + (ch >> 3)) * T::kPanelQ + row * 128 + (((ch & 7) ^ (row & 7)) << 4), p.q + max(from, (int64_t)0) + 8 * ch, from >= 0 ? 16 : 0);
                 }
+            };
+            const auto hand_q = [&]() {
+                asm volatile("cp.async.wait_all;" ::: "memory");
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(qf(t));
             };
-            if (rd.n > 0) load_q(segs[0]);
+            if (rd.n > 0) { request_q(segs[0]); hand_q(); }
             const bool wide_out = ((reinterpret_cast<uintptr_t>(p.out) | (uintptr_t)(p.out_ld * 2)) & 31) == 0;
             uint32_t it = rd.it0;
             bool ok = true;
@@ -361,8 +359,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     if (lane == 0) mbar_arrive(pf(slot));
                 }
                 if (!ok) break;
-                if (si + 1 < rd.n) load_q(segs[si + 1]);                    // (every product with this segment's queries is complete)
-                if (!warp_wait(of(2 * t + ((it - 1) & 1)), ((it - 1) >> 1) & 1, abort_flag, 0xA20 + t)) { ok = false; break; }
+                if (si + 1 < rd.n) request_q(segs[si + 1]);              // (every product with this segment's queries is complete)
+                const bool landed = warp_wait(of(2 * t + ((it - 1) & 1)), ((it - 1) >> 1) & 1, abort_flag, 0xA20 + t);
+                if (si + 1 < rd.n) hand_q();
+                if (!landed) { ok = false; break; }
                 tc_fence_after();
                 const float sum = (l[0].x + l[0].y) + (l[1].x + l[1].y);
                 if (s.slot < 0) {
@@ -412,6 +412,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
         while (rd.on) {
         begin_round();
             // ================================================================ unpack: K and V of every step from the raw blocks to the operands' layout
+            const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
             const int uw = warp - 8;                                     // this warp's (block, panel) pairs: pair kItems * uw + i, panels innermost
             const auto put = [&](uint8_t* row, int chunk, uint32_t word, uint32_t scale) {
                 uint32_t h[4];
@@ -429,6 +430,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     const uint8_t* src = smem + T::kOffRaw + rs * T::kRawStep + blk * paged_block_bytes(D);
                     kw[i] = *reinterpret_cast<const uint4*>(src + 512 * pn + 16 * lane);
                     ks[i] = *reinterpret_cast<const uint2*>(src + paged_k_scales(D) + g * (8 * NB) + 8 * pn);
+                    ks[i].x ^= sign; ks[i].y ^= sign;                    // (a negative scale of the scores)
                     vw[i] = *reinterpret_cast<const uint4*>(src + paged_v_data(D) + 512 * pn + 16 * lane);
                     vs[i] = *reinterpret_cast<const uint2*>(src + paged_v_scales(D) + (2 * pn + (g >> 2)) * 32 + 8 * c);
                 }
