@@ -69,7 +69,7 @@ __device__ __forceinline__ int attn_blocks(const PagedAttnParams& p, int b, int*
     *first = 0;
     if (min(rows, p.max_q) <= 0 || end <= 0) return 0;
     if (p.window > 0) *first = (int)max((int64_t)len - rows + 1 - p.window, (int64_t)0) >> 4;   // the first token that the first row sees
-    return max(0, ((end + 15) >> 4) - *first);
+    return max(0, (int)(((unsigned)end + 15) >> 4) - *first);
 }
 
 __device__ __forceinline__ uint32_t move_matrix(uint32_t a)

@@ -119,7 +119,7 @@ __device__ __forceinline__ int tile_steps(int row0, int n_rows, int rows_all, in
     *first = 0;
     if (row0 >= n_rows || end <= 0) return 0;
     if (window > 0) *first = (int)max((int64_t)pos0 + i0 + 1 - window, (int64_t)0) / N;
-    return max(0, (end + N - 1) / N - *first);
+    return max(0, (int)(((unsigned)end + N - 1) / N) - *first);
 }
 
 template <int D, bool CAP>
@@ -434,6 +434,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     vw[i] = *reinterpret_cast<const uint4*>(src + paged_v_data(D) + 512 * pn + 16 * lane);
                     vs[i] = *reinterpret_cast<const uint2*>(src + paged_v_scales(D) + (2 * pn + (g >> 2)) * 32 + 8 * c);
                 }
+                fence_async_smem();                                      // (these reads before the copy that the arrival allows: without it a copy overtook them, now and then)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(re(rs));
                 if (!warp_wait(empty(sk), ((nk / NS) & 1) ^ 1, abort_flag, 0xA40)) break;

@@ -406,6 +406,22 @@ def test_another_stream_and_determinism(P, torch, new):
     assert all(torch.equal(first, o) for o in outs)
 
 
+@pytest.mark.parametrize("h_q,h_kv,d", [(32, 8, 128), (16, 8, 64), (8, 4, 256)])
+@pytest.mark.parametrize("lens,new", [([3300, 2900, 2501], 3300), ([9001], 400), ([4100] * 24, 1), ([30011, 7], 1)])
+def test_long_batches(P, torch, lens, new, h_q, h_kv, d):
+    """Enough segments and steps to keep every ring full on every SM: the same bits from every run, and sampled rows against 64 bits."""
+    batch = Batch(torch, lens, [new] * len(lens), 64)
+    cache, kv = filled(P, torch, batch, h_kv, d)
+    q = f16(np.random.default_rng(5), batch.T, h_q, d)
+    dev = torch.from_numpy(q).cuda()
+    outs = [cache.attention(dev, *batch.args, batch.max_q) for _ in range(8)]
+    assert all(torch.equal(outs[0], o) for o in outs)
+    rows = batch.rows()
+    rows = [rows[i] for i in np.random.default_rng(6).permutation(len(rows))[:24]]
+    want, tol = attention64(q, kv, batch, d ** -0.5, rows=rows)
+    check(outs[0].cpu().numpy(), want, tol, rows)
+
+
 def test_many_sequences(P, torch):
     """More sequences than a CTA has threads; most of them short."""
     rng = np.random.default_rng(13)
