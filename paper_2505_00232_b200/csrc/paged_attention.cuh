@@ -289,7 +289,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
         int u = s.first + warp;
 #pragma unroll 1
         for (int i = 0; i < n_mine; ++i, u += kAttnWarps) {
-            __syncwarp();                                                // (no lane still reads the block before)
+            fence_async_smem();                                          // (every lane's reads of the block before come before the copy over it)
+            __syncwarp();
             while (requested < min(i + S, AttnRing<D>::kMeetApart ? n_mine + n_next : n_mine)) {
                 const bool here = requested < n_mine;
                 const int k = here ? requested : requested - n_mine;
