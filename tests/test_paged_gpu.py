@@ -422,6 +422,30 @@ def test_long_batches(P, torch, lens, new, h_q, h_kv, d):
     check(outs[0].cpu().numpy(), want, tol, rows)
 
 
+def test_two_streams_at_once(P, torch):
+    """Prompts and generated tokens of two caches, captured apart and replayed side by side: what each gives alone."""
+    jobs = []
+    for lens, new, h_kv, d, seed in (([2000, 1500], 2000, 4, 128, 1), ([5000] * 12, 1, 4, 128, 2)):
+        batch = Batch(torch, lens, [new] * len(lens), 16, seed=seed)
+        cache, _ = filled(P, torch, batch, h_kv, d, seed=seed)
+        q = torch.from_numpy(f16(np.random.default_rng(seed), batch.T, 8, d)).cuda()
+        jobs.append((cache, q, batch))
+    alone = [c.attention(q, *b.args, b.max_q) for c, q, b in jobs]
+    torch.cuda.synchronize()
+    graphs, outs, streams = [], [], [torch.cuda.Stream() for _ in jobs]
+    for c, q, b in jobs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append([c.attention(q, *b.args, b.max_q) for _ in range(3)])
+        graphs.append(g)
+    for _ in range(10):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for got, want in zip(outs, alone) for o in got)
+
+
 def test_many_sequences(P, torch):
     """More sequences than a CTA has threads; most of them short."""
     rng = np.random.default_rng(13)
