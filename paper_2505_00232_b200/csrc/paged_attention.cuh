@@ -32,7 +32,10 @@ namespace ql {
 
 constexpr int kAttnWarps = 8;
 constexpr int kAttnCols = 8;
-constexpr int kAttnMaxRows = 32;                                         // query rows per KV head that this kernel takes (8 at a time); more: paged_tiles.cuh
+// The query rows per KV head that this kernel takes, 8 at a time; more go to paged_tiles.cuh, whose time does not depend on them (us, here and there, 16 sequences of 4096: 16 KV heads
+// of 64, 40 rows 119 and 140, 64 rows 184 and 140; 8 of 128, 32 rows 78 and 86, 40 rows 94 and 86; 4 of 256, 16 rows 55 and 67, 24 rows 75 and 66, 32 rows 94 and 67; one of 16384: 40 rows 35
+// and 47; 30 and 40; 38 and 48, and 24 rows of 256 31 and 47).
+__host__ __device__ constexpr int attn_max_rows(int d) { return d == 64 ? 48 : d == 128 ? 32 : 24; }
 constexpr int kAttnOverhead = 32;                                        // a segment without blocks, in blocks
 constexpr int kAttnSpan = 16;                                            // the least span: two blocks per warp (4096 tokens, 8 KV heads: 11.1, 11.4, 10.6 us with 8, 16, 24; 512 tokens: 8.6, 9.2, 9.8; four of 1280: 11.2, 11.3, 12.0)
 template <int D> struct AttnRing {

@@ -217,7 +217,7 @@ bool attn_plan(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t max_q, AttnPla
     a->group = h_q / h->d.h_kv;
     const int64_t rows = (int64_t)max_q * a->group;
     if (rows > INT32_MAX / 2) return false;
-    a->tiles = rows > kAttnMaxRows;
+    a->tiles = rows > attn_max_rows(h->d.d_h);
     a->rows = a->tiles ? (h->d.d_h == 256 ? TileShape<256>::kRows : TileShape<128>::kRows) : kAttnCols;
     a->row_blocks = (int32_t)((rows + a->rows - 1) / a->rows);
     a->grid = (a->tiles ? 1 : 2) * h->shared.sms;

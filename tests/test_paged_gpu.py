@@ -83,13 +83,13 @@ def filled(P, torch, batch, h_kv, d, seed=1, k_scale=1.0):
 
 
 def attention64(q, kv, batch, scale, softcap=0.0, window=0, rows=None, max_q=None):
-    """(out, bound per element): the definition in 64 bits.  Beyond 32 rows per KV head the keys are rounded to fp16(q s) as well: 2^-11 of each product.  The kernels round the unnormalised weights to fp16 (2^-11 relative, 2^-25 absolute below 2^-14,
+    """(out, bound per element): the definition in 64 bits.  Beyond 48, 32, 24 rows per KV head (d 64, 128, 256) the keys are rounded to fp16(q s) as well: 2^-11 of each product.  The kernels round the unnormalised weights to fp16 (2^-11 relative, 2^-25 absolute below 2^-14,
     of weights whose largest is at least 1), the values q s to fp16 (2^-11) and the result (2^-11, 2^-25 absolute); scores are sums of d products in fp32 whose
     error moves a weight by exp(error) - 1."""
     T, h_q, d = q.shape
     out, tol = np.zeros((T, h_q, d)), np.zeros((T, h_q, d))
     g = h_q // kv[0][0].shape[1]
-    key = 2.0 ** -11 if (max_q or batch.max_q) * g > 32 else 0.0
+    key = 2.0 ** -11 if (max_q or batch.max_q) * g > {64: 48, 128: 32, 256: 24}[d] else 0.0
     for t, b, pos in rows or batch.rows():
         k, v = kv[b]
         lo, hi = (max(0, pos - window + 1) if window else 0), min(pos + 1, len(k))
@@ -420,6 +420,17 @@ def test_long_batches(P, torch, lens, new, h_q, h_kv, d):
     rows = [rows[i] for i in np.random.default_rng(6).permutation(len(rows))[:24]]
     want, tol = attention64(q, kv, batch, d ** -0.5, rows=rows)
     check(outs[0].cpu().numpy(), want, tol, rows)
+
+
+@pytest.mark.parametrize("d,new", [(64, 24), (64, 25), (128, 16), (128, 17), (256, 12), (256, 13)])
+def test_rows_where_the_kernels_change(P, torch, d, new):
+    """The most rows (two query heads a KV head) that the kernel of few rows takes, and one token more."""
+    batch = Batch(torch, [300, new, 77], [new] * 3, 16)
+    cache, kv = filled(P, torch, batch, 2, d)
+    q = f16(np.random.default_rng(8), batch.T, 4, d)
+    got = cache.attention(torch.from_numpy(q).cuda(), *batch.args, new).cpu().numpy()
+    want, tol = attention64(q, kv, batch, d ** -0.5)
+    check(got, want, tol, batch.rows())
 
 
 def test_two_streams_at_once(P, torch):
