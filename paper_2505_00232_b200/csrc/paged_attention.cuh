@@ -14,8 +14,9 @@
 // from the lengths on the device (a scan), so a captured launch follows them.  A CTA's 8 warps take the blocks of a segment in turn, each
 // through a ring of its own in shared memory that goes on from segment to segment (bulk copies, requested by the lane that looked up the page), and
 // meet at the segment's end, when the first blocks of the next one are on their way.  A segment cut by a span's end leaves (m, l, o) in the
-// workspace, which paged_combine_kernel joins in order.  Weights are fp16 relative to a maximum that is raised only when it is passed by 2^8
-// (sums are fp32; at most 2^8 of 2^16 are used).
+// workspace, which paged_combine_kernel joins in order.  Weights are fp16, w_j = exp(x_j - m) with m lying 2^7 (kWeightLift) below the largest score when it is set
+// and raised only when a score passes it by 2^15: they use the range up to 2^15 of fp16's 2^16, and what vanishes from the products, weights below 2^-25, is below 2^-32 of the largest
+// (at m = the largest score it was 2^-25 of it, and the weight of 100000 such tokens, which the fp32 sums of weights did count, was missing from the result).
 //
 // Bound: the instructions that unpack, not the memory.  About 430 warp instructions per block of 16 tokens and 128 elements give 4.5 TB/s of cache
 // in the loop; 131071 tokens of one sequence take 43 us (151 MB, 23 us at the copy rate), of which 8 are the two launches' fixed part.
@@ -30,6 +31,7 @@
 
 namespace ql {
 
+constexpr float kWeightLift = 7.f, kWeightRange = 15.f;                  // the largest weight is 2^7 when m is set, m is raised before one passes 2^15
 constexpr int kAttnWarps = 8;
 constexpr int kAttnCols = 8;
 // The query rows per KV head that this kernel takes, 8 at a time; more go to paged_tiles.cuh, whose time does not depend on them (us, here and there, 16 sequences of 4096: 16 KV heads
@@ -234,7 +236,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
         to = to + 1 == S ? 0 : to + 1;
     };
     int requested = 0;                                                   // blocks of the segment, and on into the next one
-    const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * 1.4426950408889634f, 1e-30f), margin = 8.f / cc;   // weights exp2(cc (x - m)); (cc never 0: hidden scores are -infinity)
+    const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * 1.4426950408889634f, 1e-30f), margin = kWeightRange / cc, lift = kWeightLift / cc;   // weights exp2(cc (x - m)); (cc never 0: hidden scores are -infinity)
     const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
     const SoftCap cap(mag, p.softcap);
 
@@ -357,7 +359,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
                     if (j > last[e & 1] || j <= lowest[e & 1] || no_page) x[e] = -INFINITY;
                 }
             }
-            // the maximum is raised when it is passed by 2^8
+            // m is raised when a weight would pass 2^15
             if (__any_sync(0xffffffffu, fmaxf(x[0], x[2]) > m0 + margin || fmaxf(x[1], x[3]) > m1 + margin)) {
                 float n0 = fmaxf(x[0], x[2]), n1 = fmaxf(x[1], x[3]);
 #pragma unroll
@@ -365,7 +367,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
                     n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, d));
                     n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, d));
                 }
-                n0 = fmaxf(n0, m0); n1 = fmaxf(n1, m1);
+                n0 = fmaxf(n0 - lift, m0); n1 = fmaxf(n1 - lift, m1);
                 const float f0 = exp2_fast((m0 - n0) * cc), f1 = exp2_fast((m1 - n1) * cc);
                 m0 = n0; m1 = n1; l0 *= f0; l1 *= f1;
 #pragma unroll

@@ -8,7 +8,7 @@
 //     O += P V       tcgen05.mma with P from tensor memory, O in tensor memory (fp32)
 // so the scores never leave the SM and no thread needs another's row.  A tile has two buffers of S: the scores of the next step are computed while the softmax has
 // the last ones, which never waits for the tensor core then (steps of 128 keys with one buffer per tile: 1073 TFLOP/s, a chunk of 4096 at 16384; the two tiles ran in
-// step, softmax and products in turn).  The maximum m of a row is raised, and O rescaled, only when it is passed by 2^8.  Keys and values are unpacked from the cache's integers by warps of their own
+// step, softmax and products in turn).  The reference m of a row's weights is raised, and O rescaled, only when a weight would pass 2^15 (as in paged_attention.cuh).  Keys and values are unpacked from the cache's integers by warps of their own
 // to fp16(q s), which go to shared memory in the operands' swizzled layout: K as rows of elements, V as rows of elements too, read transposed.
 //
 // Warps 0-3, 4-7: softmax of the two tiles (at d_h 256 there is one); warps 8-15: unpack; warps 16 and 17 issue the two products; warp 18 looks up the pages and
@@ -316,8 +316,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                         mx[2] = fmaxf(mx[2], x[e + 2]); mx[3] = fmaxf(mx[3], x[e + 3]);
                     }
                     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * cc;
-                    if (__any_sync(0xffffffffu, top > m + 8.f)) {        // the maximum is raised, and with it the scale of the sums
-                        const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
+                    if (__any_sync(0xffffffffu, top > m + kWeightRange)) {   // m is raised, and with it the scale of the sums
+                        const float mn = fmaxf(m, top - kWeightLift), f = exp2_fast(m - mn);
                         m = mn;
                         l[0].x *= f; l[0].y *= f; l[1].x *= f; l[1].y *= f;
                         if (j > 0) {

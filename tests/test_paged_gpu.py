@@ -599,3 +599,26 @@ def test_both_halves_agree(P, torch, monkeypatch):
     monkeypatch.setattr(P.binding, "_serving", Python())
     slow = calls()
     assert all(torch.equal(a, b) and a.shape == b.shape for a, b in zip(fast, slow))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("B,n,new,h_kv,group", [(400, 8191, 1, 1, 2), (1, 70000, 2500, 4, 8)])
+def test_many_light_tokens_behind_a_heavy_one(P, torch, B, n, new, h_kv, group, d):
+    """The first token has nearly all the weight and no value, every other one 2^-25.6 of that weight: the result is what the light ones add up to.  Bound: the scores' sums (and, with
+    many rows, the keys' rounding), weights, values and result in fp16 (2^-11 each), and 2^-32 of the largest weight for every light one: half a step of fp16 below 2^-14, where weights up to 2^7 are held."""
+    cache = P.PagedKV(-(-n // 16), 16, h_kv, d)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    table = torch.arange(-(-n // 16), dtype=torch.int32, device="cuda").expand(B, -1).contiguous()           # (all sequences are the same tokens)
+    k, v = (torch.zeros((n, h_kv, d), dtype=torch.float16, device="cuda") for _ in range(2))
+    k[0], v[1:] = 1, 1
+    cache.append(k, v, table[:1], i32([n]), i32([0, n]))
+    one = held(np.ones((1, d), np.float16))[0]
+    scale = 25.6 * np.log(2) / one.sum()
+    q = torch.ones((B * new, h_kv * group, d), dtype=torch.float16, device="cuda")
+    got = cache.attention(q, table, i32([n] * B), i32((np.arange(B + 1) * new).tolist()), new, scale=scale).double().cpu().numpy()
+    x0 = one.sum() * float(np.float32(scale))
+    light, w = n - new + np.tile(np.arange(new), B), np.exp(-x0)
+    y = light * w / (1 + light * w) * one[0]
+    dx = ((d + 60) * 2.0 ** -24 + (2.0 ** -11 if new > 1 else 0)) * x0
+    tol = y * (2 * np.expm1(dx) + 3 * 2.0 ** -11 + n * 2.0 ** -24) + 2.0 ** -32 * light / (1 + light * w) + 2.0 ** -25
+    assert (np.abs(got - y[:, None, None]).max((1, 2)) <= tol).all()
