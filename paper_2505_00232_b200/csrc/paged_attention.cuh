@@ -51,6 +51,38 @@ template <int D> struct AttnRing {
     static_assert(kMeet <= kRing, "or the ring's memory");
 };
 
+__device__ __forceinline__ float exp2_fast(float x)                      // (2 ulp; subnormal results are zero)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+__device__ __forceinline__ float rcp_fast(float x)                       // (1 ulp; 0 of infinity)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// The soft cap of scores on a base-2 scale: cap log2(e) tanh(y), y = scale dot / cap.  One of two forms, chosen by the host:
+// kCapPlain, caps up to 128: tanh(y) = 1 - 2 / (exp(2 y) + 1), whose rounding errors are of 1, so that a score is off by up to 6 * 2^-24 cap: below 2^-14 there, an eighth of what the
+// fp16 weights are rounded by.  A higher cap would lose the scores in it (10^5: 2 % of a weight; 10^8: everything).
+// kCapHigh: for |y| < 1/4 the score times the series tanh(y) / y = 1 - y^2 / 3 + 2 y^4 / 15 - 17 y^6 / 315 (the next term is below 2^-21 there), else the same exponential: all errors are of
+// the score, which stays what it is as the cap grows.  Ten instructions a score more: two prompts of 4096, 4 KV heads of 128, 184 us plain and 372 high; a token of 24 sequences 23.4 and 24.5.
+enum AttnCap { kCapNone, kCapPlain, kCapHigh };
+constexpr float kMostPlainCap = 128.f;
+struct SoftCap {
+    float in, out, linear, shrink;
+    __device__ SoftCap(float scale, float cap) : in(cap > 0.f ? 2.f * 1.4426950408889634f * scale / cap : 0.f), out(cap * 1.4426950408889634f), linear(scale * 1.4426950408889634f), shrink(cap > 0.f ? scale / cap : 0.f) {}
+    template <AttnCap CAP> __device__ __forceinline__ float of(float dot) const
+    {
+        const float plain = fmaf(-2.f * out, rcp_fast(exp2_fast(dot * in) + 1.f), out);
+        if (CAP == kCapPlain) return plain;
+        const float y = dot * shrink, z = y * y, s = dot * linear;
+        return fabsf(y) < 0.25f ? fmaf(s * z, fmaf(z, fmaf(z, -17.f / 315, 2.f / 15), -1.f / 3), s) : plain;
+    }
+};
+
 struct PagedAttnParams {
     PagedBatch batch;
     const __half* q;             // row t, head h at q + t * q_ld + h * D
@@ -59,7 +91,7 @@ struct PagedAttnParams {
     int4* split;                 // per CTA: sequence (-1: none), KV head, row block of the segment that begins in its span and ends in another's, and the last CTA that holds a part
     int64_t q_ld, out_ld;
     int32_t h_q, group, max_q, row_blocks, window;
-    float scale, softcap;        // (softcap 0: none)
+    float scale, softcap;        // (softcap 0: none; not so far from the scale that SoftCap's constants leave fp32)
     int32_t grid;
 };
 
@@ -83,26 +115,6 @@ __device__ __forceinline__ uint32_t move_matrix(uint32_t a)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
     return r;
 }
-__device__ __forceinline__ float exp2_fast(float x)                      // (2 ulp; subnormal results are zero)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
-__device__ __forceinline__ float rcp_fast(float x)                       // (1 ulp; 0 of infinity)
-{
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-// The soft cap of scores on a base-2 scale: cap log2(e) tanh(scale dot / cap), tanh(y) = 1 - 2 / (exp(2 y) + 1).
-struct SoftCap {
-    float in, out;
-    __device__ SoftCap(float scale, float cap) : in(cap > 0.f ? 2.f * 1.4426950408889634f * scale / cap : 0.f), out(cap * 1.4426950408889634f) {}
-    __device__ __forceinline__ float operator()(float dot) const { return fmaf(-2.f * out, rcp_fast(exp2_fast(dot * in) + 1.f), out); }
-};
-
 // Sums over a scan of the sequences' lengths: pre[b] before sequence b (per head and row block).  Every thread takes part.
 __device__ __forceinline__ void attn_scan(const PagedAttnParams& p, int* pre)
 {
@@ -135,7 +147,7 @@ struct AttnSegment {
     int64_t table, next;                                                 // offset of the sequence's row of the page table; where the next segment begins in the numbering
 };
 
-template <int D, bool CAP>
+template <int D, AttnCap CAP>
 __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(const PagedAttnParams p)
 {
     constexpr int NB = D / 64, kBlock = AttnRing<D>::kBlock, S = AttnRing<D>::kStages, kStride = AttnRing<D>::kMergeStride;
@@ -236,7 +248,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
         to = to + 1 == S ? 0 : to + 1;
     };
     int requested = 0;                                                   // blocks of the segment, and on into the next one
-    const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * 1.4426950408889634f, 1e-30f), margin = kWeightRange / cc, lift = kWeightLift / cc;   // weights exp2(cc (x - m)); (cc never 0: hidden scores are -infinity)
+    const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * 1.4426950408889634f, 1e-30f), margin = kWeightRange / cc;   // weights exp2(cc (x - m)); (cc never 0: hidden scores are -infinity)
     const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
     const SoftCap cap(mag, p.softcap);
 
@@ -348,7 +360,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
             }
             if (CAP) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = cap(x[e]);
+                for (int e = 0; e < 4; ++e) x[e] = cap.of<CAP>(x[e]);
             }
             // hidden tokens (only blocks that some column does not see whole, or without a page)
             if ((uint32_t)(u - seen) >= (uint32_t)n_seen || no_page) {
@@ -367,7 +379,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
                     n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, d));
                     n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, d));
                 }
-                n0 = fmaxf(n0 - lift, m0); n1 = fmaxf(n1 - lift, m1);
+                constexpr float kLift = kWeightLift / kWeightRange;
+                n0 = fmaxf(fmaf(margin, -kLift, n0), m0); n1 = fmaxf(fmaf(margin, -kLift, n1), m1);
                 const float f0 = exp2_fast((m0 - n0) * cc), f1 = exp2_fast((m1 - n1) * cc);
                 m0 = n0; m1 = n1; l0 *= f0; l1 *= f1;
 #pragma unroll

@@ -122,7 +122,7 @@ __device__ __forceinline__ int tile_steps(int row0, int n_rows, int rows_all, in
     return max(0, (int)(((unsigned)end + N - 1) / N) - *first);
 }
 
-template <int D, bool CAP>
+template <int D, AttnCap CAP>
 __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const PagedAttnParams p)
 {
     using T = TileShape<D>;
@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     for (int e = 0; e < N; e += 64) tmem_ld64(ts + e, x + e);
                     if (CAP) {
 #pragma unroll
-                        for (int e = 0; e < N; ++e) x[e] = cap(x[e]);
+                        for (int e = 0; e < N; ++e) x[e] = cap.of<CAP>(x[e]);
                     }
                     const int hi = last - (s.step0 + j) * N, lo = lowest - (s.step0 + j) * N;
                     if (__any_sync(0xffffffffu, hi < N - 1 || lo >= 0) || blocks != (1u << T::kBlocks) - 1) {

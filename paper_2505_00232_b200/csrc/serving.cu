@@ -226,8 +226,8 @@ bool attn_plan(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t max_q, AttnPla
     return true;
 }
 
-template <int D, bool CAP>
-cudaError_t launch_attention(const PagedAttnParams& p, bool tiles, int device, cudaStream_t st, bool pdl)
+template <int D, AttnCap CAP>
+cudaError_t launch_attention_as(const PagedAttnParams& p, bool tiles, int device, cudaStream_t st, bool pdl)
 {
     using T = TileShape<D>;
     static std::atomic<bool> flags[64];
@@ -246,6 +246,13 @@ cudaError_t launch_attention(const PagedAttnParams& p, bool tiles, int device, c
     if (e != cudaSuccess) return e;
     return tiles ? launch(paged_combine_kernel<D, T::kRows, 4, 1>, p, dim3(p.grid, T::kRows / 32), dim3(256), 0, st, 1, pdl)
                  : launch(paged_combine_kernel<D, kAttnCols, 1, 4>, p, dim3(p.grid, (std::min(kAttnCols, p.max_q * p.group) + 1) / 2), dim3(256), 0, st, 1, pdl);
+}
+
+template <int D>
+cudaError_t launch_attention(const PagedAttnParams& p, bool tiles, int device, cudaStream_t st, bool pdl)
+{
+    if (!(p.softcap > 0.f)) return launch_attention_as<D, kCapNone>(p, tiles, device, st, pdl);
+    return p.softcap <= kMostPlainCap ? launch_attention_as<D, kCapPlain>(p, tiles, device, st, pdl) : launch_attention_as<D, kCapHigh>(p, tiles, device, st, pdl);
 }
 
 }  // namespace
@@ -282,14 +289,12 @@ extern "C" ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q, i
     p.split = reinterpret_cast<int4*>(static_cast<char*>(workspace) + a.split_at);
     p.q_ld = q_ld; p.out_ld = out_ld;
     p.h_q = h_q; p.group = a.group; p.max_q = max_q; p.row_blocks = a.row_blocks; p.window = window;
-    p.scale = scale; p.softcap = softcap; p.grid = a.grid;
+    p.scale = scale; p.grid = a.grid;
+    // (a cap below makes all scores one to 30 digits, a cap above leaves them what they are)
+    p.softcap = softcap > 0.f ? std::min(std::max(softcap, 1e-30f * std::max(std::fabs(scale), 1.f)), 1e38f) : 0.f;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool cap = softcap > 0.f;
-    cudaError_t e;
-    if (d == 64) e = cap ? launch_attention<64, true>(p, a.tiles, h->device, st, h->pdl) : launch_attention<64, false>(p, a.tiles, h->device, st, h->pdl);
-    else if (d == 128) e = cap ? launch_attention<128, true>(p, a.tiles, h->device, st, h->pdl) : launch_attention<128, false>(p, a.tiles, h->device, st, h->pdl);
-    else e = cap ? launch_attention<256, true>(p, a.tiles, h->device, st, h->pdl) : launch_attention<256, false>(p, a.tiles, h->device, st, h->pdl);
-    return launched(e);
+    const auto go = d == 64 ? launch_attention<64> : d == 128 ? launch_attention<128> : launch_attention<256>;
+    return launched(go(p, a.tiles, h->device, st, h->pdl));
 }
 
 // ---------------------------------------------------------------------------------------------------- logits

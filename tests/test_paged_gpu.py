@@ -622,3 +622,29 @@ def test_many_light_tokens_behind_a_heavy_one(P, torch, B, n, new, h_kv, group, 
     dx = ((d + 60) * 2.0 ** -24 + (2.0 ** -11 if new > 1 else 0)) * x0
     tol = y * (2 * np.expm1(dx) + 3 * 2.0 ** -11 + n * 2.0 ** -24) + 2.0 ** -32 * light / (1 + light * w) + 2.0 ** -25
     assert (np.abs(got - y[:, None, None]).max((1, 2)) <= tol).all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("new", [1, 60])
+@pytest.mark.parametrize("softcap", [1e-3, 128.0, 1e3, 1e5, 1e8, 3e38])
+def test_soft_caps_of_every_size(P, torch, softcap, new, d):
+    """Caps far below the scores and far above them, where capped scores are the scores.  Up to 128 a score is off by roundings of numbers up to the cap (as in attention64); above, by those of the score
+    alone: exponential form for |y| >= 1/4, 1.5 * 2^-22 absolute of tanh(y) >= 0.244 (2 ulp of the exponential, 1 of the reciprocal, a sum, a product) and 3 roundings of its argument, and 2 of the factor, 30 * 2^-24 in all;
+    series below, 6 * 2^-24 cut off and 8 roundings."""
+    batch = Batch(torch, [500, 61], [new, new], 16)
+    cache, kv = filled(P, torch, batch, 2, d)
+    q = f16(np.random.default_rng(3), batch.T, 4, d)
+    key = 2.0 ** -11 if new * 2 > {64: 48, 128: 32, 256: 24}[d] else 0.0
+    for size in (1.0, 300.0):                                            # (scores of a few units; of hundreds: tanh of 1e3 on both sides of 1/4)
+        scale = size * d ** -0.5
+        got = cache.attention(torch.from_numpy(q).cuda(), *batch.args, new, scale=scale, softcap=softcap).cpu().numpy().astype(np.float64)
+        for t, b, pos in batch.rows():
+            for h in range(4):
+                k, v, q64 = kv[b][0][:pos + 1, h // 2], kv[b][1][:pos + 1, h // 2], q[t, h].astype(np.float64)
+                x = softcap * np.tanh(k @ q64 * scale / softcap)
+                dx = np.minimum((key + (d + 40) * 2.0 ** -24) * (np.abs(k) @ np.abs(q64)) * scale, 2 * softcap) + (16 * 2.0 ** -24 * softcap if softcap <= 128 else 40 * 2.0 ** -24 * np.abs(x))
+                w = np.exp(x - x.max())
+                rel = np.expm1(dx + 2.0 ** -21 * (1 + np.abs(x - x.max()))).max()
+                want = w @ v / w.sum()
+                tol = (2 * rel + 2 * 2.0 ** -11 + len(k) * 2.0 ** -24) * (w @ np.abs(v)) / w.sum() + 2.0 ** -32 / w.sum() * np.abs(v).sum(0)
+                assert (np.abs(got[t, h] - want) <= 1.01 * tol + 2.0 ** -11 * np.abs(want) + 2.0 ** -25).all(), (t, h, size)
