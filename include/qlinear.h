@@ -334,8 +334,8 @@ ql_status qlinear_rope_tables(float* cos_dev, float* sin_dev, int32_t first, int
  *
  * The calls below take a BATCH: sequence b of B has the rows q_start[b] .. q_start[b + 1] - 1 of the call's T rows (its new tokens, its last ones) and
  * kv_len[b] tokens with them; token j of it lies in page table[b * table_ld + j / page_size], j < table_width * page_size.  table, kv_len and q_start [B + 1] are int32 device
- * memory, read by the kernels: a captured call follows what they hold when it is replayed.  Entries of the table that no visible token needs are not looked at, and
- * those outside the pool (-1, say) give a token no place: it is not stored, reads as zero and is not attended to.  Rows of no sequence (before q_start[0], from q_start[B] on:
+ * memory, read by the kernels: a captured call follows what they hold when it is replayed.  Of the table only the entries of tokens are read
+ * that a row of the call appends, reads or sees (and, with a window and many rows, of up to 63 tokens in front of the first one): it need not hold more.  Entries outside the pool (-1, say) give a token no place: it is not stored, reads as zero and is not attended to.  Rows of no sequence (before q_start[0], from q_start[B] on:
  * a padded batch) are left as they are, in every output; a sequence whose rows do not lie in [0, T) has none, and no row may be two sequences'.  B <= QL_PAGED_MAX_SEQUENCES.  Two rows must not
  * stand for one place of the pool in one append.
  *

@@ -50,7 +50,7 @@ constexpr int kTileThreads = 640;
 constexpr int kTileOverhead = 6;                                         // a segment without steps, in steps (three ragged prompts of up to 4096: 444 us with 5, 447 with 6, 450 with 7, 455 with 8; a prompt of 4096: 166, 168, 168, 169)
 
 struct TileSegment {
-    int32_t head, row0, n_rows, t0, pos0, end, step0, n, slot;           // rows of the sequence row0 .. (n_rows of it), row 0's token and position, keys [.., end), steps step0 .. + n
+    int32_t head, row0, n_rows, t0, pos0, end, step0, n, slot;           // rows of the sequence row0 .. (n_rows of it), row 0's token and position, keys [.., end) that one of them sees, steps step0 .. + n
     int64_t table;                                                       // (offset of the sequence's row of the page table)
 };
 
@@ -272,9 +272,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                 float m = -1e30f;
                 float2 l[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 const int32_t* table = bt.table + s.table;
-                const auto page_of = [&](int step) {                     // (lane: the page of the block `lane` from that step on)
-                    const int at = (step * T::kBlocks + lane) >> bt.log2_blocks;
-                    return at < bt.table_width ? table[at] : -1;
+                const int end_block = (int)(((unsigned)s.end + kPagedBlock - 1) / kPagedBlock);
+                const auto page_of = [&](int step) {                     // (lane: the page of the block `lane` from that step on; any page for blocks behind the last: no row sees their tokens, and the table may end there)
+                    const int block = step * T::kBlocks + lane;
+                    return block < end_block ? table[block >> bt.log2_blocks] : 0;
                 };
                 constexpr int kAhead = 32 / T::kBlocks;                  // steps of one look-up
                 int pg = page_of(s.step0);
@@ -517,7 +518,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     if (sb > sa) {
                         const bool whole = sa == 0 && sb == steps;
                         if (lane == 0) {
-                            segs[n] = TileSegment{head, r * T::kRows, n_rows, t0, len - rows_all, min(len, held), first + sa, sb - sa, whole ? -1 : sa > 0 ? 0 : 1, lo * bt.table_ld};
+                            segs[n] = TileSegment{head, r * T::kRows, n_rows, t0, len - rows_all, min(len - rows_all + (min((r + 1) * T::kRows, n_rows) - 1) / p.group + 1, held), first + sa, sb - sa, whole ? -1 : sa > 0 ? 0 : 1, lo * bt.table_ld};
                             if (sa == 0 && !whole) p.split[blockIdx.x] = make_int4(lo, head, r, (int)((ww - ua + length - 1) / span));
                         }
                         ++n;
@@ -604,8 +605,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                 while (sl < rd.n && jl >= segs[sl].n) jl -= segs[sl++].n;
                 pages_next = -1;
                 if (sl < rd.n) {
-                    const int at = ((segs[sl].step0 + jl) * T::kBlocks + (lane & (T::kBlocks - 1))) >> bt.log2_blocks;
-                    if (at < bt.table_width) pages_next = bt.table[segs[sl].table + at];
+                    const int block = (segs[sl].step0 + jl) * T::kBlocks + (lane & (T::kBlocks - 1));
+                    if (block < (int)(((unsigned)segs[sl].end + kPagedBlock - 1) / kPagedBlock)) pages_next = bt.table[segs[sl].table + (block >> bt.log2_blocks)];
                 }
                 j_w += kWindow;
                 while (si_w < rd.n && j_w >= segs[si_w].n) j_w -= segs[si_w++].n;

@@ -648,3 +648,20 @@ def test_soft_caps_of_every_size(P, torch, softcap, new, d):
                 want = w @ v / w.sum()
                 tol = (2 * rel + 2 * 2.0 ** -11 + len(k) * 2.0 ** -24) * (w @ np.abs(v)) / w.sum() + 2.0 ** -32 / w.sum() * np.abs(v).sum(0)
                 assert (np.abs(got[t, h] - want) <= 1.01 * tol + 2.0 ** -11 * np.abs(want) + 2.0 ** -25).all(), (t, h, size)
+
+
+@pytest.mark.parametrize("new,most", [(1, 1), (3, 3), (3, 2), (70, 70), (700, 700), (700, 300)])
+@pytest.mark.parametrize("window", [0, 90])
+def test_a_table_that_ends_with_the_last_token(P, torch, new, most, window):
+    """A table said to be wide that holds the entries up to the last row's token (or to that of the last row served) and no more: none behind them is read."""
+    n, d = 1111, 128
+    batch = Batch(torch, [n], [new], 16)
+    cache, _ = filled(P, torch, batch, 2, d)
+    q = torch.from_numpy(f16(np.random.default_rng(4), new, 8, d)).cuda()
+    want = cache.attention(q, *batch.args, most, window=window, out=torch.zeros_like(q))
+    short = batch.args[0][0, :-(-(n - new + most) // 16)].clone()
+    work = torch.empty(P.lib.qlinear_paged_attention_workspace(cache._h, 8, 1, most), dtype=torch.uint8, device="cuda")
+    out = torch.zeros_like(q)
+    assert P.lib.qlinear_paged_attention(cache._h, q.data_ptr(), 8 * d, out.data_ptr(), 8 * d, 8, short.data_ptr(), 1 << 20, 1 << 20, batch.args[1].data_ptr(), batch.args[2].data_ptr(), 1, new, most,
+                                         d ** -0.5, 0.0, window, work.data_ptr(), work.numel(), torch.cuda.current_stream().cuda_stream) == P.binding.QL_OK
+    assert torch.equal(out, want)
