@@ -547,6 +547,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                         const int slot = 2 * t + (it & 1);
                         // (the weights of step it - 2 lay in this buffer)
                         if (it >= 2 && !(ok = __all_sync(0xffffffffu, mbar_wait_hot(of(slot), ((it >> 1) & 1) ^ 1, abort_flag, 0xA64 + slot)))) break;
+                        tc_fence_after();
                         if (elect_one()) {
 #pragma unroll
                             for (int pn = 0; pn < NB; ++pn)
