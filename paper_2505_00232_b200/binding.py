@@ -443,6 +443,12 @@ def _on_stream(device, stream):
     return _raw_stream(device.index), torch.cuda.device(device)
 
 
+def _check_i32(where: str, *numbers) -> None:
+    """Refuses what int32_t does not hold: ctypes would pass its lower 32 bits."""
+    if not all(-2 ** 31 <= n < 2 ** 31 for n in numbers):
+        raise QLinearError(QL_ERR_INVALID_ARG, where + " (a number beyond 32 bits)")
+
+
 def qlinear_rope_tables(n_pos: int, rot: int, base: float = 10000.0, scaling=None, factor: float = 1.0, original: int = 8192, slow=None, fast=None, first: int = 0, device=None, stream=None):
     """(cos, sin) fp32 CUDA [n_pos, rot / 2] of the positions first .. first + n_pos - 1, with the frequency scaling of a long context (None, "linear", "ntk",
     "llama3", "yarn"; the formulas: include/qlinear.h), for qlinear_rope_qkv and PagedKV.append."""
@@ -450,6 +456,7 @@ def qlinear_rope_tables(n_pos: int, rot: int, base: float = 10000.0, scaling=Non
     kind = ROPE_SCALINGS.get(scaling)
     if kind is None or n_pos < 0 or rot < 0:
         raise QLinearError(QL_ERR_INVALID_ARG, "qlinear_rope_tables (unknown scaling or negative size)")
+    _check_i32("qlinear_rope_tables", n_pos, rot, original, first)
     turns = _ROPE_TURNS.get(kind, (1.0, 2.0))
     slow, fast = turns[0] if slow is None else slow, turns[1] if fast is None else fast
     if device is not None:
@@ -486,6 +493,7 @@ def qlinear_adjust_logits(logits, tokens=None, start=None, n_prompt=None, repeti
     if logits.dtype not in (torch.float16, torch.float32) or not rows_of(logits, logits.dtype):
         raise QLinearError(QL_ERR_INVALID_ARG, where + " (logits must be fp16 or fp32 CUDA [rows, vocab])")
     R, V = logits.shape
+    _check_i32(where, R, V, *(t.numel() for t in (tokens, bias_ids) if t is not None))
     if (tokens is None) != (start is None) or not vector(tokens, torch.int32, None) or not vector(start, torch.int32, R + 1) or not vector(n_prompt, torch.int32, R) \
             or not all(vector(t, torch.float32, R) for t in (repetition, presence, frequency)):
         raise QLinearError(QL_ERR_INVALID_ARG, where + " (history: int32 tokens, start [rows + 1], n_prompt [rows]; fp32 penalties [rows])")
@@ -518,6 +526,7 @@ class PagedKV:
     def __init__(self, n_pages: int, page_size: int, h_kv: int, d_h: int, device=None):
         import torch
         _bind_torch()
+        _check_i32("PagedKV", n_pages, page_size, h_kv, d_h)
         self.n_pages, self.page_size, self.h_kv, self.d_h = n_pages, page_size, h_kv, d_h
         desc = qlinear_paged_desc(n_pages, page_size, h_kv, d_h)
         size = int(lib.qlinear_paged_page_bytes(ctypes.byref(desc)))
@@ -548,6 +557,7 @@ class PagedKV:
         B, W = page_table.shape if ok else (0, 0)
         if not ok or tuple(kv_len.shape) != (B,) or tuple(q_start.shape) != (B + 1,) or not kv_len.is_contiguous() or not q_start.is_contiguous() or (W > 1 and page_table.stride(1) != 1):
             raise QLinearError(QL_ERR_INVALID_ARG, where + " (int32 page_table [B, pages], kv_len [B], q_start [B + 1] on the cache's device)")
+        _check_i32(where, B, W, T)
         return page_table.data_ptr() if page_table.numel() else None, max(page_table.stride(0), W) if B <= 1 else page_table.stride(0), W, kv_len.data_ptr(), q_start.data_ptr(), B, T
 
     def append(self, k, v, page_table, kv_len, q_start, q=None, cos=None, sin=None, interleaved: bool = False, q_out=None, stream=None):
@@ -570,10 +580,12 @@ class PagedKV:
             if any(t.dtype != torch.float32 or t.device != self.device or t.dim() != 2 or not t.is_contiguous() for t in (cos, sin)) or cos.shape != sin.shape:
                 raise QLinearError(QL_ERR_INVALID_ARG, where + " (cos, sin must be contiguous fp32 CUDA [n_pos, rot / 2])")
             n_pos, rot = cos.shape[0], 2 * cos.shape[1]
+            _check_i32(where, n_pos, rot)
         st, here = _on_stream(self.device, stream)
         q_ld = out_ld = h_q = 0
         if q is not None:
             q_ld, h_q = self._rows(q, None, where)
+            _check_i32(where, h_q)
             if q_out is None:
                 with here:
                     q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -614,6 +626,7 @@ class PagedKV:
         q_ld, h_q = self._rows(q, None, where)
         T = q.shape[0]
         batch = self._batch(page_table, kv_len, q_start, T, where)
+        _check_i32(where, h_q, max_q, window)
         if h_q % self.h_kv or max_q < 0:
             raise QLinearError(QL_ERR_INVALID_ARG, where + " (query heads a multiple of the KV heads, max_q >= 0)")
         st, here = _on_stream(self.device, stream)

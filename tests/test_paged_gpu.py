@@ -665,3 +665,15 @@ def test_a_table_that_ends_with_the_last_token(P, torch, new, most, window):
     assert P.lib.qlinear_paged_attention(cache._h, q.data_ptr(), 8 * d, out.data_ptr(), 8 * d, 8, short.data_ptr(), 1 << 20, 1 << 20, batch.args[1].data_ptr(), batch.args[2].data_ptr(), 1, new, most,
                                          d ** -0.5, 0.0, window, work.data_ptr(), work.numel(), torch.cuda.current_stream().cuda_stream) == P.binding.QL_OK
     assert torch.equal(out, want)
+
+
+def test_numbers_beyond_32_bits(P, torch):
+    """Refused: their lower 32 bits would be another call (a window of 5, a single row)."""
+    batch = Batch(torch, [60], [2], 16)
+    cache, _ = filled(P, torch, batch, 2, 64)
+    q = torch.zeros((2, 4, 64), dtype=torch.float16, device="cuda")
+    for call in (lambda: cache.attention(q, *batch.args, 2, window=2 ** 32 + 5), lambda: cache.attention(q, *batch.args, 2 ** 32 + 1), lambda: cache.read(*batch.args, 2 ** 32)):
+        with pytest.raises(P.QLinearError) as e:
+            call()
+        assert e.value.status == P.QL_ERR_INVALID_ARG
+    cache.attention(q, *batch.args, 2, window=2 ** 31 - 1)

@@ -75,3 +75,18 @@ def test_logits_refused(change):
 
 def test_logits_of_nothing():
     assert logits(rows=0) == binding.QL_OK
+
+
+@pytest.mark.parametrize("change", [{"n_pos": 2 ** 32}, {"rot": 2 ** 32 + 64}, {"first": 2 ** 32}, {"first": 2 ** 31}, {"first": -2 ** 32}, {"scaling": "yarn", "factor": 2.0, "original": 2 ** 32 + 8192}])
+def test_tables_of_numbers_beyond_32_bits(change):
+    """Refused: their lower 32 bits would be another call."""
+    with pytest.raises(P.QLinearError) as e:
+        P.qlinear_rope_tables(**{"n_pos": 4, "rot": 64, **change})
+    assert e.value.status == BAD
+
+
+@pytest.mark.parametrize("args", [(2 ** 32 + 4, 16, 2, 64), (4, 2 ** 32 + 16, 2, 64), (4, 16, 2 ** 32 + 2, 64), (4, 16, 2, 2 ** 32 + 64)])
+def test_caches_of_numbers_beyond_32_bits(args):
+    with pytest.raises(P.QLinearError) as e:
+        P.PagedKV(*args)
+    assert e.value.status == BAD
