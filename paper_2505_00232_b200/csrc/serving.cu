@@ -64,6 +64,7 @@ bool batch_of(qlinear_paged_t h, const int32_t* table, int64_t table_ld, int32_t
 }
 bool rows_ok(const void* p, int64_t ld, int64_t width) { return p && aligned(p, 16) && ld >= width && ld % 8 == 0; }
 bool timed_out(qlinear_paged_t h) { return *h->shared.status_host != 0; }
+unsigned pieces(int64_t n, int64_t size) { return (unsigned)((n + size - 1) / size); }   // (n up to 2^31 - 1)
 ql_status launched(cudaError_t e)
 {
     if (e != cudaSuccess) cudaGetLastError();
@@ -113,7 +114,7 @@ extern "C" ql_status qlinear_rope_tables(float* cos_dev, float* sin_dev, int32_t
     DeviceGuard guard(device);
     if (!guard.ok) { cudaGetLastError(); return QL_ERR_CUDA; }
     const int per_block = 256 / (p.pairs / 4);
-    return launched(launch(rope_tables_kernel, p, dim3((unsigned)std::min((n_pos + per_block - 1) / per_block, 8 * sms)), dim3(256), 0, static_cast<cudaStream_t>(stream), 1, pdl_enabled()));
+    return launched(launch(rope_tables_kernel, p, dim3(std::min(pieces(n_pos, per_block), 8u * sms)), dim3(256), 0, static_cast<cudaStream_t>(stream), 1, pdl_enabled()));
 }
 
 // ---------------------------------------------------------------------------------------------------- paged cache
@@ -311,15 +312,15 @@ cudaError_t launch_logits(LogitsParams p, int device, int sms, cudaStream_t st)
         flags[device].store(true, std::memory_order_release);
     }
     const bool pdl = pdl_enabled(), some = p.tokens || p.bias_ids;
-    const int tiles = (p.vocab + TILE - 1) / TILE;
+    const unsigned tiles = pieces(p.vocab, TILE);
     // one launch until its CTAs fill the SMs a few times over: each goes through its row's whole history (rows of 128256, history of 1280, one launch / two: 1 row 5.6 / 7.4 us,
     // 8 rows 6.4 / 7.4, 16 rows 7.8 / 8.2, 256 rows 79 / 29)
     if (some && (int64_t)p.rows * tiles <= 4 * sms)
         return launch(adjust_logits_kernel<T, TILE>, p, dim3(tiles, p.rows), dim3(kLogitsThreads), TILE * 8, st, 1, pdl);
     p.masked = p.mask || p.x != p.y;
     cudaError_t e = cudaSuccess;
-    if (p.masked) e = launch(mask_logits_kernel<T>, p, dim3((p.vocab + kPiece - 1) / kPiece, p.rows), dim3(kLogitsThreads), 0, st, 1, pdl);
-    if (e == cudaSuccess && some) e = launch(adjust_seen_kernel<T>, p, dim3((p.vocab + kSeenTokens - 1) / kSeenTokens, p.rows), dim3(kSeenThreads), kSeenBytes, st, 1, pdl);
+    if (p.masked) e = launch(mask_logits_kernel<T>, p, dim3(pieces(p.vocab, kPiece), p.rows), dim3(kLogitsThreads), 0, st, 1, pdl);
+    if (e == cudaSuccess && some) e = launch(adjust_seen_kernel<T>, p, dim3(pieces(p.vocab, kSeenTokens), p.rows), dim3(kSeenThreads), kSeenBytes, st, 1, pdl);
     return e;
 }
 

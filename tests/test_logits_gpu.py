@@ -188,3 +188,21 @@ def test_refusals(P):
     refused(x, mask=mask[:3])
     refused(x, out=x.float())
     refused(x, out=x[:, :499])
+
+
+def test_the_largest_vocabulary(P):
+    """2^31 - 1 tokens of a row: the first and the last ones, and the bits of the last word of the mask."""
+    import torch
+    V = 2 ** 31 - 1
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    x = torch.zeros((1, V), dtype=torch.float16, device="cuda")
+    at = torch.tensor([0, 3, 2 ** 30, V - 2050, V - 2, V - 1], device="cuda")
+    history = dict(tokens=i32(3, V - 1, -1, -2 ** 31), start=i32(0, 4), presence=torch.ones(1, device="cuda"))
+    biases = dict(bias_ids=i32(3, V - 2, 2 ** 30), bias_values=torch.tensor([5.0, 6.0, 7.0], device="cuda"), bias_start=i32(0, 3))
+    y = P.qlinear_adjust_logits(x, **history, **biases)
+    assert y[0, at].tolist() == [0, 4, 7, 0, 6, -1] and int(y.count_nonzero()) == 4
+    mask = torch.full((1, 2 ** 26), -1, dtype=torch.int32, device="cuda")
+    mask[0, 0], mask[0, -1] = ~1, ~(1 << 30)
+    y = P.qlinear_adjust_logits(x, **history, **biases, mask=mask, out=y)
+    assert y[0, at].tolist() == [-float("inf"), 4, 7, 0, 6, -float("inf")] and int(y.isinf().sum()) == 2
+    assert P.qlinear_adjust_logits(x, mask=mask, out=x) is x and x[0, at].tolist() == [-float("inf"), 0, 0, 0, 0, -float("inf")]

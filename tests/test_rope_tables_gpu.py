@@ -74,3 +74,22 @@ def test_another_stream(P):
     s.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(a, P.qlinear_rope_tables(3000, 128)))
     assert P.qlinear_rope_tables(0, 64)[0].shape == (0, 32)
+
+
+def test_every_position(P):
+    """2^31 - 1 positions of the smallest head: the first, some in between and the last ones (bounds: test_tables)."""
+    import torch
+    torch.cuda.empty_cache()
+    n, rot = 2 ** 31 - 1, 16
+    if torch.cuda.mem_get_info()[0] < 4 * n * rot + (4 << 30):
+        pytest.skip("the tables take 137 GB")
+    tables = P.qlinear_rope_tables(n, rot)
+    f = frequencies(rot, 10000.0, None, 1.0)
+    for pos in (np.arange(300), 2 ** 28 * np.arange(1, 8) + 5, n - 1 - np.arange(300)):
+        angle = np.outer(pos.astype(np.float64), f)
+        tol = angle * 32 * 2.0 ** -53 + 2 * math.pi * 2.0 ** -25 + 4 * 2.0 ** -24
+        at = torch.from_numpy(pos).cuda()
+        for t, want in zip(tables, (np.cos(angle), np.sin(angle))):
+            assert (np.abs(t[at].cpu().numpy() - want) <= tol).all()
+    del tables, t
+    torch.cuda.empty_cache()
