@@ -64,22 +64,59 @@ __device__ __forceinline__ float rcp_fast(float x)                       // (1 u
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float a0, float a1, float b, float c)                           // (a0 b + c, a1 b + c)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
 // The soft cap of scores on a base-2 scale: cap log2(e) tanh(y), y = scale dot / cap.  One of two forms, chosen by the host:
 // kCapPlain, caps up to 128: tanh(y) = 1 - 2 / (exp(2 y) + 1), whose rounding errors are of 1, so that a score is off by up to 6 * 2^-24 cap: below 2^-14 there, an eighth of what the
 // fp16 weights are rounded by.  A higher cap would lose the scores in it (10^5: 2 % of a weight; 10^8: everything).
 // kCapHigh: for |y| < 1/4 the score times the series tanh(y) / y = 1 - y^2 / 3 + 2 y^4 / 15 - 17 y^6 / 315 (the next term is below 2^-21 there), else the same exponential: all errors are of
-// the score, which stays what it is as the cap grows.  Ten instructions a score more: two prompts of 4096, 4 KV heads of 128, 184 us plain and 372 high; a token of 24 sequences 23.4 and 24.5.
+// the score, which stays what it is as the cap grows.  Five more instructions a score: two prompts of 4096, 4 KV heads of 128, 184 us plain and 240 high; a token of 24 sequences of 4096 23.5 and 24.9.
 enum AttnCap { kCapNone, kCapPlain, kCapHigh };
 constexpr float kMostPlainCap = 128.f;
 struct SoftCap {
     float in, out, linear, shrink;
     __device__ SoftCap(float scale, float cap) : in(cap > 0.f ? 2.f * 1.4426950408889634f * scale / cap : 0.f), out(cap * 1.4426950408889634f), linear(scale * 1.4426950408889634f), shrink(cap > 0.f ? scale / cap : 0.f) {}
-    template <AttnCap CAP> __device__ __forceinline__ float of(float dot) const
+    template <AttnCap CAP, int N> __device__ __forceinline__ void on(float* x) const   // (two scores to an instruction: the kernel of many rows waits for its instructions)
     {
-        const float plain = fmaf(-2.f * out, rcp_fast(exp2_fast(dot * in) + 1.f), out);
-        if (CAP == kCapPlain) return plain;
-        const float y = dot * shrink, z = y * y, s = dot * linear;
-        return fabsf(y) < 0.25f ? fmaf(s * z, fmaf(z, fmaf(z, -17.f / 315, 2.f / 15), -1.f / 3), s) : plain;
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+            const float2 dot = make_float2(x[e], x[e + 1]), a = mul2(dot, make_float2(in, in)), b = add2(make_float2(exp2_fast(a.x), exp2_fast(a.y)), make_float2(1.f, 1.f));
+            float2 r = fma2(rcp_fast(b.x), rcp_fast(b.y), -2.f * out, out);
+            if (CAP == kCapHigh) {
+                const float2 y = mul2(dot, make_float2(shrink, shrink)), z = mul2(y, y), s = mul2(dot, make_float2(linear, linear));
+                const float2 c = add2(mul2(z, add2(mul2(z, fma2(z.x, z.y, -17.f / 315, 2.f / 15)), make_float2(-1.f / 3, -1.f / 3))), make_float2(1.f, 1.f)), t = mul2(s, c);
+                if (fabsf(y.x) < 0.25f) r.x = t.x;
+                if (fabsf(y.y) < 0.25f) r.y = t.y;
+            }
+            x[e] = r.x;
+            x[e + 1] = r.y;
+        }
     }
 };
 
@@ -358,10 +395,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
                     x[2] = fmaf(t[2], sc.y, x[2]); x[3] = fmaf(t[3], sc.y, x[3]);
                 }
             }
-            if (CAP) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = cap.of<CAP>(x[e]);
-            }
+            if (CAP) cap.on<CAP, 4>(x);
             // hidden tokens (only blocks that some column does not see whole, or without a page)
             if ((uint32_t)(u - seen) >= (uint32_t)n_seen || no_page) {
                 const int j0 = u * 16;

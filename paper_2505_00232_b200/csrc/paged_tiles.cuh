@@ -78,25 +78,6 @@ __device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const uint32_t r
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ float2 fma2(float a0, float a1, float b, float c)                           // (a0 b + c, a1 b + c)
-{
-    float2 r;
-    asm("{\n\t.reg .b64 a, b, c, d;\n\t"
-        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
-        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a0), "f"(a1), "f"(b), "f"(c));
-    return r;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    float2 r;
-    asm("{\n\t.reg .b64 a, b, d;\n\t"
-        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
-        "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
 // 32 bytes in one store.
 __device__ __forceinline__ void store32(void* p, const uint32_t r[8])
 {
@@ -293,10 +274,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     float x[N];
 #pragma unroll
                     for (int e = 0; e < N; e += 64) tmem_ld64(ts + e, x + e);
-                    if (CAP) {
-#pragma unroll
-                        for (int e = 0; e < N; ++e) x[e] = cap.of<CAP>(x[e]);
-                    }
+                    if (CAP) cap.on<CAP, N>(x);
                     const int hi = last - (s.step0 + j) * N, lo = lowest - (s.step0 + j) * N;
                     if (__any_sync(0xffffffffu, hi < N - 1 || lo >= 0) || blocks != (1u << T::kBlocks) - 1) {
                         // one bit per key: up to hi, above lo, of blocks with a page
