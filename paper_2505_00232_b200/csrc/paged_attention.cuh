@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
                 }
             }
             // m is raised when a weight would pass 2^15
-            if (__any_sync(0xffffffffu, fmaxf(x[0], x[2]) > m0 + margin || fmaxf(x[1], x[3]) > m1 + margin)) {
+            if (__any_sync(0xffffffffu, fmaxf(x[0], x[2]) - m0 > margin || fmaxf(x[1], x[3]) - m1 > margin)) {   // (differences: exact however large the scores are)
                 float n0 = fmaxf(x[0], x[2]), n1 = fmaxf(x[1], x[3]);
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) {

@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
             const int t = NT == 2 ? warp >> 2 : 0, wq = warp & 3, in_tile = 32 * wq + lane;
             const uint32_t lanes = (uint32_t)(32 * wq) << 16, to = tmem + lanes + T::kO + D * t;
             constexpr float kLog2e = 1.4426950408889634f;
-            const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * kLog2e, 1e-30f);   // (never 0: hidden scores are -infinity)
+            const float mag = fabsf(p.scale), cc = CAP ? 1.f : fmaxf(mag * kLog2e, 1e-30f), margin = kWeightRange / cc;   // weights exp2(cc (x - m)); (cc never 0: hidden scores are -infinity)
             const SoftCap cap(mag, p.softcap);
             // this warp's 32 rows of the tile, copied without waiting, D / 8 lanes' worth of a row side by side; a lane knows where its own row lies
             const auto request_q = [&](const TileSegment& s) {
@@ -294,9 +294,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                         mx[0] = fmaxf(mx[0], x[e]); mx[1] = fmaxf(mx[1], x[e + 1]);
                         mx[2] = fmaxf(mx[2], x[e + 2]); mx[3] = fmaxf(mx[3], x[e + 3]);
                     }
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * cc;
-                    if (__any_sync(0xffffffffu, top > m + kWeightRange)) {   // m is raised, and with it the scale of the sums
-                        const float mn = fmaxf(m, top - kWeightLift), f = exp2_fast(m - mn);
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    if (__any_sync(0xffffffffu, top - m > margin)) {     // m is raised, and with it the scale of the sums
+                        const float mn = fmaxf(fmaf(margin, -kWeightLift / kWeightRange, top), m), f = exp2_fast((m - mn) * cc);
                         m = mn;
                         l[0].x *= f; l[0].y *= f; l[1].x *= f; l[1].y *= f;
                         if (j > 0) {
@@ -318,7 +318,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                         uint32_t h[16];
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
-                            const float2 y = fma2(x[e + 2 * k], x[e + 2 * k + 1], cc, -m);
+                            // (the difference first: x cc - cm with one rounding is not the difference of two scores where cm, a rounded product, is off by powers of two: scores from 2^26 on; 2 % of the time)
+                            float2 y = add2(make_float2(x[e + 2 * k], x[e + 2 * k + 1]), make_float2(-m, -m));
+                            if (!CAP) y = mul2(y, make_float2(cc, cc));
                             x[e + 2 * k] = y.x;
                             x[e + 2 * k + 1] = y.y;
                         }
@@ -378,7 +380,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
 #pragma unroll
                         for (int e = 0; e < 4; ++e) store32(part + row * D + d + 8 * e, o + 8 * e);
                     }
-                    part[T::kRows * D + row] = m;
+                    part[T::kRows * D + row] = m * cc;
                     part[T::kRows * D + T::kRows + row] = sum;
                 }
                 tc_fence_before();

@@ -677,3 +677,24 @@ def test_numbers_beyond_32_bits(P, torch):
             call()
         assert e.value.status == P.QL_ERR_INVALID_ARG
     cache.attention(q, *batch.args, 2, window=2 ** 31 - 1)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("exponent", [20, 24, 26, 27, 28, 29, 32])
+def test_scores_of_millions(P, torch, new, exponent):
+    """Scores that are far apart: the heaviest token takes all, or shares with those that are the same.  Tokens 5 and 50 and, for 60, the same key; the others' scores lie 2^-6 of that score below, many powers of two."""
+    batch = Batch(torch, [61], [new], 16)
+    cache = P.PagedKV(batch.n_pages, 16, 2, 64)
+    k = torch.full((61, 2, 64), 7.0, dtype=torch.float16, device="cuda")             # (held exactly: 7 times a scale of 1)
+    k[:, :, 1] = 0
+    k[[5, 50, 60], :, 1] = 1                                             # (a power of 2^exponent / 63 more for each of these)
+    v = torch.from_numpy(f16(np.random.default_rng(2), 61, 2, 64)).cuda()
+    cache.append(k, v, *batch.whole)
+    q = torch.ones((new, 4, 64), dtype=torch.float16, device="cuda")
+    scale = 2.0 ** exponent / (63 * 7) * np.log(2)
+    out = cache.attention(q, *batch.args, new, scale=scale).double().cpu().numpy()
+    values = held(v.cpu().numpy())
+    for i in range(new):
+        see = [t for t in (5, 50, 60) if t <= 61 - new + i]
+        want = values[see].mean(0).repeat(2, 0)
+        assert (np.abs(out[i] - want) <= 2 * 2.0 ** -11 * np.abs(values[see]).mean(0).repeat(2, 0) + 2.0 ** -11 * np.abs(want) + 2.0 ** -25).all()
