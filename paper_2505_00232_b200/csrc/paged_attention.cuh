@@ -32,6 +32,7 @@
 namespace ql {
 
 constexpr float kWeightLift = 7.f, kWeightRange = 15.f;                  // the largest weight is 2^7 when m is set, m is raised before one passes 2^15
+constexpr float kMostScale = 1e15f;                                      // scores stay far above -1e30, what a row's m is before its first token (products of fp16 vectors are below 2e12)
 constexpr int kAttnWarps = 8;
 constexpr int kAttnCols = 8;
 // The query rows per KV head that this kernel takes, 8 at a time; more go to paged_tiles.cuh, whose time does not depend on them (us, here and there, 16 sequences of 4096: 16 KV heads

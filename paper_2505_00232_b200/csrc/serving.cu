@@ -271,7 +271,7 @@ extern "C" ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q, i
     PagedAttnParams p{};
     AttnPlan a;
     if (!batch_of(h, table, table_ld, table_width, kv_len, q_start, B, T, &p.batch) || !attn_plan(h, h_q, B, max_q, &a)) return QL_ERR_INVALID_ARG;
-    if (!std::isfinite(scale) || !(softcap >= 0.f) || !std::isfinite(softcap) || window < 0) return QL_ERR_INVALID_ARG;
+    if (!(std::fabs(scale) <= kMostScale) || !(softcap >= 0.f) || !std::isfinite(softcap) || window < 0) return QL_ERR_INVALID_ARG;
     if (B == 0 || T == 0 || max_q == 0) return QL_OK;
     {   // the kernels number the steps of a KV head's segments in 32 bits
         const int64_t held = std::min((int64_t)table_width * h->d.page_size, (int64_t)INT32_MAX);

@@ -680,6 +680,24 @@ def test_numbers_beyond_32_bits(P, torch):
 
 
 @pytest.mark.parametrize("new", [1, 40])
+def test_the_largest_scale(P, torch, new):
+    """Scores of -2e29 are scores (all the same here, so the result is the values' mean, half a step of fp16 each for a value, the weights and the result); scales that would let them pass -1e30 are refused."""
+    batch = Batch(torch, [60], [new], 16)
+    cache = P.PagedKV(batch.n_pages, 16, 2, 256)
+    x = torch.full((60, 2, 256), 1000.0, dtype=torch.float16, device="cuda")
+    cache.append(x, x, *batch.whole)
+    q = torch.full((new, 4, 256), -1000.0, dtype=torch.float16, device="cuda")
+    for scale in (1e15, 1e12):
+        out = cache.attention(q, *batch.args, new, scale=scale).double()
+        want = held(x[:1, :1].cpu().numpy()).flat[0]
+        assert ((out - want).abs() <= 3 * 2.0 ** -11 * want).all()
+    for scale in (1.1e15, -1e16, 1e30, -3e38, float("inf"), float("nan")):
+        with pytest.raises(P.QLinearError) as e:
+            cache.attention(q, *batch.args, new, scale=scale)
+        assert e.value.status == P.QL_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("new", [1, 40])
 @pytest.mark.parametrize("exponent", [20, 24, 26, 27, 28, 29, 32])
 def test_scores_of_millions(P, torch, new, exponent):
     """Scores that are far apart: the heaviest token takes all, or shares with those that are the same.  Tokens 5 and 50 and, for 60, the same key; the others' scores lie 2^-6 of that score below, many powers of two."""
