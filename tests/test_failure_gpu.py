@@ -62,3 +62,28 @@ def test_handles_own_no_device_memory(_built_library):
     assert len(lins) == 28
     assert free0 - free1 < (4 << 20), f"28 handles took {(free0 - free1) / 2**20:.1f} MiB of device memory"
     del lins, first
+
+
+def test_paged_calls_see_an_expired_wait(_built_library):
+    """The calls of the paged cache refuse a device whose wait ran out, launch nothing, and report and clear it as the layers' handles do."""
+    import torch
+    import paper_2505_00232_b200 as P
+    lin = P.QLinear.from_weights(*C.layer_weights(1, C.LayerSpec("t", 128, 256, 8, 0, -128, 127)), 8, 0, device="cuda:0")
+    cache = P.PagedKV(4, 16, 2, 64)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    batch = i32(0, 1, 2, 3)[None], i32(40), i32(0, 40)
+    k, q = torch.randn((40, 2, 64), device="cuda").half(), torch.randn((40, 4, 64), device="cuda").half()
+    cache.append(k, k, *batch)
+    before, pool = cache.attention(q, *batch, 40), cache.pool.clone()
+    assert cache.device_status() == (0, 0)
+    lin.debug_expire_wait()
+    torch.cuda.synchronize()
+    out = torch.full_like(q, 7.0)
+    for call in (lambda: cache.append(k + 1, k, *batch, q=q, q_out=out), lambda: cache.read(*batch, 40), lambda: cache.attention(q, *batch, 40, out=out), lambda: cache.attention(q[-1:], *batch[:2], i32(0, 1), 1, out=out[-1:])):
+        with pytest.raises(P.QLinearError) as e:
+            call()
+        assert e.value.status == P.QL_ERR_DEVICE_TIMEOUT
+    torch.cuda.synchronize()
+    assert (out == 7).all() and torch.equal(cache.pool, pool)
+    assert cache.device_status() == (P.QL_ERR_DEVICE_TIMEOUT, 0x9A0) and cache.device_status() == (0, 0) == lin.device_status()
+    assert torch.equal(cache.attention(q, *batch, 40), before)

@@ -206,3 +206,22 @@ def test_the_largest_vocabulary(P):
     y = P.qlinear_adjust_logits(x, **history, **biases, mask=mask, out=y)
     assert y[0, at].tolist() == [-float("inf"), 4, 7, 0, 6, -float("inf")] and int(y.isinf().sum()) == 2
     assert P.qlinear_adjust_logits(x, mask=mask, out=x) is x and x[0, at].tolist() == [-float("inf"), 0, 0, 0, 0, -float("inf")]
+
+
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+@pytest.mark.parametrize("R,V,n", [(16, 256000, 3000), (12, 131072 + 5, 700), (12, 131072, 700)])
+def test_vocabularies_of_more_than_one_piece(P, dtype, R, V, n):
+    """Many rows, whose seen tokens are adjusted by a CTA per 131072 tokens: history, biases and mask in every piece, and at its ends."""
+    import torch
+    a = list(inputs(np.random.default_rng(V), R, V, n, dtype))
+    ends = np.array([0, 131071, min(131072, V - 1), V - 1], np.int32)
+    for r in range(R):
+        if a[2][r + 1] - a[2][r] >= 8:
+            a[1][a[2][r]:a[2][r] + 4] = a[1][a[2][r + 1] - 4:a[2][r + 1]] = ends
+        if a[9][r + 1] - a[9][r] >= 4:
+            a[7][a[9][r]:a[9][r] + 4] = ends
+    dev = [torch.from_numpy(t.view(np.int32) if t.dtype == np.uint32 else t).cuda() for t in a]
+    for masked in (True, False):
+        want, tol = adjusted(*a[:10], a[10] if masked else None)
+        got = P.qlinear_adjust_logits(*dev[:10], mask=dev[10] if masked else None)
+        check(got.cpu().numpy(), want, tol, dtype)

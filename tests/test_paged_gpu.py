@@ -716,3 +716,67 @@ def test_scores_of_millions(P, torch, new, exponent):
         see = [t for t in (5, 50, 60) if t <= 61 - new + i]
         want = values[see].mean(0).repeat(2, 0)
         assert (np.abs(out[i] - want) <= 2 * 2.0 ** -11 * np.abs(values[see]).mean(0).repeat(2, 0) + 2.0 ** -11 * np.abs(want) + 2.0 ** -25).all()
+
+
+@pytest.mark.parametrize("h_q,h_kv,d,new", [(32, 8, 64, 13), (32, 8, 128, 9), (16, 8, 256, 13)])
+def test_more_segments_than_a_round_takes(P, torch, h_q, h_kv, d, new):
+    """The most sequences a call takes, short, with rows enough for the kernel of many rows: about 110 segments a CTA, which lists 64 at a time.  The same bits from every run, sampled rows against 64 bits."""
+    rng = np.random.default_rng(d)
+    lens = [int(x) for x in rng.integers(0, 90, 2048)]
+    batch = Batch(torch, lens, [new] * 2048, 16, behind=1)
+    assert sum(n > 0 for n in lens) * h_kv > 2 * 64 * torch.cuda.get_device_properties(0).multi_processor_count * 0.8
+    cache, kv = filled(P, torch, batch, h_kv, d)
+    q = f16(rng, batch.T, h_q, d)
+    dev = torch.from_numpy(q).cuda()
+    outs = [cache.attention(dev, *batch.args, new, out=torch.full_like(dev, 9)) for _ in range(4)]
+    assert all(torch.equal(outs[0], o) for o in outs) and (outs[0][-1] == 9).all()
+    rows = batch.rows()
+    rows = [rows[i] for i in rng.permutation(len(rows))[:200]]
+    want, tol = attention64(q, kv, batch, d ** -0.5, rows=rows)
+    check(outs[0].cpu().numpy(), want, tol, rows)
+
+
+@pytest.mark.parametrize("h_q,h_kv,d", [(32, 8, 128), (8, 4, 256), (14, 2, 64)])
+@pytest.mark.parametrize("new", [[1, 400, 3, 1, 0, 2], [1, 4, 2, 6, 1, 3]])
+@pytest.mark.parametrize("window", [0, 1000])
+def test_rows_of_every_kind_in_one_call(P, torch, h_q, h_kv, d, new, window):
+    """A prompt's chunk beside generated tokens over thousands of cached ones, and a few tokens of each sequence, by the kernel that the largest number of rows asks for."""
+    lens = [3000, 4100, 2500, 5, 40, 1999]
+    batch = Batch(torch, lens, new, 32, seed=3, before=1, behind=2)
+    cache, kv = filled(P, torch, batch, h_kv, d)
+    q = f16(np.random.default_rng(8), batch.T, h_q, d)
+    out = torch.full((batch.T, h_q, d), 9.0, dtype=torch.float16, device="cuda")
+    got = cache.attention(torch.from_numpy(q).cuda(), *batch.args, batch.max_q, window=window, out=out).cpu().numpy()
+    rows = [r for r in batch.rows() if batch.new[r[1]] < 10 or r[0] % 23 == 0]
+    want, tol = attention64(q, kv, batch, d ** -0.5, 0.0, window, rows=rows)
+    check(got, want, tol, rows)
+    assert (got[0] == 9).all() and (got[-2:] == 9).all()
+
+
+@pytest.mark.parametrize("h_kv,d", [(2, 64), (2, 128), (2, 256)])
+def test_the_most_sequences(P, torch, h_kv, d):
+    """2048 sequences of a token each: the plan of the batch at its largest, in the kernel of few rows."""
+    rng = np.random.default_rng(d)
+    lens = [int(x) for x in rng.integers(0, 200, 2048)]
+    batch = Batch(torch, lens, [1] * 2048, 16)
+    cache, kv = filled(P, torch, batch, h_kv, d)
+    q = f16(rng, batch.T, 4, d)
+    got = cache.attention(torch.from_numpy(q).cuda(), *batch.args, 1).cpu().numpy()
+    rows = [r for r in batch.rows() if r[1] % 7 == 0]
+    want, tol = attention64(q, kv, batch, d ** -0.5, rows=rows)
+    check(got, want, tol, rows)
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_a_table_cut_from_a_wider_one(P, torch, new):
+    batch = Batch(torch, [300, 170, 44], [new] * 3, 16)
+    k, v = (torch.from_numpy(f16(np.random.default_rng(s), batch.T, 2, 128)).cuda() for s in (1, 2))
+    q = torch.from_numpy(f16(np.random.default_rng(3), batch.T, 8, 128)).cuda()
+    wide = torch.full((3, batch.table.shape[1] + 9), 2 ** 30, dtype=torch.int32, device="cuda")
+    wide[:, 4:-5] = batch.args[0]
+    results = []
+    for table in (batch.args[0], wide[:, 4:-5]):
+        cache, _ = filled(P, torch, batch, 2, 128)
+        cache.append(k, v, table, *batch.args[1:])
+        results.append([cache.pool, *cache.read(table, *batch.args[1:], batch.T), cache.attention(q, table, *batch.args[1:], new)])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
