@@ -26,7 +26,7 @@ EXPORTS = (
     "qlinear_path_for", "qlinear_debug_unpack_device", "qlinear_debug_expire_wait", "qlinear_debug_null_launch", "qlinear_device_status", "qlinear_decode_static", "qlinear_destroy",
     "qlinear_status_string", "qlinear_version", "qlinear_debug_plan", "qlinear_debug_plan_kv_output", "qlinear_debug_takes_batch_kernel", "qlinear_debug_kv_hold", "qlinear_debug_route", "qlinear_debug_plan_a8", "qlinear_debug_config_reads",
     "qlinear_rope_tables", "qlinear_paged_page_bytes", "qlinear_paged_create", "qlinear_paged_destroy", "qlinear_paged_device_status", "qlinear_paged_append", "qlinear_paged_read",
-    "qlinear_paged_attention_workspace", "qlinear_paged_attention", "qlinear_adjust_logits",
+    "qlinear_paged_attention_workspace", "qlinear_paged_attention", "qlinear_adjust_logits", "qlinear_debug_paged_ctas",
 )
 
 
@@ -140,6 +140,8 @@ def _load() -> ctypes.CDLL:
     lib.qlinear_paged_attention_workspace.argtypes = [vp, i32, i32, i32]
     lib.qlinear_paged_attention_workspace.restype = size
     lib.qlinear_paged_attention.argtypes = [vp, vp, i64, vp, i64, i32, *batch, i32, f32, f32, i32, vp, size, vp]
+    lib.qlinear_debug_paged_ctas.argtypes = [vp, i32, ctypes.POINTER(i32)]
+    lib.qlinear_debug_paged_ctas.restype = i32
     lib.qlinear_adjust_logits.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, i32, vp]
     for f in ("qlinear_rope_tables", "qlinear_paged_create", "qlinear_paged_destroy", "qlinear_paged_device_status", "qlinear_paged_append", "qlinear_paged_read", "qlinear_paged_attention", "qlinear_adjust_logits"):
         getattr(lib, f).restype = ctypes.c_int

@@ -10,7 +10,9 @@
 // Work: the segments (sequence, KV head, 8 query rows) of the batch, numbered through, each as long as its blocks and kAttnOverhead more
 // (what a segment costs besides its blocks: an empty pipeline, the warps' meeting), are cut into one span of equal length per CTA, whatever the
 // lengths: a ragged batch and a single long sequence load the SMs alike (64 sequences of 128 .. 8192 tokens, 194618 in all, 8 KV heads of 128:
-// 81.7 us with spans of blocks alone, 72.3, 68.1, 64.1, 66.0 with 8, 16, 32, 48 more; of equal lengths 63).  The plan is made by every CTA
+// 81.7 us with spans of blocks alone, 72.3, 68.1, 64.1, 66.0 with 8, 16, 32, 48 more; of equal lengths 63).  The grid is the CTAs that
+// run at once: two an SM, but one at d_h 256, where rings, queries and plan take more than half of an SM's shared memory (24 sequences of up to 7001, window 4096: 38.6 us with a grid for two,
+// 31.9 for one, 29.5 with the registers of one), and at d_h 128 beyond about 1650 sequences.  The plan is made by every CTA
 // from the lengths on the device (a scan), so a captured launch follows them.  A CTA's 8 warps take the blocks of a segment in turn, each
 // through a ring of its own in shared memory that goes on from segment to segment (bulk copies, requested by the lane that looked up the page), and
 // meet at the segment's end, when the first blocks of the next one are on their way.  A segment cut by a span's end leaves (m, l, o) in the
@@ -36,8 +38,8 @@ constexpr float kMostScale = 1e15f;                                      // scor
 constexpr int kAttnWarps = 8;
 constexpr int kAttnCols = 8;
 // The query rows per KV head that this kernel takes, 8 at a time; more go to paged_tiles.cuh, whose time does not depend on them (us, here and there, 16 sequences of 4096: 16 KV heads
-// of 64, 40 rows 119 and 140, 64 rows 184 and 140; 8 of 128, 32 rows 78 and 86, 40 rows 94 and 86; 4 of 256, 16 rows 55 and 67, 24 rows 75 and 66, 32 rows 94 and 67; one of 16384: 40 rows 35
-// and 47; 30 and 40; 38 and 48, and 24 rows of 256 31 and 47).
+// of 64, 40 rows 118 and 134, 48 rows 140 and 134, 64 rows 183 and 134; 8 of 128, 32 rows 78 and 87, 40 rows 94 and 88; 4 of 256, 16 rows 44 and 67, 24 rows 60 and 67, 32 rows 77 and 67).  The
+// rule goes by the rows alone, for batches: of ONE long sequence this kernel would still take 40 to 64 rows faster (16384: 40 rows 35 and 47, 31 and 41, 30 and 48).
 __host__ __device__ constexpr int attn_max_rows(int d) { return d == 64 ? 48 : d == 128 ? 32 : 24; }
 constexpr int kAttnOverhead = 32;                                        // a segment without blocks, in blocks
 constexpr int kAttnSpan = 16;                                            // the least span: two blocks per warp (4096 tokens, 8 KV heads: 11.1, 11.4, 10.6 us with 8, 16, 24; 512 tokens: 8.6, 9.2, 9.8; four of 1280: 11.2, 11.3, 12.0)
@@ -186,7 +188,7 @@ struct AttnSegment {
 };
 
 template <int D, AttnCap CAP>
-__global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(const PagedAttnParams p)
+__global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_attention_kernel(const PagedAttnParams p)
 {
     constexpr int NB = D / 64, kBlock = AttnRing<D>::kBlock, S = AttnRing<D>::kStages, kStride = AttnRing<D>::kMergeStride;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -194,7 +196,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) paged_attention_kernel(con
     __shared__ __align__(8) uint64_t bars[kAttnWarps * S];
     __shared__ AttnSegment segs[4];                                      // in turn: the last one (slow warps still look at it), this, the next, the one after it
     __shared__ volatile uint32_t abort_flag[4];
-    // (at d_h 256 the queries lie in shared memory, read for every block: with 128 registers they would be spilled)
+    // (at d_h 256 the queries lie in shared memory, read for every block)
     constexpr bool kQueriesApart = D == 256;
     __shared__ __align__(16) uint4 queries[kQueriesApart ? 2 * NB * 32 : 1];
     int* pre = reinterpret_cast<int*>(smem + AttnRing<D>::kBytes);       // [B + 1]

@@ -30,6 +30,7 @@ struct qlinear_paged_s {
     qlinear_paged_desc d;
     uint8_t* pool;
     int device, log2_blocks;
+    int32_t two_ctas_upto;                                               // sequences of an attention call with few rows up to which two CTAs fit on an SM
     SharedState shared;
     bool pdl;
 };
@@ -69,6 +70,24 @@ ql_status launched(cudaError_t e)
 {
     if (e != cudaSuccess) cudaGetLastError();
     return e == cudaSuccess ? QL_OK : QL_ERR_CUDA;
+}
+
+// The dynamic shared memory of the kernel of few rows (its plan holds a number per sequence), and up to how many sequences two of its CTAs fit on an SM: at d_h 64 any number, at 128
+// about 1660, at 256 none, since its queries lie in shared memory.
+template <int D> constexpr int attn_smem(int32_t B) { return AttnRing<D>::kBytes + (B + 1) * 4; }
+template <int D>
+cudaError_t two_ctas_upto(int device, int32_t* sequences)
+{
+    int all = 0, reserved = 0, fixed = 0;
+    cudaError_t e = cudaDeviceGetAttribute(&all, cudaDevAttrMaxSharedMemoryPerMultiprocessor, device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&reserved, cudaDevAttrReservedSharedMemoryPerBlock, device);
+    for (const auto kernel : {paged_attention_kernel<D, kCapNone>, paged_attention_kernel<D, kCapPlain>, paged_attention_kernel<D, kCapHigh>}) {
+        cudaFuncAttributes at;
+        if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, kernel);
+        if (e == cudaSuccess) fixed = std::max(fixed, (int)at.sharedSizeBytes);
+    }
+    *sequences = (all / 2 / 128 * 128 - reserved - fixed - attn_smem<D>(0)) / 4;   // (shared memory is given out 128 bytes at a time)
+    return e;
 }
 
 }  // namespace
@@ -141,11 +160,17 @@ extern "C" ql_status qlinear_paged_create(const qlinear_paged_desc* d, void* poo
             linked[device].store(true, std::memory_order_release);
         }
     }
+    int32_t upto = 0;
+    {
+        DeviceGuard guard(device);
+        if (!guard.ok || (d->d_h == 64 ? two_ctas_upto<64> : d->d_h == 128 ? two_ctas_upto<128> : two_ctas_upto<256>)(device, &upto) != cudaSuccess) { cudaGetLastError(); return QL_ERR_CUDA; }
+    }
     qlinear_paged_s* h = new (std::nothrow) qlinear_paged_s();
     if (!h) return QL_ERR_ALLOC;
     h->d = *d;
     h->pool = static_cast<uint8_t*>(pool_dev);
     h->device = device;
+    h->two_ctas_upto = upto;
     for (h->log2_blocks = 0; (kPagedBlock << h->log2_blocks) < d->page_size; ++h->log2_blocks) {}
     h->shared = shared;
     h->pdl = pdl_enabled();
@@ -221,7 +246,7 @@ bool attn_plan(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t max_q, AttnPla
     a->tiles = rows > attn_max_rows(h->d.d_h);
     a->rows = a->tiles ? (h->d.d_h == 256 ? TileShape<256>::kRows : TileShape<128>::kRows) : kAttnCols;
     a->row_blocks = (int32_t)((rows + a->rows - 1) / a->rows);
-    a->grid = (a->tiles ? 1 : 2) * h->shared.sms;
+    a->grid = (a->tiles || B > h->two_ctas_upto ? 1 : 2) * h->shared.sms;   // (every CTA at once: spans of equal length in two rounds take a round's start and end more)
     a->split_at = (size_t)2 * a->grid * a->rows * (h->d.d_h + 2) * sizeof(float);
     a->bytes = a->split_at + (size_t)a->grid * sizeof(int4);
     return true;
@@ -232,7 +257,7 @@ cudaError_t launch_attention_as(const PagedAttnParams& p, bool tiles, int device
 {
     using T = TileShape<D>;
     static std::atomic<bool> flags[64];
-    constexpr int kMost = AttnRing<D>::kBytes + (QL_PAGED_MAX_SEQUENCES + 1) * 4, kMostTiles = 1024 + T::kOffPre + (QL_PAGED_MAX_SEQUENCES + 1) * 4;
+    constexpr int kMost = attn_smem<D>(QL_PAGED_MAX_SEQUENCES), kMostTiles = 1024 + T::kOffPre + (QL_PAGED_MAX_SEQUENCES + 1) * 4;
     if (!flags[device].load(std::memory_order_acquire)) {
         cudaError_t e = cudaFuncSetAttribute(paged_attention_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_tiles_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostTiles);
@@ -243,7 +268,7 @@ cudaError_t launch_attention_as(const PagedAttnParams& p, bool tiles, int device
         flags[device].store(true, std::memory_order_release);
     }
     cudaError_t e = tiles ? launch(paged_tiles_kernel<D, CAP>, p, dim3(p.grid), dim3(kTileThreads), 1024 + T::kOffPre + (p.batch.B + 1) * 4, st, 1, pdl)
-                          : launch(paged_attention_kernel<D, CAP>, p, dim3(p.grid), dim3(kAttnWarps * 32), AttnRing<D>::kBytes + (p.batch.B + 1) * 4, st, 1, pdl);
+                          : launch(paged_attention_kernel<D, CAP>, p, dim3(p.grid), dim3(kAttnWarps * 32), attn_smem<D>(p.batch.B), st, 1, pdl);
     if (e != cudaSuccess) return e;
     return tiles ? launch(paged_combine_kernel<D, T::kRows, 4, 1>, p, dim3(p.grid, T::kRows / 32), dim3(256), 0, st, 1, pdl)
                  : launch(paged_combine_kernel<D, kAttnCols, 1, 4>, p, dim3(p.grid, (std::min(kAttnCols, p.max_q * p.group) + 1) / 2), dim3(256), 0, st, 1, pdl);
@@ -262,6 +287,29 @@ extern "C" size_t qlinear_paged_attention_workspace(qlinear_paged_t h, int32_t h
 {
     AttnPlan a;
     return attn_plan(h, h_q, B, max_q, &a) ? a.bytes : 0;
+}
+
+namespace {
+template <int D> int ctas_that_fit(int32_t B)
+{
+    int least = INT_MAX;
+    for (const auto kernel : {paged_attention_kernel<D, kCapNone>, paged_attention_kernel<D, kCapPlain>, paged_attention_kernel<D, kCapHigh>}) {
+        int fit = -1;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem<D>(QL_PAGED_MAX_SEQUENCES)) != cudaSuccess ||
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, kernel, kAttnWarps * 32, attn_smem<D>(B)) != cudaSuccess) { cudaGetLastError(); return -1; }
+        least = std::min(least, fit);
+    }
+    return least;
+}
+}  // namespace
+
+extern "C" int32_t qlinear_debug_paged_ctas(qlinear_paged_t h, int32_t B, int32_t* fit)
+{
+    AttnPlan a;
+    if (!h || !fit || !attn_plan(h, h->d.h_kv, B, 1, &a)) return 0;
+    DeviceGuard guard(h->device);
+    *fit = !guard.ok ? -1 : h->d.d_h == 64 ? ctas_that_fit<64>(B) : h->d.d_h == 128 ? ctas_that_fit<128>(B) : ctas_that_fit<256>(B);
+    return a.grid / h->shared.sms;
 }
 
 extern "C" ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q, int64_t q_ld, void* out, int64_t out_ld, int32_t h_q, const int32_t* table, int64_t table_ld, int32_t table_width,

@@ -780,3 +780,16 @@ def test_a_table_cut_from_a_wider_one(P, torch, new):
         cache.append(k, v, table, *batch.args[1:])
         results.append([cache.pool, *cache.read(table, *batch.args[1:], batch.T), cache.attention(q, table, *batch.args[1:], new)])
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_the_ctas_of_a_call_run_at_once(P, torch, d):
+    """The kernel of few rows cuts its work into spans of equal length for CTAs that run side by side: as many as fit, by the runtime's own count, up to two an SM, whatever the number of sequences."""
+    import ctypes
+    cache, fit = P.PagedKV(1, 16, 1, d), ctypes.c_int32()
+    launched = []
+    for B in (1, 24, 700, 1500, *range(1600, 1720, 4), 2048):
+        launched.append(P.lib.qlinear_debug_paged_ctas(cache._h, B, ctypes.byref(fit)))
+        assert launched[-1] == min(fit.value, 2) > 0, (B, launched[-1], fit.value)
+    assert set(launched) == {64: {2}, 128: {1, 2}, 256: {1}}[d]
+    assert P.lib.qlinear_debug_paged_ctas(None, 1, ctypes.byref(fit)) == 0 == P.lib.qlinear_debug_paged_ctas(cache._h, 2049, ctypes.byref(fit))
