@@ -247,8 +247,9 @@ bool attn_plan(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t max_q, AttnPla
     a->rows = a->tiles ? (h->d.d_h == 256 ? TileShape<256>::kRows : TileShape<128>::kRows) : kAttnCols;
     a->row_blocks = (int32_t)((rows + a->rows - 1) / a->rows);
     a->grid = (a->tiles || B > h->two_ctas_upto ? 1 : 2) * h->shared.sms;   // (every CTA at once: spans of equal length in two rounds take a round's start and end more)
-    a->split_at = (size_t)2 * a->grid * a->rows * (h->d.d_h + 2) * sizeof(float);
-    a->bytes = a->split_at + (size_t)a->grid * sizeof(int4);
+    const size_t most = (size_t)(a->tiles ? 1 : 2) * h->shared.sms;      // (whatever B: a workspace for many sequences serves fewer)
+    a->split_at = 2 * most * a->rows * (h->d.d_h + 2) * sizeof(float);
+    a->bytes = a->split_at + most * sizeof(int4);
     return true;
 }
 

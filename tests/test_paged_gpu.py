@@ -793,3 +793,15 @@ def test_the_ctas_of_a_call_run_at_once(P, torch, d):
         assert launched[-1] == min(fit.value, 2) > 0, (B, launched[-1], fit.value)
     assert set(launched) == {64: {2}, 128: {1, 2}, 256: {1}}[d]
     assert P.lib.qlinear_debug_paged_ctas(None, 1, ctypes.byref(fit)) == 0 == P.lib.qlinear_debug_paged_ctas(cache._h, 2049, ctypes.byref(fit))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_a_workspace_for_the_most_sequences_serves_fewer(P, torch, d):
+    batch = Batch(torch, [100, 7], [1, 1], 16)
+    cache, _ = filled(P, torch, batch, 2, d)
+    q = torch.from_numpy(f16(np.random.default_rng(4), 2, 4, d)).cuda()
+    work = torch.empty(P.lib.qlinear_paged_attention_workspace(cache._h, 4, 2048, 1), dtype=torch.uint8, device="cuda")
+    out, table = torch.zeros_like(q), batch.args[0]
+    assert P.lib.qlinear_paged_attention(cache._h, q.data_ptr(), 4 * d, out.data_ptr(), 4 * d, 4, table.data_ptr(), table.stride(0), table.shape[1], batch.args[1].data_ptr(), batch.args[2].data_ptr(), 2, 2, 1,
+                                         d ** -0.5, 0.0, 0, work.data_ptr(), work.numel(), torch.cuda.current_stream().cuda_stream) == P.binding.QL_OK
+    assert torch.equal(out, cache.attention(q, *batch.args, 1)) and out.any()
