@@ -75,7 +75,7 @@ __device__ __forceinline__ void paged_locate(const PagedBatch& p, int t0, int n,
         const int rows = paged_rows(p, b, &first);
         for (int t = max(first, t0); t < min(first + rows, t0 + n); ++t) {
             seq[t - t0] = b;
-            position[t - t0] = p.kv_len[b] - rows + (t - first);
+            position[t - t0] = (int)max((int64_t)p.kv_len[b] - rows + (t - first), (int64_t)-1);   // (negative: before the first token)
         }
     }
     __syncthreads();

@@ -142,7 +142,7 @@ __device__ __forceinline__ int attn_blocks(const PagedAttnParams& p, int b, int*
     const int rows = paged_rows(p.batch, b, &t0);
     const int len = p.batch.kv_len[b];
     const int64_t held = (int64_t)p.batch.table_width << (p.batch.log2_blocks + 4);
-    const int end = (int)min((int64_t)len - rows + min(rows, p.max_q), held);   // (up to the last served row's token)
+    const int end = (int)max(min((int64_t)len - rows + min(rows, p.max_q), held), (int64_t)0);   // (up to the last served row's token)
     *first = 0;
     if (min(rows, p.max_q) <= 0 || end <= 0) return 0;
     if (p.window > 0) *first = (int)max((int64_t)len - rows + 1 - p.window, (int64_t)0) >> 4;   // the first token that the first row sees

@@ -805,3 +805,21 @@ def test_a_workspace_for_the_most_sequences_serves_fewer(P, torch, d):
     assert P.lib.qlinear_paged_attention(cache._h, q.data_ptr(), 4 * d, out.data_ptr(), 4 * d, 4, table.data_ptr(), table.stride(0), table.shape[1], batch.args[1].data_ptr(), batch.args[2].data_ptr(), 2, 2, 1,
                                          d ** -0.5, 0.0, 0, work.data_ptr(), work.numel(), torch.cuda.current_stream().cuda_stream) == P.binding.QL_OK
     assert torch.equal(out, cache.attention(q, *batch.args, 1)) and out.any()
+
+
+@pytest.mark.parametrize("n", [0, -1, -7, -2 ** 31, -2 ** 31 + 3])
+def test_lengths_below_the_rows(P, torch, n):
+    """Rows of a sequence said to be shorter than they are many lie before its first token: left by append, zeros from attention (the rows served), whatever the length."""
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    batch = i32(0, 1)[None], i32(n), i32(0, 8)
+    cache = P.PagedKV(2, 16, 2, 64)
+    k, q = (torch.ones((8, h, 64), dtype=torch.float16, device="cuda") for h in (2, 4))
+    cos, sin = P.qlinear_rope_tables(32, 64)
+    mark = torch.full_like(q, 7)
+    cache.append(k, k, *batch, q=q, cos=cos, sin=sin, q_out=mark)
+    assert (mark == 7).all() and not cache.pool.any()
+    for most in (8, 3):
+        out = cache.attention(q, *batch, most, out=torch.full_like(q, 7))
+        assert not out[:most].any() and (out[most:] == 7).all()
+    many = torch.ones((60, 4, 64), dtype=torch.float16, device="cuda")
+    assert not cache.attention(many, *batch[:2], i32(0, 60), 60).any()
