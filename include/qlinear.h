@@ -348,7 +348,7 @@ ql_status qlinear_rope_tables(float* cos_dev, float* sin_dev, int32_t first, int
  * qlinear_paged_read: fp16(q s) of the rows' tokens, k_out_dev and v_out_dev fp16 [T, h_kv, d_h] (rows = kv_len for a whole sequence).
  * qlinear_paged_attention: out[t, h] = sum_j softmax_j(x_j) v_j with x_j = scale q.k_j, or softcap * tanh(scale q.k_j / softcap) where softcap > 0, over the visible tokens of the
  *   row's sequence: j <= p, j < kv_len, and p - j < window where window > 0.  |scale| <= 1e15.  Query head h reads KV head h / (h_q / h_kv).  A row that sees nothing gives zeros.  max_q: no sequence has
- *   more rows (rows beyond it are left as they are); scores, softmax and sums in fp32, weights and values fp16.  out_dev must not overlap q_dev.
+ *   more rows (rows beyond it are left as they are); scores, softmax and sums in fp32, weights and values fp16, with many rows (below) the keys as well.  out_dev must not overlap q_dev.
  *   With C = table_width * page_size tokens (2^31 - 1 at most), B * C must be below 2^34, and for more query rows a KV head (max_q * h_q / h_kv) than 48, 32, 24 (d_h 64, 128, 256)
  *   (T * h_q / h_kv / 128 + B) * C below 2^36: larger calls may be refused.
  *   workspace_dev: qlinear_paged_attention_workspace bytes of the caller's, 32-byte aligned, overwritten; calls that may overlap need one each.

@@ -523,7 +523,8 @@ class PagedKV:
     """A paged KV cache held in 4 bits (qlinear_paged_* in include/qlinear.h): the pool of pages, and the calls on a batch of sequences.
 
     A batch is (page_table int32 [B, pages], kv_len int32 [B], q_start int32 [B + 1]) on the cache's device: the rows q_start[b] .. q_start[b + 1] - 1 of a
-    call are the last tokens of sequence b, which has kv_len[b] with them.  Which pages a sequence gets is the caller's business."""
+    call are the last tokens of sequence b, which has kv_len[b] with them.  Which pages a sequence gets is the caller's business.  Rows of no sequence are left as they
+    are in a caller's output, and hold nothing in a new one."""
 
     def __init__(self, n_pages: int, page_size: int, h_kv: int, d_h: int, device=None):
         import torch

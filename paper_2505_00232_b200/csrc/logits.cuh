@@ -14,7 +14,7 @@
 //
 // Many rows: every tile of a row going through its whole history costs more than the logits (256 rows of 128256, histories of 512 to 4096: 65 us with tiles of 8192).  So mask_logits_kernel copies the logits
 // under the mask, nothing else (and is left out where there is no mask and nothing to copy), and adjust_seen_kernel, a CTA per row, goes through the history twice: once for a bitmap of what it
-// holds, whose bits, counted up to each word, number the distinct tokens; once to count into a table of that many entries; and then adjusts those logits only (the same: 31 us, of 21 for the bytes).
+// holds, whose bits, counted up to each word, number the distinct tokens; once to count into a table of that many entries; and then adjusts those logits only (the same: 38 us, of 21 for the bytes).
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

@@ -516,8 +516,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
 
 // Joins the parts of the segment that begins in a CTA's span and ends in another's, in a fixed order: CTA blockIdx.x's, 8 / W x R of its rows
 // per CTA.  W warps share a row's parts, 8 of them in flight each: one long sequence is many parts of few segments, and reading them one after
-// the other took as long as a fifth of the pass (131071 tokens, 8 KV heads of 128, 37 parts each: 52.8 -> 42.8 us for the call; 4 KV heads of
-// 256, 74 parts: 79.7 -> 55.8).
+// the other took as long as a fifth of the pass (131071 tokens, 8 KV heads of 128, 37 parts each: 52.8 -> 42.8 us for the call).
 template <int D, int ROWS, int R, int W>
 __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnParams p)
 {

@@ -14,7 +14,7 @@
 // Warps 0-3, 4-7: softmax of the two tiles (at d_h 256 there is one); warps 8-15: unpack; warps 16 and 17 issue the two products; warp 18 looks up the pages and
 // requests the blocks of 16 tokens (bulk copies to a ring of raw steps in shared memory), so that nothing else waits for global memory between two
 // segments but the softmax warps for the next queries, which they have copied (without passing through registers) while the last product runs.
-// Bound: the softmax (64 exponentials, conversions and a maximum per row and step) and the shared memory's ports; a chunk of 4096 at 16384 runs at 1120 TFLOP/s.
+// Bound: the softmax (64 exponentials, conversions and a maximum per row and step) and the shared memory's ports; a chunk of 4096 at 16384 runs at 1090 TFLOP/s.
 //
 // Work: the segments of the whole batch, numbered through, each as long as its steps and kTileOverhead more (queries in, rows out, an empty pipeline), in one span of
 // equal length per CTA, as in paged_attention.cuh; a segment cut by a span's end leaves its rows' (m, l, O) in the workspace for paged_combine_kernel.
