@@ -345,7 +345,7 @@ ql_status qlinear_rope_tables(float* cos_dev, float* sin_dev, int32_t first, int
  *   the cache; the query to q_out_dev (q_dev NULL: no queries; q_out_dev may be q_dev with the same leading dimension, and must not overlap it otherwise).
  *   k_dev, v_dev: fp16, head i of row t at t * k_ld + i * d_h; q_dev, q_out_dev: the same with h_q heads.  16-byte aligned, leading dimensions multiples of 8 (slices of one
  *   q/k/v projection are).
- * qlinear_paged_read: fp16(q s) of the rows' tokens, k_out_dev and v_out_dev fp16 [T, h_kv, d_h] (rows = kv_len for a whole sequence).
+ * qlinear_paged_read: fp16(q s) of the rows' tokens, k_out_dev and v_out_dev fp16 [T, h_kv, d_h] (rows = kv_len for a whole sequence; zeros for a row with p < 0).
  * qlinear_paged_attention: out[t, h] = sum_j softmax_j(x_j) v_j with x_j = scale q.k_j, or softcap * tanh(scale q.k_j / softcap) where softcap > 0, over the visible tokens of the
  *   row's sequence: j <= p, j < kv_len, and p - j < window where window > 0.  |scale| <= 1e15.  Query head h reads KV head h / (h_q / h_kv).  A row that sees nothing gives zeros.  max_q: no sequence has
  *   more rows (rows beyond it are left as they are); scores, softmax and sums in fp32, weights and values fp16, with many rows (below) the keys as well.  out_dev must not overlap q_dev.
