@@ -374,6 +374,65 @@ ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q_dev, int64_t 
                                   const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T, int32_t max_q, float scale, float softcap, int32_t window,
                                   void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
 
+/* Pages that requests share.  refs_dev [n_pages] int32, the caller's: how many entries of its page tables hold a page, 0: free.  The calls keep it so; it has to be so when they
+ * begin.  Tables are those of the calls above (entries outside the pool: no page), changed in place; all decisions are made on the device from what the arrays hold when the kernels run.
+ * qlinear_paged_fork: row i of children_dev (n rows of table_width columns) := the pages of the first lengths[i] tokens of row parents[i] of the table, -1 behind them and where parents[i] is no row; each of
+ *   these pages has one holder more.  What the row held before is overwritten, not given back.  children_dev must not overlap the table (other rows of the same array are fine).  n <= QL_PAGED_MAX_SEQUENCES.
+ * qlinear_paged_release: row rows[i] gives back the pages behind its first keep[i] tokens (keep NULL: all): entries -1, one holder less each.  Numbers that are no row are passed over; a row named twice gives
+ *   back what any of the two says.  n <= 65535.
+ * qlinear_paged_reserve: gives every sequence of the batch pages of its own for its new tokens (positions max(kv_len - rows, 0) to kv_len - 1, as far as the table has columns): a column without a page gets a free one,
+ *   a page with more than one holder is replaced by a free one (one holder less; what it holds of the sequence's older tokens is copied).  In the order of sequences and columns they get the lowest
+ *   free pages, whose refs become 1.  missing_dev[0] := 0; or, if the pool has too few free pages, how many it is short of, and nothing else is changed.  Pages whose last holder was replaced are free for the next call.
+ * qlinear_paged_compact: the live pages (refs > 0), n of them, take the places 0 to n - 1: those numbered n and up move to the free places below n, both in order, with contents, refs and, if given, the
+ *   summaries (below).  The table's entries follow (an entry of a free page becomes -1); moved_dev [n_pages]: where each page is now, -1 for those that were free (for tables that the call does not see).
+ *   workspace_dev: qlinear_paged_pages_workspace bytes of the caller's for reserve and compact, 32-byte aligned, overwritten; calls that may overlap need one each.
+ * Calls that change refs, a table or the pool must be ordered against every other call on them.  Asynchronous, allocate nothing.  Errors as above. */
+ql_status qlinear_paged_fork(qlinear_paged_t h, int32_t* refs_dev, const int32_t* table, int64_t table_ld, int32_t table_width, int32_t B, const int32_t* parents, const int32_t* lengths, int32_t n,
+                             int32_t* children_dev, int64_t children_ld, void* cuda_stream);
+ql_status qlinear_paged_release(qlinear_paged_t h, int32_t* refs_dev, int32_t* table, int64_t table_ld, int32_t table_width, int32_t B, const int32_t* rows, const int32_t* keep, int32_t n, void* cuda_stream);
+size_t qlinear_paged_pages_workspace(qlinear_paged_t h);
+ql_status qlinear_paged_reserve(qlinear_paged_t h, int32_t* refs_dev, int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T,
+                                int32_t* missing_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+ql_status qlinear_paged_compact(qlinear_paged_t h, int32_t* refs_dev, int32_t* table, int64_t table_ld, int32_t table_width, int32_t B, void* bounds_dev, float* scales_dev, int32_t* moved_dev,
+                                void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/* Attention over a few pages of long sequences, for calls of few rows: summaries of pages, the choice of pages for a row by them, and the attention over the chosen ones.
+ *   bounds_dev int8 [n_pages, h_kv, 2, d_h], 16-byte aligned, and scales_dev fp32 [n_pages, h_kv]: the caller's, what the summaries of the pool's pages are held in.
+ * qlinear_paged_summarise: for every page that one of the batch's rows lies in (after they have been appended), over its tokens j < kv_len, with hi_c and lo_c the largest and the smallest key element fp16(q s) of channel c of a
+ *   KV head and top = max_c max(hi_c, -lo_c):  scale = top / 127,  r = 127 / top,  bounds = min(127, ceil(hi_c r)) and max(-127, floor(lo_c r))     (IEEE fp32 operations; top 0: zeros).
+ * qlinear_paged_select: for row t at position p and KV head k the candidates are the columns c <= min(p / page_size, table_width - 1) of its sequence's table row whose entry lies in the pool.  With Q+ and Q- the sums over
+ *   the query heads that read k, in their order, of max(q, 0) and min(q, 0), a = the largest magnitude of both and r = 32767 / a (a 0: all zero), in IEEE fp32, their codes rint(Q r), and of the page
+ *       score = fp32(sum_c code+_c hi_c + code-_c lo_c) * scale            (the sum exact; it bounds the sum of the heads' scores from above, but for the codes' rounding)
+ *   the `first` first and the `recent` last candidate columns' places (columns c < first, c > the last column - recent) come before all others, then the largest scores, of equal ones the lowest columns.
+ *   pages_dev[t, k, :] := the min(budget, candidates) columns so chosen, ascending, -1 behind them.  first + recent <= budget.  table_width <= 262144.  Queries must be finite (others choose some of the candidates).
+ *   Rows of no sequence are left as they are; a row at a negative position has no candidates.  No row may be two sequences'.
+ * qlinear_paged_attention_selected: qlinear_paged_attention (no window) over those visible tokens of the row's sequence that lie in the listed pages of each KV head: pages_dev as select leaves it, or columns
+ *   of the caller's choice in any order, of which the first min(budget, ceil(kv_len / page_size)) count; a column named twice counts twice, numbers outside [0, table_width) and columns whose entry lies outside the pool are passed
+ *   over.  A row that sees nothing gives zeros.  T * (budget * page_size / 16 + 33) * (h_q / h_kv / 8, rounded up) must be below 2^31.  Every row reads its pages by itself: for many rows
+ *   that share most of them qlinear_paged_attention reads less.  workspace_dev: qlinear_paged_attention_selected_workspace bytes, 32-byte aligned, overwritten.
+ *
+ * qlinear_paged_attention_shared: qlinear_paged_attention (no window) for a batch of which sequences share the beginning: group g is the sequences group_start[g] .. group_start[g + 1] - 1 (int32 [n_groups + 1]),
+ *   whose first prefix_len[g] tokens are the same, the table rows of the group holding the same pages for them or pages of the same contents.  The prefix is read and multiplied once for all rows of the group (from the pages of one of
+ *   its sequences), what follows once per sequence, and the two are joined; the result is that of qlinear_paged_attention up to rounding.  A prefix longer than what one of the group's rows sees counts as
+ *   far as all see it.  Sequences of no group, and groups that do not lie in [0, B) or that have less than two sequences, share nothing; no sequence may be in two groups.  n_groups <= QL_PAGED_MAX_SEQUENCES.
+ *   Calls with max_q * h_q / h_kv >= 256 query rows a sequence and KV head, which gain nothing by it, are qlinear_paged_attention calls.  The limits on B * C and T are those of that call with n_groups + B in the place of B.
+ *   workspace_dev: qlinear_paged_attention_shared_workspace bytes, 32-byte aligned, overwritten.
+ * Asynchronous, allocate nothing; ordered against appends, summaries and moves of the same pages by the caller.  Errors as above. */
+ql_status qlinear_paged_summarise(qlinear_paged_t h, const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T,
+                                  void* bounds_dev, float* scales_dev, void* cuda_stream);
+ql_status qlinear_paged_select(qlinear_paged_t h, const void* q_dev, int64_t q_ld, int32_t h_q, const void* bounds_dev, const float* scales_dev,
+                               const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T,
+                               int32_t budget, int32_t first, int32_t recent, int32_t* pages_dev, void* cuda_stream);
+size_t qlinear_paged_attention_selected_workspace(qlinear_paged_t h, int32_t h_q);
+ql_status qlinear_paged_attention_selected(qlinear_paged_t h, const void* q_dev, int64_t q_ld, void* out_dev, int64_t out_ld, int32_t h_q, const int32_t* pages_dev, int32_t budget,
+                                           const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T,
+                                           float scale, float softcap, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+size_t qlinear_paged_attention_shared_workspace(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t T, int32_t max_q, int32_t n_groups);
+ql_status qlinear_paged_attention_shared(qlinear_paged_t h, const void* q_dev, int64_t q_ld, void* out_dev, int64_t out_ld, int32_t h_q,
+                                         const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T, int32_t max_q,
+                                         const int32_t* group_start, const int32_t* prefix_len, int32_t n_groups, float scale, float softcap,
+                                         void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
 /* Adjusts the logits of an LM head before sampling.  Row r of `rows` has the history tokens[start[r]] .. tokens[start[r + 1] - 1], its first n_prompt[r] tokens the prompt
  * (n_prompt NULL: none), the others the output.  For every token v of the vocabulary, x = logits[r, v] in fp32:
  *     seen in the history:               x = x > 0 ? x / repetition[r] : x * repetition[r]

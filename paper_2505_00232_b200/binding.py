@@ -27,6 +27,8 @@ EXPORTS = (
     "qlinear_status_string", "qlinear_version", "qlinear_debug_plan", "qlinear_debug_plan_kv_output", "qlinear_debug_takes_batch_kernel", "qlinear_debug_kv_hold", "qlinear_debug_route", "qlinear_debug_plan_a8", "qlinear_debug_config_reads",
     "qlinear_rope_tables", "qlinear_paged_page_bytes", "qlinear_paged_create", "qlinear_paged_destroy", "qlinear_paged_device_status", "qlinear_paged_append", "qlinear_paged_read",
     "qlinear_paged_attention_workspace", "qlinear_paged_attention", "qlinear_adjust_logits", "qlinear_debug_paged_ctas",
+    "qlinear_paged_fork", "qlinear_paged_release", "qlinear_paged_pages_workspace", "qlinear_paged_reserve", "qlinear_paged_compact", "qlinear_paged_summarise", "qlinear_paged_select",
+    "qlinear_paged_attention_selected_workspace", "qlinear_paged_attention_selected", "qlinear_paged_attention_shared_workspace", "qlinear_paged_attention_shared",
 )
 
 
@@ -143,7 +145,22 @@ def _load() -> ctypes.CDLL:
     lib.qlinear_debug_paged_ctas.argtypes = [vp, i32, ctypes.POINTER(i32)]
     lib.qlinear_debug_paged_ctas.restype = i32
     lib.qlinear_adjust_logits.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, i32, vp]
-    for f in ("qlinear_rope_tables", "qlinear_paged_create", "qlinear_paged_destroy", "qlinear_paged_device_status", "qlinear_paged_append", "qlinear_paged_read", "qlinear_paged_attention", "qlinear_adjust_logits"):
+    lib.qlinear_paged_fork.argtypes = [vp, vp, vp, i64, i32, i32, vp, vp, i32, vp, i64, vp]
+    lib.qlinear_paged_release.argtypes = [vp, vp, vp, i64, i32, i32, vp, vp, i32, vp]
+    lib.qlinear_paged_reserve.argtypes = [vp, vp, *batch, vp, vp, size, vp]
+    lib.qlinear_paged_compact.argtypes = [vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, size, vp]
+    lib.qlinear_paged_summarise.argtypes = [vp, *batch, vp, vp, vp]
+    lib.qlinear_paged_select.argtypes = [vp, vp, i64, i32, vp, vp, *batch, i32, i32, i32, vp, vp]
+    lib.qlinear_paged_attention_selected.argtypes = [vp, vp, i64, vp, i64, i32, vp, i32, *batch, f32, f32, vp, size, vp]
+    lib.qlinear_paged_attention_shared.argtypes = [vp, vp, i64, vp, i64, i32, *batch, i32, vp, vp, i32, f32, f32, vp, size, vp]
+    lib.qlinear_paged_pages_workspace.argtypes = [vp]
+    lib.qlinear_paged_attention_selected_workspace.argtypes = [vp, i32]
+    lib.qlinear_paged_attention_shared_workspace.argtypes = [vp, i32, i32, i32, i32, i32]
+    for f in ("qlinear_paged_pages_workspace", "qlinear_paged_attention_selected_workspace", "qlinear_paged_attention_shared_workspace"):
+        getattr(lib, f).restype = size
+    for f in ("qlinear_rope_tables", "qlinear_paged_create", "qlinear_paged_destroy", "qlinear_paged_device_status", "qlinear_paged_append", "qlinear_paged_read", "qlinear_paged_attention", "qlinear_adjust_logits",
+              "qlinear_paged_fork", "qlinear_paged_release", "qlinear_paged_reserve", "qlinear_paged_compact", "qlinear_paged_summarise", "qlinear_paged_select", "qlinear_paged_attention_selected",
+              "qlinear_paged_attention_shared"):
         getattr(lib, f).restype = ctypes.c_int
     return lib
 
@@ -217,7 +234,9 @@ def qlinear_unpack(desc: Desc, packed: np.ndarray):
 _half = _raw_stream = _device = _native = _serving = None
 _NATIVE_API = ("qlinear_forward", "qlinear_forward_a8", "qlinear_forward_group", "qlinear_forward_gated", "qlinear_residual_rmsnorm", "qlinear_rope_qkv", "qlinear_embed",
                "qlinear_kv_append_heads", "qlinear_kv_scores_heads", "qlinear_kv_output_heads", "qlinear_kv_output", "qlinear_kv_output_uses_tmp")
-_SERVING_API = ("qlinear_paged_append", "qlinear_paged_read", "qlinear_paged_attention_workspace", "qlinear_paged_attention", "qlinear_adjust_logits", "qlinear_rope_tables")
+_SERVING_API = ("qlinear_paged_append", "qlinear_paged_read", "qlinear_paged_attention_workspace", "qlinear_paged_attention", "qlinear_adjust_logits", "qlinear_rope_tables",
+                "qlinear_paged_fork", "qlinear_paged_release", "qlinear_paged_pages_workspace", "qlinear_paged_reserve", "qlinear_paged_compact", "qlinear_paged_summarise", "qlinear_paged_select",
+                "qlinear_paged_attention_selected_workspace", "qlinear_paged_attention_selected", "qlinear_paged_attention_shared_workspace", "qlinear_paged_attention_shared")
 
 
 def _bind_torch():
@@ -642,6 +661,191 @@ class PagedKV:
         if out.shape[0] != T:
             raise QLinearError(QL_ERR_INVALID_ARG, where + " (bad out tensor)")
         _check(lib.qlinear_paged_attention(self._h, q.data_ptr(), q_ld, out.data_ptr(), out_ld, h_q, *batch, max_q, scale, softcap, window, work.data_ptr(), size, st), where)
+        return out
+
+    def _ints(self, where, *tensors):
+        """The addresses of int32 vectors (or None) on the cache's device, of the length that comes with each (None: any)."""
+        import torch
+        for t, n in tensors:
+            if t is not None and (t.dtype != torch.int32 or t.device != self.device or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.shape[0] != n) or t.shape[0] > 2 ** 31 - 1):
+                raise QLinearError(QL_ERR_INVALID_ARG, where + " (int32 CUDA vectors of the right lengths on the cache's device)")
+        return [None if t is None else t.data_ptr() for t, _ in tensors]
+
+    def _table(self, table, where):
+        """(address, leading dimension, columns, rows) of a page table."""
+        import torch
+        if table.dtype != torch.int32 or table.device != self.device or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (page_table int32 [rows, pages] on the cache's device)")
+        n, W = table.shape
+        _check_i32(where, n, W)
+        return table.data_ptr() if table.numel() else None, max(table.stride(0), W) if n <= 1 else table.stride(0), W, n
+
+    def _bounds(self, bounds, where):
+        import torch
+        ok = len(bounds) == 2 and all(t.device == self.device and t.is_contiguous() for t in bounds) and bounds[0].dtype == torch.int8 and bounds[1].dtype == torch.float32
+        if not ok or tuple(bounds[0].shape) != (self.n_pages, self.h_kv, 2, self.d_h) or tuple(bounds[1].shape) != (self.n_pages, self.h_kv):
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (bounds: what key_bounds returns)")
+        return bounds[0].data_ptr(), bounds[1].data_ptr()
+
+    def fork(self, refs, page_table, parents, lengths, out=None, stream=None):
+        """parents, lengths int32 [n] -> int32 [n, pages]: rows with the pages of the first lengths[i] tokens of row parents[i], -1 behind them; refs (int32 [n_pages], how many entries of the caller's page tables hold a
+        page) counts the new entries.  out: rows to write them to, which hold no pages; they must not overlap page_table."""
+        y = _serving.paged_fork(self._native, refs, page_table, parents, lengths, out, self.n_pages, _raw(stream))
+        if y is not None:
+            return y
+        import torch
+        where, n = "qlinear_paged_fork", parents.shape[0]
+        table = self._table(page_table, where)
+        at = self._ints(where, (refs, self.n_pages), (parents, n), (lengths, n))
+        _check_i32(where, n)
+        st, here = _on_stream(self.device, stream)
+        if out is None:
+            with here:
+                out = torch.empty((n, table[2]), dtype=torch.int32, device=self.device)
+        to = self._table(out, where)
+        if to[2:] != (table[2], n):
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (bad out tensor)")
+        _check(lib.qlinear_paged_fork(self._h, at[0], *table, at[1], at[2], n, to[0], to[1], st), where)
+        return out
+
+    def release(self, refs, page_table, rows, keep=None, stream=None) -> None:
+        """Rows `rows` (int32 [n]) of the page table give back their pages behind their first keep[i] tokens (None: all of them)."""
+        if _serving.paged_release(self._native, refs, page_table, rows, keep, self.n_pages, _raw(stream)) is not None:
+            return
+        where, n = "qlinear_paged_release", rows.shape[0]
+        table = self._table(page_table, where)
+        at = self._ints(where, (refs, self.n_pages), (rows, n), (keep, n))
+        _check_i32(where, n)
+        _check(lib.qlinear_paged_release(self._h, at[0], *table, at[1], at[2], n, _on_stream(self.device, stream)[0]), where)
+
+    def reserve(self, refs, page_table, kv_len, q_start, T: int, stream=None):
+        """Gives every sequence of the batch pages of its own for its T new rows, before they are appended: free ones where the page table has none, copies where others hold the page too.  Returns int32 [1]: 0,
+        or how many pages the pool is short of, in which case nothing has changed."""
+        y = _serving.paged_reserve(self._native, refs, page_table, kv_len, q_start, T, self.n_pages, _raw(stream))
+        if y is not None:
+            return y
+        import torch
+        where = "qlinear_paged_reserve"
+        batch = self._batch(page_table, kv_len, q_start, T, where)
+        at = self._ints(where, (refs, self.n_pages))
+        st, here = _on_stream(self.device, stream)
+        size = lib.qlinear_paged_pages_workspace(self._h)
+        with here:
+            missing = torch.empty(1, dtype=torch.int32, device=self.device)
+            work = torch.empty(size, dtype=torch.uint8, device=self.device)
+        _check(lib.qlinear_paged_reserve(self._h, at[0], *batch, missing.data_ptr(), work.data_ptr(), size, st), where)
+        return missing
+
+    def compact(self, refs, page_table, bounds=None, stream=None):
+        """Moves the live pages (refs > 0) to the front of the pool, with their entries of the page table, refs and (what key_bounds returns) summaries.  Returns int32 [n_pages]: where each page is now, -1 for free ones."""
+        y = _serving.paged_compact(self._native, refs, page_table, None if bounds is None else bounds[0], None if bounds is None else bounds[1], self.n_pages, _raw(stream))
+        if y is not None:
+            return y
+        import torch
+        where = "qlinear_paged_compact"
+        table = self._table(page_table, where)
+        at = self._ints(where, (refs, self.n_pages))
+        b = (None, None) if bounds is None else self._bounds(bounds, where)
+        st, here = _on_stream(self.device, stream)
+        size = lib.qlinear_paged_pages_workspace(self._h)
+        with here:
+            moved = torch.empty(self.n_pages, dtype=torch.int32, device=self.device)
+            work = torch.empty(size, dtype=torch.uint8, device=self.device)
+        _check(lib.qlinear_paged_compact(self._h, at[0], *table, *b, moved.data_ptr(), work.data_ptr(), size, st), where)
+        return moved
+
+    def key_bounds(self):
+        """(int8 [n_pages, h_kv, 2, d_h], fp32 [n_pages, h_kv]), zeros: what `summarise` keeps of every page, the largest and the smallest key element per channel and the unit that they are held in."""
+        import torch
+        return (torch.zeros((self.n_pages, self.h_kv, 2, self.d_h), dtype=torch.int8, device=self.device), torch.zeros((self.n_pages, self.h_kv), dtype=torch.float32, device=self.device))
+
+    def summarise(self, bounds, page_table, kv_len, q_start, T: int, stream=None) -> None:
+        """Brings the summaries of the pages that the batch's T new rows lie in up to date, after they have been appended."""
+        if _serving.paged_summarise(self._native, bounds[0], bounds[1], page_table, kv_len, q_start, T, self.n_pages, _raw(stream)) is not None:
+            return
+        where = "qlinear_paged_summarise"
+        batch = self._batch(page_table, kv_len, q_start, T, where)
+        _check(lib.qlinear_paged_summarise(self._h, *batch, *self._bounds(bounds, where), _on_stream(self.device, stream)[0]), where)
+
+    def select(self, q, bounds, page_table, kv_len, q_start, budget: int, first: int = 1, recent: int = 1, out=None, stream=None):
+        """q fp16 [T, h_q * d_h] or [T, h_q, d_h] -> int32 [T, h_kv, budget]: for every row and KV head the columns of its page table row that promise the largest scores by their summaries, the `first`
+        first and the `recent` last ones always among them; ascending, -1 behind them."""
+        y = _serving.paged_select(self._native, q, bounds[0], bounds[1], page_table, kv_len, q_start, budget, first, recent, out, self.n_pages, _raw(stream))
+        if y is not None:
+            return y
+        import torch
+        where = "qlinear_paged_select"
+        q_ld, h_q = self._rows(q, None, where)
+        T = q.shape[0]
+        batch = self._batch(page_table, kv_len, q_start, T, where)
+        _check_i32(where, h_q, budget, first, recent)
+        if h_q % self.h_kv or budget < 1:
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (query heads a multiple of the KV heads, budget >= 1)")
+        b = self._bounds(bounds, where)
+        st, here = _on_stream(self.device, stream)
+        if out is None:
+            with here:
+                out = torch.empty((T, self.h_kv, budget), dtype=torch.int32, device=self.device)
+        elif out.dtype != torch.int32 or out.device != self.device or tuple(out.shape) != (T, self.h_kv, budget) or not out.is_contiguous():
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (bad out tensor)")
+        _check(lib.qlinear_paged_select(self._h, q.data_ptr(), q_ld, h_q, *b, *batch, budget, first, recent, out.data_ptr(), st), where)
+        return out
+
+    def attention_selected(self, q, pages, page_table, kv_len, q_start, scale=None, softcap: float = 0.0, out=None, stream=None):
+        """q fp16 [T, h_q * d_h] or [T, h_q, d_h] -> fp16 [T, h_q, d_h]: causal attention over the columns of the page table that pages (int32 [T, h_kv, budget], as `select` returns it) lists for each
+        row and KV head.  scale None: 1 / sqrt(d_h)."""
+        scale = self.d_h ** -0.5 if scale is None else scale
+        y = _serving.paged_attention_selected(self._native, q, pages, page_table, kv_len, q_start, scale, softcap, out, _raw(stream))
+        if y is not None:
+            return y
+        import torch
+        where = "qlinear_paged_attention_selected"
+        q_ld, h_q = self._rows(q, None, where)
+        T = q.shape[0]
+        batch = self._batch(page_table, kv_len, q_start, T, where)
+        if h_q % self.h_kv:
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (query heads a multiple of the KV heads)")
+        if pages.dtype != torch.int32 or pages.device != self.device or pages.dim() != 3 or tuple(pages.shape[:2]) != (T, self.h_kv) or not pages.is_contiguous():
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (pages must be contiguous int32 [T, h_kv, budget] on the cache's device)")
+        _check_i32(where, h_q, pages.shape[2])
+        st, here = _on_stream(self.device, stream)
+        size = lib.qlinear_paged_attention_selected_workspace(self._h, h_q)
+        with here:
+            if out is None:
+                out = torch.empty((T, h_q, self.d_h), dtype=torch.float16, device=self.device)
+            work = torch.empty(size, dtype=torch.uint8, device=self.device)
+        out_ld, n = self._rows(out, h_q, where)
+        if out.shape[0] != T:
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (bad out tensor)")
+        _check(lib.qlinear_paged_attention_selected(self._h, q.data_ptr(), q_ld, out.data_ptr(), out_ld, h_q, pages.data_ptr() if pages.numel() else None, pages.shape[2], *batch, scale, softcap, work.data_ptr(), size, st), where)
+        return out
+
+    def attention_shared(self, q, page_table, kv_len, q_start, max_q: int, group_start, prefix_len, scale=None, softcap: float = 0.0, out=None, stream=None):
+        """`attention` (without a window) of a batch of which sequences share their beginning: the sequences group_start[g] .. group_start[g + 1] - 1 (int32 [groups + 1]) have the same first prefix_len[g] (int32 [groups])
+        tokens, which are read and multiplied once for all of them."""
+        scale = self.d_h ** -0.5 if scale is None else scale
+        y = _serving.paged_attention_shared(self._native, q, page_table, kv_len, q_start, max_q, group_start, prefix_len, scale, softcap, out, _raw(stream))
+        if y is not None:
+            return y
+        import torch
+        where = "qlinear_paged_attention_shared"
+        q_ld, h_q = self._rows(q, None, where)
+        T, G = q.shape[0], prefix_len.shape[0]
+        batch = self._batch(page_table, kv_len, q_start, T, where)
+        groups = self._ints(where, (group_start, G + 1), (prefix_len, G))
+        _check_i32(where, h_q, max_q, G)
+        if h_q % self.h_kv or max_q < 0:
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (query heads a multiple of the KV heads, max_q >= 0)")
+        st, here = _on_stream(self.device, stream)
+        size = lib.qlinear_paged_attention_shared_workspace(self._h, h_q, batch[5], T, max_q, G)
+        with here:
+            if out is None:
+                out = torch.empty((T, h_q, self.d_h), dtype=torch.float16, device=self.device)
+            work = torch.empty(size, dtype=torch.uint8, device=self.device)
+        out_ld, n = self._rows(out, h_q, where)
+        if out.shape[0] != T:
+            raise QLinearError(QL_ERR_INVALID_ARG, where + " (bad out tensor)")
+        _check(lib.qlinear_paged_attention_shared(self._h, q.data_ptr(), q_ld, out.data_ptr(), out_ld, h_q, *batch, max_q, *groups, G, scale, softcap, work.data_ptr(), size, st), where)
         return out
 
     def device_status(self):

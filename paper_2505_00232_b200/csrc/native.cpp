@@ -367,6 +367,17 @@ struct ServingApi {
     decltype(&qlinear_paged_attention) attention;
     decltype(&qlinear_adjust_logits) adjust_logits;
     decltype(&qlinear_rope_tables) rope_tables;
+    decltype(&qlinear_paged_fork) fork;
+    decltype(&qlinear_paged_release) release;
+    decltype(&qlinear_paged_pages_workspace) pages_workspace;
+    decltype(&qlinear_paged_reserve) reserve;
+    decltype(&qlinear_paged_compact) compact;
+    decltype(&qlinear_paged_summarise) summarise;
+    decltype(&qlinear_paged_select) select;
+    decltype(&qlinear_paged_attention_selected_workspace) selected_workspace;
+    decltype(&qlinear_paged_attention_selected) selected;
+    decltype(&qlinear_paged_attention_shared_workspace) shared_workspace;
+    decltype(&qlinear_paged_attention_shared) shared;
 } serving;
 
 bool small_int(PyObject* o, int64_t* v)                                  // a Python int from 0 to INT_MAX
@@ -511,6 +522,218 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t)     // (cac
     });
 }
 
+// ---- pages, summaries, shared and sparse contexts.  n_pages: the cache's, for refs and summaries.
+bool ints_of(PyObject* o, const Paged& p, int64_t n, int32_t** v)        // an int32 vector of n numbers on the cache's device
+{
+    const at::Tensor* t = plain(o, at::kInt);
+    if (!t || t->dim() != 1 || t->size(0) != n || t->get_device() != p.device) return false;
+    *v = static_cast<int32_t*>(t->data_ptr());
+    return true;
+}
+int64_t length_of(PyObject* o)                                           // of an int32 vector, -1: none
+{
+    const at::Tensor* t = plain(o, at::kInt);
+    return t && t->dim() == 1 && t->size(0) <= INT_MAX ? t->size(0) : -1;
+}
+struct Table { int32_t* at; int64_t ld; int32_t width, rows; };
+bool table_of(PyObject* o, const Paged& p, Table* r)
+{
+    const at::Tensor* t = strided(o, at::kInt);
+    if (!matrix_rows(t, &r->ld) || t->get_device() != p.device || t->size(0) > INT_MAX || t->size(1) > INT_MAX) return false;
+    r->at = t->numel() ? static_cast<int32_t*>(t->data_ptr()) : nullptr;
+    r->rows = (int32_t)t->size(0);
+    r->width = (int32_t)t->size(1);
+    return true;
+}
+bool bounds_of(PyObject* b, PyObject* s, const Paged& p, int64_t n_pages, void** bounds, float** scales)
+{
+    const at::Tensor *t = plain(b, at::kChar), *u = plain(s, at::kFloat);
+    if (!t || !u || t->get_device() != p.device || u->get_device() != p.device || t->dim() != 4 || u->dim() != 2) return false;
+    if (t->size(0) != n_pages || t->size(1) != p.h_kv || t->size(2) != 2 || t->size(3) != p.d || u->size(0) != n_pages || u->size(1) != p.h_kv) return false;
+    *bounds = t->data_ptr();
+    *scales = static_cast<float*>(u->data_ptr());
+    return true;
+}
+at::Tensor made_ints(at::IntArrayRef sizes, const Paged& p) { return at::detail::empty_cuda(sizes, at::kInt, at::Device(at::kCUDA, (c10::DeviceIndex)p.device), std::nullopt); }
+at::Tensor made_bytes(size_t n, const Paged& p) { return at::detail::empty_cuda({(int64_t)n}, at::kByte, at::Device(at::kCUDA, (c10::DeviceIndex)p.device), std::nullopt); }
+
+PyObject* paged_fork(PyObject*, PyObject* const* a, Py_ssize_t)          // (cache, refs, table, parents, lengths, out, n_pages, stream)
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Table t, o{};
+        int64_t n_pages;
+        int32_t *refs, *parents, *lengths;
+        if (a[7] != Py_None || !paged_of(a[0], &p) || !small_int(a[6], &n_pages) || !table_of(a[2], p, &t) || !ints_of(a[1], p, n_pages, &refs)) Py_RETURN_NONE;
+        const int64_t n = length_of(a[3]);
+        if (n < 0 || !ints_of(a[3], p, n, &parents) || !ints_of(a[4], p, n, &lengths)) Py_RETURN_NONE;
+        const bool make = a[5] == Py_None;
+        if (!make && (!table_of(a[5], p, &o) || o.rows != n || o.width != t.width)) Py_RETURN_NONE;
+        at::Tensor made;
+        void* st = stream_on(p.device);
+        if (!done([&] {
+                if (make) { made = made_ints({n, t.width}, p); o = {made.numel() ? static_cast<int32_t*>(made.data_ptr()) : nullptr, t.width, t.width, (int32_t)n}; }
+                return serving.fork(p.h, refs, t.at, t.ld, t.width, t.rows, parents, lengths, (int32_t)n, o.at, o.ld, st);
+            }, "qlinear_paged_fork")) return nullptr;
+        return make ? THPVariable_Wrap(std::move(made)) : Py_NewRef(a[5]);
+    });
+}
+
+PyObject* paged_release(PyObject*, PyObject* const* a, Py_ssize_t)       // (cache, refs, table, rows, keep, n_pages, stream)
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Table t;
+        int64_t n_pages;
+        int32_t *refs, *rows, *keep = nullptr;
+        if (a[6] != Py_None || !paged_of(a[0], &p) || !small_int(a[5], &n_pages) || !table_of(a[2], p, &t) || !ints_of(a[1], p, n_pages, &refs)) Py_RETURN_NONE;
+        const int64_t n = length_of(a[3]);
+        if (n < 0 || !ints_of(a[3], p, n, &rows) || (a[4] != Py_None && !ints_of(a[4], p, n, &keep))) Py_RETURN_NONE;
+        void* st = stream_on(p.device);
+        if (!done([&] { return serving.release(p.h, refs, t.at, t.ld, t.width, t.rows, rows, keep, (int32_t)n, st); }, "qlinear_paged_release")) return nullptr;
+        Py_RETURN_TRUE;
+    });
+}
+
+PyObject* paged_reserve(PyObject*, PyObject* const* a, Py_ssize_t)       // (cache, refs, table, kv_len, q_start, T, n_pages, stream)
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Batch b;
+        int64_t n_pages, T;
+        int32_t* refs;
+        if (a[7] != Py_None || !paged_of(a[0], &p) || !small_int(a[6], &n_pages) || !small_int(a[5], &T) || !batch_of(a + 2, p, &b) || !ints_of(a[1], p, n_pages, &refs)) Py_RETURN_NONE;
+        at::Tensor missing, work;
+        void* st = stream_on(p.device);
+        const size_t bytes = serving.pages_workspace(p.h);
+        if (!done([&] {
+                missing = made_ints({1}, p);
+                work = made_bytes(bytes, p);
+                return serving.reserve(p.h, refs, const_cast<int32_t*>(b.table), b.ld, b.width, b.kv_len, b.q_start, b.B, (int32_t)T, static_cast<int32_t*>(missing.data_ptr()), work.data_ptr(), bytes, st);
+            }, "qlinear_paged_reserve")) return nullptr;
+        return THPVariable_Wrap(std::move(missing));
+    });
+}
+
+PyObject* paged_compact(PyObject*, PyObject* const* a, Py_ssize_t)       // (cache, refs, table, bounds, scales, n_pages, stream)
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Table t;
+        int64_t n_pages;
+        int32_t* refs;
+        void* bounds = nullptr;
+        float* scales = nullptr;
+        if (a[6] != Py_None || !paged_of(a[0], &p) || !small_int(a[5], &n_pages) || !table_of(a[2], p, &t) || !ints_of(a[1], p, n_pages, &refs)) Py_RETURN_NONE;
+        if (a[3] != Py_None && !bounds_of(a[3], a[4], p, n_pages, &bounds, &scales)) Py_RETURN_NONE;
+        at::Tensor moved, work;
+        void* st = stream_on(p.device);
+        const size_t bytes = serving.pages_workspace(p.h);
+        if (!done([&] {
+                moved = made_ints({n_pages}, p);
+                work = made_bytes(bytes, p);
+                return serving.compact(p.h, refs, t.at, t.ld, t.width, t.rows, bounds, scales, static_cast<int32_t*>(moved.data_ptr()), work.data_ptr(), bytes, st);
+            }, "qlinear_paged_compact")) return nullptr;
+        return THPVariable_Wrap(std::move(moved));
+    });
+}
+
+PyObject* paged_summarise(PyObject*, PyObject* const* a, Py_ssize_t)     // (cache, bounds, scales, table, kv_len, q_start, T, n_pages, stream)
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Batch b;
+        int64_t n_pages, T;
+        void* bounds;
+        float* scales;
+        if (a[8] != Py_None || !paged_of(a[0], &p) || !small_int(a[7], &n_pages) || !small_int(a[6], &T) || !batch_of(a + 3, p, &b) || !bounds_of(a[1], a[2], p, n_pages, &bounds, &scales)) Py_RETURN_NONE;
+        void* st = stream_on(p.device);
+        if (!done([&] { return serving.summarise(p.h, b.table, b.ld, b.width, b.kv_len, b.q_start, b.B, (int32_t)T, bounds, scales, st); }, "qlinear_paged_summarise")) return nullptr;
+        Py_RETURN_TRUE;
+    });
+}
+
+PyObject* paged_select(PyObject*, PyObject* const* a, Py_ssize_t)        // (cache, q, bounds, scales, table, kv_len, q_start, budget, first, recent, out, n_pages, stream)
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Rows q;
+        Batch b;
+        int64_t n_pages, budget, first, recent;
+        void* bounds;
+        float* scales;
+        if (a[12] != Py_None || !paged_of(a[0], &p) || !rows_of(a[1], p, &q) || q.heads % p.h_kv || !small_int(a[11], &n_pages) || !batch_of(a + 4, p, &b) || !bounds_of(a[2], a[3], p, n_pages, &bounds, &scales) ||
+            !small_int(a[7], &budget) || budget < 1 || !small_int(a[8], &first) || !small_int(a[9], &recent)) Py_RETURN_NONE;
+        const bool make = a[10] == Py_None;
+        const at::Tensor* out = make ? nullptr : plain(a[10], at::kInt);
+        if (!make && (!out || out->get_device() != p.device || !out->sizes().equals({q.T, p.h_kv, budget}))) Py_RETURN_NONE;
+        at::Tensor made;
+        const void* qp = q.t->data_ptr();
+        void* st = stream_on(p.device);
+        if (!done([&] {
+                if (make) { made = made_ints({q.T, p.h_kv, budget}, p); out = &made; }
+                return serving.select(p.h, qp, q.ld, (int32_t)q.heads, bounds, scales, b.table, b.ld, b.width, b.kv_len, b.q_start, b.B, (int32_t)q.T, (int32_t)budget, (int32_t)first, (int32_t)recent,
+                                      static_cast<int32_t*>(out->data_ptr()), st);
+            }, "qlinear_paged_select")) return nullptr;
+        return make ? THPVariable_Wrap(std::move(made)) : Py_NewRef(a[10]);
+    });
+}
+
+PyObject* paged_attention_selected(PyObject*, PyObject* const* a, Py_ssize_t)   // (cache, q, pages, table, kv_len, q_start, scale, softcap, out, stream)
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Rows q, o{};
+        Batch b;
+        float scale, softcap;
+        if (a[9] != Py_None || !paged_of(a[0], &p) || !rows_of(a[1], p, &q) || q.heads % p.h_kv || !batch_of(a + 3, p, &b) || !real(a[6], &scale) || !real(a[7], &softcap)) Py_RETURN_NONE;
+        const at::Tensor* pages = plain(a[2], at::kInt);
+        if (!pages || pages->get_device() != p.device || pages->dim() != 3 || pages->size(0) != q.T || pages->size(1) != p.h_kv || pages->size(2) > INT_MAX) Py_RETURN_NONE;
+        const bool make = a[8] == Py_None;
+        if (!make && (!rows_of(a[8], p, &o) || o.T != q.T || o.heads != q.heads)) Py_RETURN_NONE;
+        at::Tensor made, work;
+        const void* qp = q.t->data_ptr();
+        const int32_t* list = pages->numel() ? static_cast<const int32_t*>(pages->data_ptr()) : nullptr;
+        const int32_t budget = (int32_t)pages->size(2);
+        void* st = stream_on(p.device);
+        const size_t bytes = serving.selected_workspace(p.h, (int32_t)q.heads);
+        if (!done([&] {
+                if (make) { made = half_like(*q.t, {q.T, q.heads, p.d}); o.t = &made; o.ld = q.heads * p.d; }
+                work = made_bytes(bytes, p);
+                return serving.selected(p.h, qp, q.ld, o.t->data_ptr(), o.ld, (int32_t)q.heads, list, budget, b.table, b.ld, b.width, b.kv_len, b.q_start, b.B, (int32_t)q.T, scale, softcap, work.data_ptr(), bytes, st);
+            }, "qlinear_paged_attention_selected")) return nullptr;
+        return make ? THPVariable_Wrap(std::move(made)) : Py_NewRef(a[8]);
+    });
+}
+
+PyObject* paged_attention_shared(PyObject*, PyObject* const* a, Py_ssize_t)   // (cache, q, table, kv_len, q_start, max_q, group_start, prefix_len, scale, softcap, out, stream)
+{
+    return guarded([&]() -> PyObject* {
+        Paged p;
+        Rows q, o{};
+        Batch b;
+        int64_t max_q;
+        float scale, softcap;
+        int32_t *start, *prefix;
+        if (a[11] != Py_None || !paged_of(a[0], &p) || !rows_of(a[1], p, &q) || q.heads % p.h_kv || !batch_of(a + 2, p, &b) || !small_int(a[5], &max_q) || !real(a[8], &scale) || !real(a[9], &softcap)) Py_RETURN_NONE;
+        const int64_t G = length_of(a[7]);
+        if (G < 0 || !ints_of(a[6], p, G + 1, &start) || !ints_of(a[7], p, G, &prefix)) Py_RETURN_NONE;
+        const bool make = a[10] == Py_None;
+        if (!make && (!rows_of(a[10], p, &o) || o.T != q.T || o.heads != q.heads)) Py_RETURN_NONE;
+        at::Tensor made, work;
+        const void* qp = q.t->data_ptr();
+        void* st = stream_on(p.device);
+        const size_t bytes = serving.shared_workspace(p.h, (int32_t)q.heads, b.B, (int32_t)q.T, (int32_t)max_q, (int32_t)G);
+        if (!done([&] {
+                if (make) { made = half_like(*q.t, {q.T, q.heads, p.d}); o.t = &made; o.ld = q.heads * p.d; }
+                work = made_bytes(bytes, p);
+                return serving.shared(p.h, qp, q.ld, o.t->data_ptr(), o.ld, (int32_t)q.heads, b.table, b.ld, b.width, b.kv_len, b.q_start, b.B, (int32_t)q.T, (int32_t)max_q, start, prefix, (int32_t)G, scale, softcap,
+                                      work.data_ptr(), bytes, st);
+            }, "qlinear_paged_attention_shared")) return nullptr;
+        return make ? THPVariable_Wrap(std::move(made)) : Py_NewRef(a[10]);
+    });
+}
+
 // (logits, tokens, start, n_prompt, repetition, presence, frequency, bias_ids, bias_values, bias_start, mask, out, stream)
 PyObject* adjust_logits(PyObject*, PyObject* const* a, Py_ssize_t)
 {
@@ -610,6 +833,7 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n)
 PyMethodDef methods[] = {FAST(init), FAST(forward), FAST(forward_a8), FAST(forward_group), FAST(forward_gated), FAST(residual_rmsnorm), FAST(rope_qkv), FAST(embed),
                          FAST(kv_append), FAST(kv_scores), FAST(kv_scores_one), FAST(kv_output_heads), FAST(kv_output), {nullptr, nullptr, 0, nullptr}};
 PyMethodDef serving_methods[] = {{"init", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(init_serving)), METH_FASTCALL, nullptr}, FAST(paged_append), FAST(paged_read), FAST(paged_attention), FAST(adjust_logits), FAST(rope_tables),
+                                 FAST(paged_fork), FAST(paged_release), FAST(paged_reserve), FAST(paged_compact), FAST(paged_summarise), FAST(paged_select), FAST(paged_attention_selected), FAST(paged_attention_shared),
                                  {nullptr, nullptr, 0, nullptr}};
 PyModuleDef serving_module = {PyModuleDef_HEAD_INIT, "_native._serving", nullptr, -1, serving_methods, nullptr, nullptr, nullptr, nullptr};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

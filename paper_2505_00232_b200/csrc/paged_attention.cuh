@@ -27,6 +27,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "dequant.cuh"
 #include "paged.cuh"
 #include "sm100_ptx.cuh"
@@ -123,6 +125,15 @@ struct SoftCap {
     }
 };
 
+// What a call's segments are: kAttnAll, the tokens that a row sees (qlinear_paged_attention); kAttnListed, those of the pages listed for a row and KV head (.._selected), a segment per row; kAttnShared, the
+// shared beginning of a group's sequences for all rows of the group, and what follows of each sequence (.._shared), as paged_shared.cuh planned them: no segment is a row's whole result there.
+enum AttnKind { kAttnAll, kAttnListed, kAttnShared };
+
+// A stretch of tokens that some rows see (kAttnShared): rows t0 .. of the call, row 0's position, tokens first .. end - 1 (first a multiple of 64) as far as a row's position goes.
+struct AttnStretch {
+    int32_t t0, rows, pos0, first, end, seq, blocks, row_blocks;         // blocks of 16 tokens, blocks of kAttnCols rows: of the kernel of few rows
+};
+
 struct PagedAttnParams {
     PagedBatch batch;
     const __half* q;             // row t, head h at q + t * q_ld + h * D
@@ -133,7 +144,27 @@ struct PagedAttnParams {
     int32_t h_q, group, max_q, row_blocks, window;
     float scale, softcap;        // (softcap 0: none; not so far from the scale that SoftCap's constants leave fp32)
     int32_t grid;
+    // kAttnListed: columns of the page table [T, h_kv, budget]
+    const int32_t* pages;
+    int32_t budget;
+    // kAttnShared: stretches v0 .. v1 - 1 are this launch's; the first n_groups are groups'; sums of their lengths; o, and m and l, of the rows of uncut segments [2][T][h_q]
+    int32_t v0, v1, n_groups;
+    const AttnStretch* stretches;
+    const int32_t* lengths;
+    float* row_o;
+    float2* row_ml;
 };
+// Where the result of a row lies that an uncut segment of a stretch leaves.
+__device__ __forceinline__ int64_t attn_row(const PagedAttnParams& p, int part, int t, int head, int in_group)
+{
+    return ((int64_t)part * p.batch.T + t) * p.h_q + head * p.group + in_group;
+}
+// Blocks of the pages listed for a row of sequence b.
+__device__ __forceinline__ int listed_blocks(const PagedAttnParams& p, int b)
+{
+    const int len = p.batch.kv_len[b];
+    return len <= 0 ? 0 : min(p.budget, ((len - 1) >> (p.batch.log2_blocks + 4)) + 1) << p.batch.log2_blocks;
+}
 
 // Blocks [*first, *first + n) of 16 tokens that any served row of sequence b sees.
 __device__ __forceinline__ int attn_blocks(const PagedAttnParams& p, int b, int* first)
@@ -156,13 +187,16 @@ __device__ __forceinline__ uint32_t move_matrix(uint32_t a)
     return r;
 }
 // Sums over a scan of the sequences' lengths: pre[b] before sequence b (per head and row block).  Every thread takes part.
+template <AttnKind KIND>
 __device__ __forceinline__ void attn_scan(const PagedAttnParams& p, int* pre)
 {
     __shared__ int warp_sum[kAttnWarps];
     const int B = p.batch.B, tid = threadIdx.x, per = (B + 255) / 256, lo = min(B, tid * per), hi = min(B, lo + per);
     int sum = 0, first;
     for (int b = lo; b < hi; ++b) {
-        const int blocks = attn_blocks(p, b, &first), n = blocks > 0 ? blocks + kAttnOverhead : 0;
+        const int blocks = KIND == kAttnListed ? listed_blocks(p, b) : attn_blocks(p, b, &first);
+        int n = blocks > 0 ? blocks + kAttnOverhead : 0;
+        if (KIND == kAttnListed) n *= paged_rows(p.batch, b, &first);    // (a segment per row)
         pre[b + 1] = n;
         sum += n;
     }
@@ -186,15 +220,18 @@ struct AttnSegment {
     int32_t head, row0, n_rows, t0, pos0, first, n, slot;                // rows of the sequence row0 .. (n_rows of it), row 0's token and position; slot -1: the whole segment
     int64_t table, next;                                                 // offset of the sequence's row of the page table; where the next segment begins in the numbering
 };
+struct ListedSegment : AttnSegment { int64_t list; };                    // offset of the row's list
 
-template <int D, AttnCap CAP>
+template <int D, AttnCap CAP, AttnKind KIND = kAttnAll>
 __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_attention_kernel(const PagedAttnParams p)
 {
     constexpr int NB = D / 64, kBlock = AttnRing<D>::kBlock, S = AttnRing<D>::kStages, kStride = AttnRing<D>::kMergeStride;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float meet_m[2][kAttnWarps][kAttnCols], meet_l[2][kAttnWarps][kAttnCols];
     __shared__ __align__(8) uint64_t bars[kAttnWarps * S];
-    __shared__ AttnSegment segs[4];                                      // in turn: the last one (slow warps still look at it), this, the next, the one after it
+    using Segment = std::conditional_t<KIND == kAttnListed, ListedSegment, AttnSegment>;
+    __shared__ int where[KIND == kAttnListed ? kAttnWarps * S : 1];      // the block of the sequence in a stage of a ring, -1: none
+    __shared__ Segment segs[4];                                      // in turn: the last one (slow warps still look at it), this, the next, the one after it
     __shared__ volatile uint32_t abort_flag[4];
     // (at d_h 256 the queries lie in shared memory, read for every block)
     constexpr bool kQueriesApart = D == 256;
@@ -209,14 +246,19 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    attn_scan(p, pre);
+    if constexpr (KIND == kAttnShared) {
+        for (int v = tid; v <= p.v1 - p.v0; v += kAttnWarps * 32) pre[v] = p.lengths[p.v0 + v] - p.lengths[p.v0];
+        __syncthreads();
+    } else {
+        attn_scan<KIND>(p, pre);
+    }
 
-    const int h_kv = p.batch.h_kv, per_head = h_kv * p.row_blocks;
-    const int64_t total = (int64_t)pre[p.batch.B] * per_head;
+    const int h_kv = p.batch.h_kv, per_head = KIND == kAttnShared ? h_kv : h_kv * p.row_blocks, n_seqs = KIND == kAttnShared ? p.v1 - p.v0 : p.batch.B;   // (a stretch's length has its row blocks in it)
+    const int64_t total = (int64_t)pre[n_seqs] * per_head;
     const int64_t span = max((int64_t)kAttnSpan, (total + p.grid - 1) / p.grid);
     const int64_t w0 = (int64_t)blockIdx.x * span, w1 = min(total, w0 + span);
-    if (tid == 0) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    for (int b = blockIdx.x; b < p.batch.B; b += p.grid) {               // rows of sequences that see nothing: zeros
+    if (KIND != kAttnShared && tid == 0) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    for (int b = blockIdx.x; KIND != kAttnShared && b < p.batch.B; b += p.grid) {   // rows of sequences that see nothing: zeros
         int t0;
         const int rows = min(paged_rows(p.batch, b, &t0), p.max_q);
         if (pre[b + 1] > pre[b]) continue;
@@ -224,36 +266,54 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
             *reinterpret_cast<uint4*>(p.out + (t0 + e / (p.h_q * (D / 8))) * p.out_ld + 8 * (e % (p.h_q * (D / 8)))) = make_uint4(0, 0, 0, 0);
     }
     // The first segment from place w of the numbering on of which this CTA has blocks (n 0: none).  (by the warp with the fewest blocks; every lane computes it)
-    const auto describe = [&](int64_t w, AttnSegment* to) {
-        AttnSegment s{};
+    const auto describe = [&](int64_t w, Segment* to) {
+        Segment s{};
         while (w < w1) {
             const int x = (int)(w / per_head);
-            int lo = 0, hi = p.batch.B;                                  // pre[lo] <= x < pre[hi]
+            int lo = 0, hi = n_seqs;                                     // pre[lo] <= x < pre[hi]
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (pre[mid] <= x) lo = mid;
                 else hi = mid;
             }
-            const int b = lo, length = pre[b + 1] - pre[b], blocks = length - kAttnOverhead;
+            const int b = lo;
+            int length = pre[b + 1] - pre[b];
+            AttnStretch v;
+            if constexpr (KIND == kAttnListed) length = listed_blocks(p, b) + kAttnOverhead;
+            if constexpr (KIND == kAttnShared) { v = p.stretches[p.v0 + b]; length = v.blocks + kAttnOverhead; }
+            const int blocks = length - kAttnOverhead;
             const int64_t local = w - (int64_t)pre[b] * per_head;
             const int seg = (int)(local / length), ua = (int)(local - (int64_t)seg * length), ub = (int)min((int64_t)length, ua + (w1 - w));
             const int sa = max(ua - kAttnOverhead, 0), sb = max(ub - kAttnOverhead, 0);
             const int64_t begin = w - ua;
             w += ub - ua;
             if (sb <= sa) continue;
-            int first;
-            attn_blocks(p, b, &first);
-            const int rows_all = paged_rows(p.batch, b, &s.t0);
-            s.head = seg / p.row_blocks;
-            s.row0 = (seg - s.head * p.row_blocks) * kAttnCols;
-            s.n_rows = min(rows_all, p.max_q) * p.group;
-            s.pos0 = p.batch.kv_len[b] - rows_all;
-            s.first = first + sa;
             s.n = sb - sa;
             const bool whole = sa == 0 && sb == blocks;
             s.slot = whole ? -1 : sa > 0 ? 0 : 1;
-            s.table = b * p.batch.table_ld;
-            if (sa == 0 && !whole && lane == 0) p.split[blockIdx.x] = make_int4(b, s.head, s.row0 / kAttnCols, (int)((begin + length - 1) / span));
+            if constexpr (KIND == kAttnShared) {
+                s.head = seg / v.row_blocks;
+                s.row0 = (seg - s.head * v.row_blocks) * kAttnCols;
+                s.n_rows = v.rows * p.group;
+                s.t0 = v.t0;
+                s.pos0 = v.pos0;
+                s.first = v.first / kPagedBlock + sa;
+                s.table = v.seq * p.batch.table_ld;
+                if (whole && p.v0 + b >= p.n_groups) s.slot = -2;        // (uncut segments of a group's beginning and of what follows leave their rows apart)
+            } else {
+                int first = 0;
+                if (KIND == kAttnAll) attn_blocks(p, b, &first);
+                const int rows_all = paged_rows(p.batch, b, &s.t0), row = KIND == kAttnListed ? seg / per_head : 0, in_row = seg - row * per_head;
+                s.head = in_row / p.row_blocks;
+                s.row0 = (in_row - s.head * p.row_blocks) * kAttnCols;
+                s.n_rows = KIND == kAttnListed ? p.group : min(rows_all, p.max_q) * p.group;
+                s.pos0 = p.batch.kv_len[b] - rows_all + row;
+                s.t0 += row;
+                s.first = first + sa;
+                s.table = b * p.batch.table_ld;
+                if constexpr (KIND == kAttnListed) s.list = ((int64_t)s.t0 * h_kv + s.head) * p.budget;
+                if (sa == 0 && !whole && lane == 0) p.split[blockIdx.x] = make_int4(KIND == kAttnListed ? s.t0 : b, s.head, s.row0 / kAttnCols, (int)((begin + length - 1) / span));
+            }
             break;
         }
         s.next = w;
@@ -269,19 +329,29 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
     const uint8_t* src = nullptr;
     int page_next = -1, stage = 0, parity = 0, to = 0;                   // the stage (and its phase) that is read next, the one that is filled next
     uint32_t none_even = 0, none_odd = 0, none_after = 0;
-    const auto mine_of = [&](const AttnSegment& s) { return s.n > warp ? (s.n - warp + kAttnWarps - 1) / kAttnWarps : 0; };
-    const auto look_up = [&](const AttnSegment& s, int i) {              // the page of block i + lane
+    int column_next = -1, block_at = -1;                                 // kAttnListed: the column listed for it, and the block of the sequence that lane k's is
+    const auto mine_of = [&](const Segment& s) { return s.n > warp ? (s.n - warp + kAttnWarps - 1) / kAttnWarps : 0; };
+    const auto look_up = [&](const Segment& s, int i) {                  // the page of block i + lane
+        if constexpr (KIND == kAttnListed) {
+            const int entry = (s.first + warp + (i + lane) * kAttnWarps) >> p.batch.log2_blocks;
+            column_next = i + lane < mine_of(s) ? p.pages[s.list + entry] : -1;
+            if (column_next >= min(p.batch.table_width, 1 << (27 - p.batch.log2_blocks))) column_next = -1;   // (tokens of 31 bits)
+            page_next = column_next >= 0 ? p.batch.table[s.table + column_next] : -1;
+            return;
+        }
         const int at = (s.first + warp + (i + lane) * kAttnWarps) >> p.batch.log2_blocks;
         page_next = i + lane < mine_of(s) && at < p.batch.table_width ? p.batch.table[s.table + at] : -1;
     };
-    const auto place = [&](const AttnSegment& s, int i) {                // of block i + lane, from the page that has been looked up; which have none
+    const auto place = [&](const Segment& s, int i) {                // of block i + lane, from the page that has been looked up; which have none
         const bool ok = page_next >= 0 && page_next < p.batch.n_pages;
         const int u = s.first + warp + (i + lane) * kAttnWarps;
+        if (KIND == kAttnListed) block_at = ok ? column_next << p.batch.log2_blocks | (u & ((1 << p.batch.log2_blocks) - 1)) : -1;
         src = p.batch.pool + ((((int64_t)(ok ? page_next : 0) * h_kv + s.head) << p.batch.log2_blocks) + (u & ((1 << p.batch.log2_blocks) - 1))) * kBlock;
         return ~__ballot_sync(0xffffffffu, ok);
     };
     const auto request = [&](int i) {                                    // (block i lies in the window of `src`)
         if (lane == (i & 31)) {
+            if (KIND == kAttnListed) where[warp * S + to] = block_at;    // (seen by those who have waited for the stage)
             mbar_expect_tx(bar0 + 8 * to, kBlock);
             bulk_copy_g2s(ring_u32 + to * kBlock, src, kBlock, bar0 + 8 * to);
         }
@@ -293,7 +363,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
     const SoftCap cap(mag, p.softcap);
 
     uint32_t qf[kQueriesApart ? 1 : NB][2][4];
-    const auto load_queries = [&](const AttnSegment& s) {                // column g of the second operand
+    const auto load_queries = [&](const Segment& s) {                // column g of the second operand
         const int r = s.row0 + g, i = r / p.group;
         const __half* from = p.q + (int64_t)(s.t0 + i) * p.q_ld + (int64_t)(s.head * p.group + r - i * p.group) * D + 8 * c;
 #pragma unroll
@@ -315,7 +385,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
     bool ok = true;
     int meeting = 0;
     for (int it = 0; segs[it].n > 0; it = (it + 1) & 3) {
-        const AttnSegment &s = segs[it], &nx = segs[(it + 1) & 3];
+        const Segment &s = segs[it], &nx = segs[(it + 1) & 3];
         const int n_mine = mine_of(s), n_next = mine_of(nx);
         if (n_mine == 0 || (requested > 0 && n_mine <= 32)) look_up(nx, 0);
         if (warp == kAttnWarps - 1) describe(nx.next, &segs[(it + 2) & 3]);
@@ -352,7 +422,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
                 const bool here = requested < n_mine;
                 const int k = here ? requested : requested - n_mine;
                 if ((k & 31) == 0) {
-                    const AttnSegment& of = here ? s : nx;
+                    const Segment& of = here ? s : nx;
                     const uint32_t none = place(of, k);
                     if (!here) none_after = none;
                     else if (k & 32) none_odd = none;
@@ -368,7 +438,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
                 requested -= i;
                 break;
             }
-            const bool no_page = (i & 32 ? none_odd : none_even) >> (i & 31) & 1;
+            const int block = KIND == kAttnListed ? where[warp * S + stage] : u;
+            const bool no_page = KIND == kAttnListed ? block < 0 : (i & 32 ? none_odd : none_even) >> (i & 31) & 1;
             const uint8_t* blk = ring + stage * kBlock;
             if (++stage == S) { stage = 0; parity ^= 1; }
 
@@ -400,8 +471,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
             }
             if (CAP) cap.on<CAP, 4>(x);
             // hidden tokens (only blocks that some column does not see whole, or without a page)
-            if ((uint32_t)(u - seen) >= (uint32_t)n_seen || no_page) {
-                const int j0 = u * 16;
+            if ((uint32_t)(block - seen) >= (uint32_t)n_seen || no_page) {
+                const int j0 = block * 16;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = j0 + g + 8 * (e >> 1);
@@ -492,6 +563,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
             if (s.slot >= 0) {
                 *reinterpret_cast<float4*>(part + e) = sum;
                 if (d == 0) { part[kAttnCols * D + col] = top * cc; part[kAttnCols * D + kAttnCols + col] = l; }
+            } else if (KIND == kAttnShared) {
+                const int i = r / p.group;
+                const int64_t row = attn_row(p, -1 - s.slot, s.t0 + i, s.head, r - i * p.group);
+                if (r < s.n_rows) {
+                    *reinterpret_cast<float4*>(p.row_o + row * D + d) = sum;
+                    if (d == 0) p.row_ml[row] = make_float2(top * cc, l);
+                }
             } else if (r < s.n_rows) {
                 const float inv = l > 0.f || l != l ? 1.f / l : 0.f;     // (no visible token: zeros)
                 const int i = r / p.group;
@@ -517,7 +595,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, D == 256 ? 1 : 2) paged_atten
 // Joins the parts of the segment that begins in a CTA's span and ends in another's, in a fixed order: CTA blockIdx.x's, 8 / W x R of its rows
 // per CTA.  W warps share a row's parts, 8 of them in flight each: one long sequence is many parts of few segments, and reading them one after
 // the other took as long as a fifth of the pass (131071 tokens, 8 KV heads of 128, 37 parts each: 52.8 -> 42.8 us for the call).
-template <int D, int ROWS, int R, int W>
+template <int D, int ROWS, int R, int W, AttnKind KIND = kAttnAll>
 __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnParams p)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -532,7 +610,9 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnParam
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = (blockIdx.y * (8 / W) + warp / W) * R, sub = warp % W;
     const int c0 = blockIdx.x, parts = split.w - c0 + 1;
     int t0;
-    const int n_rows = min(paged_rows(p.batch, split.x, &t0), p.max_q) * p.group;
+    int n_rows = p.group;
+    if (KIND == kAttnListed) t0 = split.x;                               // (a row's segment)
+    else n_rows = min(paged_rows(p.batch, split.x, &t0), p.max_q) * p.group;
     if (split.z * ROWS + blockIdx.y * (8 / W) * R >= n_rows) return;     // (the whole CTA; ROWS and the partial results hold the rows behind the last one)
     const auto part_of = [&](int c) { return p.partial + (2 * (c0 + c) + (c == 0 ? 1 : 0)) * kStride; };
     float m[R], l[R], acc[R][V];

@@ -1,0 +1,280 @@
+// Attention over the paged cache for sequences that share their beginning: the beginning of a group's sequences is one stretch of tokens that all rows of the group see whole, what follows it is a
+// stretch of each sequence's own.  Both are worked on by the kernels of paged_attention.cuh (few rows) and paged_tiles.cuh (many), whose softmax is one pass with (m, l, o), and joined here:
+//   o = sum_parts 2^(m_i - m) o_i / sum_parts 2^(m_i - m) l_i,   m = max m_i
+// So 64 sequences of one generated token and 4 query heads a KV head are one tile of 256 rows over the prefix, which is read and unpacked once instead of 64 times.
+//
+// The plan is a kernel of its own, one CTA: stretches, their lengths as the kernels number their segments, and each row's sequence, from the arrays on the device.  The length of a shared beginning is cut to a
+// multiple of 64 tokens (a step of the tiles) and to what all rows of the group see, so that nothing of it needs a mask; what is cut off belongs to what follows, from each sequence's own pages.
+#pragma once
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "paged.cuh"
+#include "paged_attention.cuh"
+#include "paged_tiles.cuh"
+
+namespace ql {
+
+constexpr int kSharedThreads = 1024, kMostStretches = QL_PAGED_MAX_SEQUENCES;
+constexpr int kStretchUnit = 64;
+constexpr int kMostPrefix = 1 << 30;                                     // (positions and rows add up below 2^31)
+
+struct SharedPlanParams {
+    PagedBatch batch;
+    const int32_t* group_start;
+    const int32_t* prefix_len;
+    int32_t n_groups, group, max_q, tile_rows;
+    bool prefix_tiles, own_tiles;
+    AttnStretch* stretches;      // [n_groups + B]
+    int32_t* lengths;            // [n_groups + B + 1]
+    int32_t* group_of;           // [B] the group whose beginning a sequence shares, -1: none
+    int32_t* row_seq;            // [T] the sequence of a served row, -1: none
+};
+
+template <int kRows>
+__device__ __forceinline__ int stretch_length(const AttnStretch& v, int group, bool tiles)
+{
+    if (!tiles) return v.blocks > 0 ? v.row_blocks * (v.blocks + kAttnOverhead) : 0;
+    const int n = (v.rows * group + kRows - 1) / kRows;
+    int end, sum = 0;
+    if (v.first == 0 && v.pos0 >= v.end - 1) return n * tile_length(stretch_steps<64, kRows>(v, 0, group, &end));   // (every row sees it whole)
+    for (int r = 0; r < n; ++r) sum += tile_length(stretch_steps<64, kRows>(v, r * kRows, group, &end));
+    return sum;
+}
+
+__global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const SharedPlanParams p)
+{
+    __shared__ int group_of[kMostStretches], prefix[kMostStretches], sums[32];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const PagedBatch& bt = p.batch;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = p.n_groups, V = G + bt.B;
+    const int64_t held = min((int64_t)bt.table_width << (bt.log2_blocks + 4), (int64_t)INT32_MAX);
+    for (int b = tid; b < bt.B; b += kSharedThreads) group_of[b] = -1;
+    for (int t = tid; t < bt.T; t += kSharedThreads) p.row_seq[t] = -1;
+    __syncthreads();
+    for (int g = warp; g < G; g += kSharedThreads / 32) {
+        const int s = p.group_start[g], e = p.group_start[g + 1];
+        const bool some = s >= 0 && e <= bt.B && (int64_t)e - s >= 2;
+        int64_t least = min(held, (int64_t)kMostPrefix);
+        int first = INT32_MAX;                                           // the first sequence with rows
+        bool ok = some;
+        for (int b = s + lane; some && b < e; b += 32) {
+            const int t0 = bt.q_start[b], t1 = bt.q_start[b + 1];
+            ok = ok && t0 >= 0 && t1 >= t0 && t1 <= bt.T;
+            if (t1 <= t0 || bt.kv_len[b] <= 0) continue;                 // (a request that is done keeps the others' beginning as it is)
+            first = min(first, b);
+            least = min(least, (int64_t)bt.kv_len[b] - ((int64_t)t1 - t0) + 1);   // what its first row sees
+        }
+        first = __reduce_min_sync(0xffffffffu, first);
+        int sees = __reduce_min_sync(0xffffffffu, (int)max(least, (int64_t)0));
+        ok = __all_sync(0xffffffffu, ok) && first != INT32_MAX;
+        sees = ok ? max(min(sees, p.prefix_len[g]), 0) / kStretchUnit * kStretchUnit : 0;
+        for (int b = s + lane; sees > 0 && b < e; b += 32)
+            if (bt.kv_len[b] > 0) atomicMax(&group_of[b], g);
+        if (lane == 0) {
+            prefix[g] = sees;
+            const int t0 = sees > 0 ? bt.q_start[s] : 0, rows = sees > 0 ? bt.q_start[e] - t0 : 0;
+            p.stretches[g] = AttnStretch{t0, rows, sees - 1, 0, sees, sees > 0 ? first : 0, sees / kPagedBlock, (rows * p.group + kAttnCols - 1) / kAttnCols};
+        }
+    }
+    __syncthreads();
+    int before = 0;
+    for (int v0 = 0; v0 < V; v0 += kSharedThreads) {
+        const int v = v0 + tid;
+        int n = 0;
+        if (v < V) {
+            AttnStretch st{};
+            if (v < G) st = p.stretches[v];                              // (written by this CTA, before its threads met)
+            else {
+                const int b = v - G, g = group_of[b], rows_all = paged_rows(bt, b, &st.t0), len = bt.kv_len[b];
+                p.group_of[b] = g;
+                st.rows = len > 0 ? min(rows_all, p.max_q) : 0;
+                st.first = g >= 0 ? prefix[g] : 0;
+                st.end = (int)held;
+                st.seq = b;
+                if (st.rows > 0) {
+                    st.pos0 = len - rows_all;
+                    const int end = (int)min((int64_t)st.pos0 + st.rows, held);
+                    st.blocks = max((int)(((unsigned)max(end, 0) + kPagedBlock - 1) / kPagedBlock) - st.first / kPagedBlock, 0);
+                    st.row_blocks = (st.rows * p.group + kAttnCols - 1) / kAttnCols;
+                }
+                for (int i = 0; i < min(rows_all, p.max_q); ++i) p.row_seq[st.t0 + i] = b;
+                p.stretches[v] = st;
+            }
+            const bool tiles = v < G ? p.prefix_tiles : p.own_tiles;
+            n = st.rows <= 0 ? 0 : p.tile_rows == 128 ? stretch_length<128>(st, p.group, tiles) : stretch_length<256>(st, p.group, tiles);
+        }
+        int run = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, run, o);
+            if (lane >= o) run += u;
+        }
+        __syncthreads();
+        if (lane == 31) sums[warp] = run;
+        __syncthreads();
+        int mine = sums[lane], all = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, all, o);
+            if (lane >= o) all += u;
+        }
+        run += before + __shfl_sync(0xffffffffu, all - mine, warp);
+        if (v < V) p.lengths[v + 1] = run;
+        before += __shfl_sync(0xffffffffu, all, 31);
+    }
+    if (tid == 0) p.lengths[0] = 0;
+}
+
+// One launch of a kernel over stretches, as the join finds its parts.
+struct SharedLaunch {
+    const float* partial;
+    int32_t v0, v1, grid;
+    bool tiles;
+};
+struct SharedJoinParams {
+    AttnStretch const* stretches;
+    const int32_t *lengths, *group_of, *row_seq;
+    const float* row_o;
+    const float2* row_ml;
+    __half* out;
+    int64_t out_ld;
+    int32_t T, h_q, group, h_kv, n_groups, tile_rows;
+    SharedLaunch prefix, own;
+};
+
+// The parts of a row in one of its stretches: n of them, part i with o at o + (i == 0 ? first : i * stride), and its m and l.
+struct SharedParts {
+    const float *first, *others;                                         // of part 0, and where part 1 would lie with the others' stride (their slots 0)
+    const float *ml_first, *ml_others;
+    int64_t stride;
+    int ml_step, n;                                                      // from m to l
+};
+template <int D>
+__device__ __forceinline__ SharedParts shared_parts(const SharedJoinParams& p, const SharedLaunch& at, int part, int v, int t, int head, int in_group)
+{
+    const AttnStretch st = p.stretches[v];
+    SharedParts r{};
+    const int row = (t - st.t0) * p.group + in_group, block_rows = at.tiles ? p.tile_rows : kAttnCols, block = row / block_rows;
+    int64_t begin = (int64_t)(p.lengths[v] - p.lengths[at.v0]) * p.h_kv;
+    int length, overhead = kAttnOverhead, end;
+    if (st.rows <= 0) return r;
+    if (at.tiles) {
+        overhead = kTileOverhead;
+        const auto steps = [&](int k) { return p.tile_rows == 128 ? stretch_steps<64, 128>(st, k * 128, p.group, &end) : stretch_steps<64, 256>(st, k * 256, p.group, &end); };
+        length = tile_length(steps(block));
+        if (length == 0) return r;
+        if (v < p.n_groups) begin += (int64_t)block * length * p.h_kv;
+        else for (int k = 0; k < block; ++k) begin += (int64_t)tile_length(steps(k)) * p.h_kv;
+        begin += (int64_t)head * length;
+    } else {
+        if (st.blocks == 0) return r;
+        length = st.blocks + kAttnOverhead;
+        begin += ((int64_t)head * st.row_blocks + block) * length;
+    }
+    const int64_t total = (int64_t)(p.lengths[at.v1] - p.lengths[at.v0]) * p.h_kv, span = max((total + at.grid - 1) / at.grid, (int64_t)(at.tiles ? 1 : kAttnSpan));
+    const int c0 = (int)((begin + overhead) / span), c1 = (int)((begin + length - 1) / span);   // the CTAs with something of it
+    r.n = c1 - c0 + 1;
+    if (r.n == 1) {
+        const int64_t at_row = ((int64_t)part * p.T + t) * p.h_q + head * p.group + in_group;
+        r.first = p.row_o + at_row * D;
+        r.ml_first = reinterpret_cast<const float*>(p.row_ml + at_row);
+        r.ml_step = 1;
+        return r;
+    }
+    r.stride = 2ll * block_rows * (D + 2);                               // (slots 0 of neighbouring CTAs; the first part lies in slot 1)
+    r.others = at.partial + c0 * r.stride + (row - block * block_rows) * D;
+    r.first = r.others + block_rows * (D + 2);
+    r.ml_others = at.partial + c0 * r.stride + block_rows * D + (row - block * block_rows);
+    r.ml_first = r.ml_others + block_rows * (D + 2);
+    r.ml_step = block_rows;
+    return r;
+}
+
+// A row of the call and a KV head per CTA; W of its 8 warps share a row's parts, in a fixed order.
+template <int D, int W>
+__global__ void __launch_bounds__(256) paged_shared_join_kernel(const SharedJoinParams p)
+{
+    constexpr int V = D / 32;
+    __shared__ __align__(16) float sums[8][D];
+    __shared__ float sums_l[8];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int t = blockIdx.x, head = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % W;
+    const int b = p.row_seq[t];
+    if (b < 0) return;
+    const int g = p.group_of[b];
+    for (int r0 = 0; r0 < p.group; r0 += 8 / W) {
+        const int r = r0 + warp / W;
+        float acc[V], l = 0.f, m = -1e30f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = 0.f;
+        if (r < p.group) {
+            SharedParts parts[2] = {};
+            if (g >= 0) parts[0] = shared_parts<D>(p, p.prefix, 0, g, t, head, r);
+            parts[1] = shared_parts<D>(p, p.own, 1, p.n_groups + b, t, head, r);
+            const int n = parts[0].n + parts[1].n;
+            const auto ml_of = [&](int i) {
+                const bool one = i >= parts[0].n;
+                const SharedParts& s = parts[one];
+                const int k = one ? i - parts[0].n : i;
+                return k == 0 ? s.ml_first : s.ml_others + k * s.stride;
+            };
+            const auto step_of = [&](int i) { return parts[i >= parts[0].n].ml_step; };
+            for (int i = lane; i < n; i += 32) m = fmaxf(m, *ml_of(i));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            for (int at = sub; at < n; at += 32 * W) {                   // 32 parts' weights side by side, then their values
+                const int mine = at + lane * W, here = min(32, (n - at + W - 1) / W);
+                float f = 0.f;
+                if (mine < n) {
+                    const float* ml = ml_of(mine);
+                    f = exp2_fast(ml[0] - m);
+                    l += ml[step_of(mine)] * f;
+                }
+#pragma unroll 8
+                for (int j = 0; j < here; ++j) {
+                    const int i = at + j * W;
+                    const bool one = i >= parts[0].n;
+                    const SharedParts& s = parts[one];
+                    const int k = one ? i - parts[0].n : i;
+                    const float* from = (k == 0 ? s.first : s.others + k * s.stride) + V * lane;
+                    const float fj = __shfl_sync(0xffffffffu, f, j);
+                    float y[V];
+                    if constexpr (V == 2) *reinterpret_cast<float2*>(y) = *reinterpret_cast<const float2*>(from);
+                    else
+#pragma unroll
+                        for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(y + e) = *reinterpret_cast<const float4*>(from + e);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] = fmaf(y[e], fj, acc[e]);
+                }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        }
+        if (W > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < V; ++e) sums[warp][e * 32 + lane] = acc[e];
+            if (lane == 0) sums_l[warp] = l;
+            __syncthreads();
+            if (sub == 0)
+#pragma unroll
+                for (int w = 1; w < W; ++w) {
+                    l += sums_l[warp + w];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] += sums[warp + w][e * 32 + lane];
+                }
+        }
+        if (sub == 0 && r < p.group) {
+            const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+            __half* to = p.out + (int64_t)t * p.out_ld + (int64_t)(head * p.group + r) * D + V * lane;
+#pragma unroll
+            for (int e = 0; e < V; e += 2) *reinterpret_cast<__half2*>(to + e) = __floats2half2_rn(acc[e] * inv, acc[e + 1] * inv);
+        }
+    }
+}
+
+}  // namespace ql

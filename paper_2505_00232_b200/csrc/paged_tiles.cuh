@@ -103,7 +103,18 @@ __device__ __forceinline__ int tile_steps(int row0, int n_rows, int rows_all, in
     return max(0, (int)(((unsigned)end + N - 1) / N) - *first);
 }
 
-template <int D, AttnCap CAP>
+// Steps of N keys that the rows [row0, row0 + kRows) of a stretch see, *end the keys that they see.
+template <int N, int kRows>
+__device__ __forceinline__ int stretch_steps(const AttnStretch& v, int row0, int group, int* end)
+{
+    const int n_rows = v.rows * group;
+    *end = 0;
+    if (row0 >= n_rows) return 0;
+    *end = min(v.pos0 + (min(row0 + kRows, n_rows) - 1) / group + 1, v.end);
+    return *end <= 0 ? 0 : max(0, (int)(((unsigned)*end + N - 1) / N) - v.first / N);
+}
+
+template <int D, AttnCap CAP, AttnKind KIND = kAttnAll>
 __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const PagedAttnParams p)
 {
     using T = TileShape<D>;
@@ -148,50 +159,55 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
 
     const PagedBatch& bt = p.batch;
     const int held = (int)min((int64_t)bt.table_width << (bt.log2_blocks + 4), (int64_t)INT32_MAX);
-    // ---- the plan: the length of every sequence, their sums
-    for (int b = warp; b < bt.B; b += kTileThreads / 32) {
-        int t0, first, sum = 0;
-        const int rows_all = paged_rows(bt, b, &t0), n_rows = min(rows_all, p.max_q) * p.group, len = bt.kv_len[b];
-        for (int r = lane; r * T::kRows < n_rows; r += 32) sum += tile_length(tile_steps<N, T::kRows>(r * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &first));
+    const int n_seqs = KIND == kAttnShared ? p.v1 - p.v0 : bt.B;
+    if constexpr (KIND == kAttnShared) {
+        for (int v = tid; v <= n_seqs; v += kTileThreads) pre[v] = p.lengths[p.v0 + v] - p.lengths[p.v0];
+    } else {
+        // ---- the plan: the length of every sequence, their sums
+        for (int b = warp; b < bt.B; b += kTileThreads / 32) {
+            int t0, first, sum = 0;
+            const int rows_all = paged_rows(bt, b, &t0), n_rows = min(rows_all, p.max_q) * p.group, len = bt.kv_len[b];
+            for (int r = lane; r * T::kRows < n_rows; r += 32) sum += tile_length(tile_steps<N, T::kRows>(r * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &first));
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) pre[b + 1] = sum;
-    }
-    if (tid == 0) pre[0] = 0;
-    __syncthreads();
-    if (warp == 0) {
-        int carry = 0;
-        for (int b0 = 0; b0 < bt.B; b0 += 32) {
-            int v = b0 + lane < bt.B ? pre[b0 + lane + 1] : 0;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int u = __shfl_up_sync(0xffffffffu, v, o);
-                if (lane >= o) v += u;
-            }
-            v += carry;
-            if (b0 + lane < bt.B) pre[b0 + lane + 1] = v;
-            carry = __shfl_sync(0xffffffffu, v, 31);
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == 0) pre[b + 1] = sum;
         }
-    }
-    // rows of row tiles that see nothing at all: zeros (there are none unless the first or the last row tile is one)
-    for (int b = blockIdx.x; b < bt.B; b += gridDim.x) {
-        int t0, first;
-        const int rows_all = paged_rows(bt, b, &t0), n_rows = min(rows_all, p.max_q) * p.group, len = bt.kv_len[b];
-        if (n_rows <= 0) continue;
-        const auto steps = [&](int row) { return tile_steps<N, T::kRows>(row / T::kRows * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &first); };
-        if (steps(0) > 0 && steps(n_rows - 1) > 0) continue;
-        for (int64_t e = tid; e < (int64_t)n_rows * bt.h_kv * (D / 8); e += kTileThreads) {
-            const int m = (int)(e % (D / 8)), row = (int)(e / (D / 8) % n_rows), head = (int)(e / (D / 8) / n_rows), i = row / p.group;
-            if (steps(row) == 0) *reinterpret_cast<uint4*>(p.out + (int64_t)(t0 + i) * p.out_ld + (int64_t)(head * p.group + row - i * p.group) * D + 8 * m) = make_uint4(0, 0, 0, 0);
+        if (tid == 0) pre[0] = 0;
+        __syncthreads();
+        if (warp == 0) {
+            int carry = 0;
+            for (int b0 = 0; b0 < bt.B; b0 += 32) {
+                int v = b0 + lane < bt.B ? pre[b0 + lane + 1] : 0;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int u = __shfl_up_sync(0xffffffffu, v, o);
+                    if (lane >= o) v += u;
+                }
+                v += carry;
+                if (b0 + lane < bt.B) pre[b0 + lane + 1] = v;
+                carry = __shfl_sync(0xffffffffu, v, 31);
+            }
+        }
+        // rows of row tiles that see nothing at all: zeros (there are none unless the first or the last row tile is one)
+        for (int b = blockIdx.x; b < bt.B; b += gridDim.x) {
+            int t0, first;
+            const int rows_all = paged_rows(bt, b, &t0), n_rows = min(rows_all, p.max_q) * p.group, len = bt.kv_len[b];
+            if (n_rows <= 0) continue;
+            const auto steps = [&](int row) { return tile_steps<N, T::kRows>(row / T::kRows * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &first); };
+            if (steps(0) > 0 && steps(n_rows - 1) > 0) continue;
+            for (int64_t e = tid; e < (int64_t)n_rows * bt.h_kv * (D / 8); e += kTileThreads) {
+                const int m = (int)(e % (D / 8)), row = (int)(e / (D / 8) % n_rows), head = (int)(e / (D / 8) / n_rows), i = row / p.group;
+                if (steps(row) == 0) *reinterpret_cast<uint4*>(p.out + (int64_t)(t0 + i) * p.out_ld + (int64_t)(head * p.group + row - i * p.group) * D + 8 * m) = make_uint4(0, 0, 0, 0);
+            }
         }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
-    const int64_t total = (int64_t)pre[bt.B] * bt.h_kv, span = max((total + p.grid - 1) / p.grid, (int64_t)1);
+    const int64_t total = (int64_t)pre[n_seqs] * bt.h_kv, span = max((total + p.grid - 1) / p.grid, (int64_t)1);
     const int64_t w_first = (int64_t)blockIdx.x * span, w_end = min(total, w_first + span);
-    if (tid == 16 * 32) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    if (KIND != kAttnShared && tid == 16 * 32) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
 
     // Rounds of at most kMaxSegments segments; every role has a loop of its own.
     struct Round { int64_t w; uint32_t it0, seg0, steps; int n; bool on; } rd{w_first, 0, 0, 0, 0, w_first < w_end};
@@ -346,7 +362,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                 if (!landed) { ok = false; break; }
                 tc_fence_after();
                 const float sum = (l[0].x + l[0].y) + (l[1].x + l[1].y);
-                if (s.slot < 0) {
+                if (KIND == kAttnShared && s.slot < 0) {
+                    const int64_t row = attn_row(p, -1 - s.slot, s.t0 + i, s.head, rr - i * p.group);
+#pragma unroll 1
+                    for (int d = 0; d < D; d += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(to + d, o);
+                        if (rr < s.n_rows)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) store32(p.row_o + row * D + d + 8 * e, o + 8 * e);
+                    }
+                    if (rr < s.n_rows) p.row_ml[row] = make_float2(m * cc, sum);
+                } else if (s.slot < 0) {
                     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
                     __half* dst = p.out + (int64_t)(s.t0 + i) * p.out_ld + (int64_t)(s.head * p.group + rr - i * p.group) * D;
 #pragma unroll 1
@@ -461,35 +488,45 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
             int n = 0;
             int64_t ww = rd.w;
             while (ww < w_end && n < T::kMaxSegments) {
-                int lo = 0, hi = bt.B;                                   // pre[lo] * h_kv <= ww < pre[hi] * h_kv
+                int lo = 0, hi = n_seqs;                                 // pre[lo] * h_kv <= ww < pre[hi] * h_kv
                 while (hi - lo > 1) {
                     const int mid = (lo + hi) >> 1;
                     if ((int64_t)pre[mid] * bt.h_kv <= ww) lo = mid;
                     else hi = mid;
                 }
-                int t0;
-                const int rows_all = paged_rows(bt, lo, &t0), n_rows = min(rows_all, p.max_q) * p.group, len = bt.kv_len[lo];
+                int t0, rows_all = 0, n_rows, len = 0, unused;
+                AttnStretch v;
+                if constexpr (KIND == kAttnShared) {
+                    v = p.stretches[p.v0 + lo];
+                    t0 = v.t0;
+                    n_rows = v.rows * p.group;
+                } else {
+                    rows_all = paged_rows(bt, lo, &t0);
+                    n_rows = min(rows_all, p.max_q) * p.group;
+                    len = bt.kv_len[lo];
+                }
                 int64_t local = ww - (int64_t)pre[lo] * bt.h_kv;
                 int r = 0, steps = 0, first = 0;
                 for (int r0 = 0;; r0 += 32) {                            // the row tile: sums over 32 at a time
                     int f;
-                    const int mine = tile_steps<N, T::kRows>((r0 + lane) * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &f);
-                    int v = tile_length(mine);
+                    const int mine = KIND == kAttnShared ? stretch_steps<N, T::kRows>(v, (r0 + lane) * T::kRows, p.group, &unused)
+                                                         : tile_steps<N, T::kRows>((r0 + lane) * T::kRows, n_rows, rows_all, len, held, p.group, p.window, &f);
+                    int run = tile_length(mine);
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
-                        const int u = __shfl_up_sync(0xffffffffu, v, o);
-                        if (lane >= o) v += u;
+                        const int u = __shfl_up_sync(0xffffffffu, run, o);
+                        if (lane >= o) run += u;
                     }
-                    const uint32_t beyond = __ballot_sync(0xffffffffu, (int64_t)v * bt.h_kv > local);
+                    const uint32_t beyond = __ballot_sync(0xffffffffu, (int64_t)run * bt.h_kv > local);
                     if (beyond) {
                         const int at = __ffs(beyond) - 1;
                         r = r0 + at;
                         steps = __shfl_sync(0xffffffffu, mine, at);
-                        first = __shfl_sync(0xffffffffu, f, at);
-                        local -= (int64_t)(__shfl_sync(0xffffffffu, v, at) - tile_length(steps)) * bt.h_kv;
+                        first = KIND == kAttnShared ? v.first / N : __shfl_sync(0xffffffffu, f, at);
+                        local -= (int64_t)(__shfl_sync(0xffffffffu, run, at) - tile_length(steps)) * bt.h_kv;
                         break;
                     }
-                    local -= (int64_t)__shfl_sync(0xffffffffu, v, 31) * bt.h_kv;
+                    local -= (int64_t)__shfl_sync(0xffffffffu, run, 31) * bt.h_kv;
                 }
                 const int length = tile_length(steps), head0 = (int)(local / length);
                 int ua = (int)(local - (int64_t)head0 * length);
@@ -497,7 +534,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     const int ub = (int)min((int64_t)length, ua + (w_end - ww)), sa = max(ua - kTileOverhead, 0), sb = max(ub - kTileOverhead, 0);
                     if (sb > sa) {
                         const bool whole = sa == 0 && sb == steps;
-                        if (lane == 0) {
+                        if (KIND == kAttnShared && lane == 0) {
+                            int end;
+                            stretch_steps<N, T::kRows>(v, r * T::kRows, p.group, &end);
+                            segs[n] = TileSegment{head, r * T::kRows, n_rows, t0, v.pos0, end, first + sa, sb - sa, whole ? (p.v0 + lo < p.n_groups ? -1 : -2) : sa > 0 ? 0 : 1, v.seq * bt.table_ld};
+                        } else if (lane == 0) {
                             segs[n] = TileSegment{head, r * T::kRows, n_rows, t0, len - rows_all, min(len - rows_all + (min((r + 1) * T::kRows, n_rows) - 1) / p.group + 1, held), first + sa, sb - sa, whole ? -1 : sa > 0 ? 0 : 1, lo * bt.table_ld};
                             if (sa == 0 && !whole) p.split[blockIdx.x] = make_int4(lo, head, r, (int)((ww - ua + length - 1) / span));
                         }
