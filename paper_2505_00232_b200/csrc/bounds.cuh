@@ -59,123 +59,121 @@ __device__ __forceinline__ int bounds_scan(int v, int* total, int* sums)
 }
 
 // A warp takes a page and KV head: in a block of 16 tokens lane 4 t + c has eight elements of each group of the tokens t and t + 8, so that the maxima over tokens are packed fp16
-// instructions on what it holds and three exchanges at the end.  Every CTA numbers the touched columns of the batch (a scan) and takes pages in turn.
-// Bound: HBM (the keys of the touched pages, once).
+// instructions on what it holds (the smallest as the largest of the negated: one operation for both), and at the end 8 lanes share the values out among them: each exchange halves what a lane goes on with (28
+// exchanges for 32 pairs, not 96), and a lane is left with elements in a row, which it encodes and stores.
+// Every CTA numbers the touched columns of the batch (a scan) and takes pages in turn, 32 of them looked up side by side.
+// Bound: HBM (the keys of the touched pages, once); for a generated token a sequence the chain length -> column -> page -> keys.
 template <int D>
-__global__ void __launch_bounds__(kBoundsThreads) paged_bounds_kernel(const PagedBoundsParams p)
+__global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : D == 128 ? 3 : 4) paged_bounds_kernel(const PagedBoundsParams p)
 {
-    constexpr int NB = D / 64, kBlock = paged_block_bytes(D);
-    extern __shared__ int pre[];                                         // [B + 1] touched columns before sequence b
+    constexpr int NB = D / 64, kBlock = paged_block_bytes(D), kPairs = 16 * NB;   // pairs of elements of a lane: largest and smallest
+    extern __shared__ int pre[];                                         // [B + 1] touched columns before sequence b, [B] the first of them
     __shared__ int sums[kBoundsWarps];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const PagedBatch& bt = p.batch;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t = lane >> 2, c = lane & 3, log2_page = bt.log2_blocks + 4;
+    int* first_of = pre + bt.B + 1;
     int total = 0;
     if (tid == 0) pre[0] = 0;
     for (int b0 = 0; b0 < bt.B; b0 += kBoundsThreads) {
         const int b = b0 + tid;
-        int first, all;
+        int first = 0, all;
         const int n = b < bt.B ? touched_columns(bt, b, &first) : 0, before = bounds_scan(n, &all, sums);
-        if (b < bt.B) pre[b + 1] = total + before + n;
+        if (b < bt.B) { pre[b + 1] = total + before + n; first_of[b] = first; }
         total += all;
     }
     __syncthreads();
-    for (int64_t item = (int64_t)blockIdx.x * kBoundsWarps + warp; item < (int64_t)total * bt.h_kv; item += (int64_t)gridDim.x * kBoundsWarps) {
-        const int k = (int)(item / bt.h_kv), head = (int)(item - (int64_t)k * bt.h_kv);
-        int b = 0, hi_b = bt.B;                                          // pre[b] <= k < pre[hi_b]
-        while (hi_b - b > 1) {
-            const int mid = (b + hi_b) >> 1;
-            if (pre[mid] <= k) b = mid;
-            else hi_b = mid;
+    const int mine = total > (int)blockIdx.x ? (total - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;   // pages of this CTA: blockIdx.x, + gridDim.x, ...
+    for (int base = 0; base < mine; base += 32) {
+        int page_of = -1, tokens_of = 0;                                 // of page base + lane
+        if (base + lane < mine) {
+            const int k = (int)blockIdx.x + (base + lane) * (int)gridDim.x;
+            int b = 0, hi_b = bt.B;                                      // pre[b] <= k < pre[hi_b]
+            while (hi_b - b > 1) {
+                const int mid = (b + hi_b) >> 1;
+                if (pre[mid] <= k) b = mid;
+                else hi_b = mid;
+            }
+            const int column = first_of[b] + k - pre[b];
+            page_of = bt.table[b * bt.table_ld + column];
+            tokens_of = (int)min((int64_t)bt.kv_len[b] - ((int64_t)column << log2_page), (int64_t)1 << log2_page);
         }
-        int first;
-        touched_columns(bt, b, &first);
-        const int column = first + k - pre[b], page = bt.table[b * bt.table_ld + column];
-        if (page < 0 || page >= bt.n_pages) continue;
-        const int tokens = (int)min((int64_t)bt.kv_len[b] - ((int64_t)column << log2_page), (int64_t)1 << log2_page);
-        const uint8_t* blk = bt.pool + (((int64_t)page * bt.h_kv + head) << bt.log2_blocks) * kBlock;
-        const uint32_t kMinusInf = 0xfc00fc00u, kPlusInf = 0x7c007c00u;
-        uint32_t top[NB][2][4], low[NB][2][4];                           // two elements each
+        const int tasks = min(32, mine - base) * bt.h_kv;
+        for (int task = warp; task < tasks; task += kBoundsWarps) {
+            const int at = task / bt.h_kv, head = task - at * bt.h_kv, page = __shfl_sync(0xffffffffu, page_of, at), tokens = __shfl_sync(0xffffffffu, tokens_of, at);
+            if (page < 0 || page >= bt.n_pages) continue;
+            const uint8_t* blk = bt.pool + (((int64_t)page * bt.h_kv + head) << bt.log2_blocks) * kBlock;
+            uint32_t top[kPairs];                                        // pairs 4 (4 j + 2 e + s) ..: panel j, group e, s: of the negated
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { top[j][e][i] = kMinusInf; low[j][e][i] = kPlusInf; }
-        const auto take = [&](uint32_t word, uint32_t scale, uint32_t* hi, uint32_t* lo) {
-            uint32_t h[4];
-            unpack_int4_word(word, h);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t v = h2_mul(h[i], scale);
-                const __half2 x = *reinterpret_cast<const __half2*>(&v);
-                const __half2 m = __hmax2(*reinterpret_cast<__half2*>(hi + i), x), n = __hmin2(*reinterpret_cast<__half2*>(lo + i), x);
-                hi[i] = *reinterpret_cast<const uint32_t*>(&m);
-                lo[i] = *reinterpret_cast<const uint32_t*>(&n);
-            }
-        };
-#pragma unroll 2
-        for (int t0 = 0; t0 < tokens; t0 += kPagedBlock, blk += kBlock) {
-            uint4 kw[NB];
-            uint2 ks[NB];
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                kw[j] = *reinterpret_cast<const uint4*>(blk + 512 * j + 16 * lane);
-                ks[j] = *reinterpret_cast<const uint2*>(blk + paged_k_scales(D) + t * (8 * NB) + 8 * j);
-            }
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                if (t0 + t < tokens) {
-                    take(kw[j].x, __byte_perm(ks[j].x, ks[j].x, 0x1010), top[j][0], low[j][0]);
-                    take(kw[j].y, __byte_perm(ks[j].y, ks[j].y, 0x1010), top[j][1], low[j][1]);
-                }
-                if (t0 + t + 8 < tokens) {
-                    take(kw[j].z, __byte_perm(ks[j].x, ks[j].x, 0x3232), top[j][0], low[j][0]);
-                    take(kw[j].w, __byte_perm(ks[j].y, ks[j].y, 0x3232), top[j][1], low[j][1]);
-                }
-            }
-        }
-        float most = 0.f;
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
+            for (int i = 0; i < kPairs; ++i) top[i] = 0xfc00fc00u;       // (-infinity)
+            const auto take = [&](uint32_t word, uint32_t scale, uint32_t* to) {
+                uint32_t h[4];
+                unpack_int4_word(word, h);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    __half2 m = *reinterpret_cast<__half2*>(&top[j][e][i]), n = *reinterpret_cast<__half2*>(&low[j][e][i]);
-#pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) {
-                        m = __hmax2(m, __shfl_xor_sync(0xffffffffu, m, o));
-                        n = __hmin2(n, __shfl_xor_sync(0xffffffffu, n, o));
-                    }
-                    top[j][e][i] = *reinterpret_cast<const uint32_t*>(&m);
-                    low[j][e][i] = *reinterpret_cast<const uint32_t*>(&n);
-                    most = fmaxf(most, fmaxf(fmaxf(__low2float(m), __high2float(m)), -fminf(__low2float(n), __high2float(n))));
+                    const uint32_t v = h2_mul(h[i], scale), w = v ^ 0x80008000u;
+                    const __half2 a = __hmax2(*reinterpret_cast<const __half2*>(to + i), *reinterpret_cast<const __half2*>(&v)), b = __hmax2(*reinterpret_cast<const __half2*>(to + 4 + i), *reinterpret_cast<const __half2*>(&w));
+                    to[i] = *reinterpret_cast<const uint32_t*>(&a);
+                    to[4 + i] = *reinterpret_cast<const uint32_t*>(&b);
                 }
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        const float r = most > 0.f ? __fdiv_rn(127.f, most) : 0.f;
-        int8_t* to = p.bounds + ((int64_t)page * bt.h_kv + head) * (2 * D);
-        // eight elements of a group by one lane each: the lane with t = 4 j + 2 e + (smallest), in turn where there are more of them
+            };
+#pragma unroll 2
+            for (int t0 = 0; t0 < tokens; t0 += kPagedBlock, blk += kBlock) {
+                uint4 kw[NB];
+                uint2 ks[NB];
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
+                for (int j = 0; j < NB; ++j) {
+                    kw[j] = *reinterpret_cast<const uint4*>(blk + 512 * j + 16 * lane);
+                    ks[j] = *reinterpret_cast<const uint2*>(blk + paged_k_scales(D) + t * (8 * NB) + 8 * j);
+                }
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-                    if (t == ((4 * j + 2 * e + s) & 7)) {
-                        uint32_t w[2] = {0, 0};
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const __half2 two = *reinterpret_cast<const __half2*>(s ? &low[j][e][i >> 1] : &top[j][e][i >> 1]);
-                            const float v = __fmul_rn(i & 1 ? __high2float(two) : __low2float(two), r);
-                            const int code = s ? max(__float2int_rd(v), -127) : min(__float2int_ru(v), 127);
-                            w[i >> 2] |= ((uint32_t)code & 255u) << (8 * (i & 3));
-                        }
-                        *reinterpret_cast<uint2*>(to + s * D + 64 * j + 32 * e + 8 * c) = make_uint2(w[0], w[1]);
+                for (int j = 0; j < NB; ++j) {
+                    if (t0 + t < tokens) {
+                        take(kw[j].x, __byte_perm(ks[j].x, ks[j].x, 0x1010), top + 16 * j);
+                        take(kw[j].y, __byte_perm(ks[j].y, ks[j].y, 0x1010), top + 16 * j + 8);
                     }
-        if (lane == 0) p.scales[(int64_t)page * bt.h_kv + head] = __fdiv_rn(most, 127.f);
+                    if (t0 + t + 8 < tokens) {
+                        take(kw[j].z, __byte_perm(ks[j].x, ks[j].x, 0x3232), top + 16 * j);
+                        take(kw[j].w, __byte_perm(ks[j].y, ks[j].y, 0x3232), top + 16 * j + 8);
+                    }
+                }
+            }
+            // the lane with t keeps the pairs kPairs / 8 * t ..
+            int held = kPairs;
+#pragma unroll
+            for (int o = 16; o >= 4; o >>= 1) {
+                held >>= 1;
+#pragma unroll
+                for (int i = 0; i < kPairs / 2; ++i) {
+                    if (i >= held) break;
+                    const bool high = lane & o;
+                    const uint32_t send = high ? top[i] : top[i + held], keep = high ? top[i + held] : top[i], got = __shfl_xor_sync(0xffffffffu, send, o);
+                    const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&keep), *reinterpret_cast<const __half2*>(&got));
+                    top[i] = *reinterpret_cast<const uint32_t*>(&m);
+                }
+            }
+            float most = 0.f;
+#pragma unroll
+            for (int i = 0; i < kPairs / 8; ++i) most = fmaxf(most, fmaxf(__low2float(*reinterpret_cast<const __half2*>(top + i)), __high2float(*reinterpret_cast<const __half2*>(top + i))));
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            const float r = most > 0.f ? __fdiv_rn(127.f, most) : 0.f;
+            int8_t* to = p.bounds + ((int64_t)page * bt.h_kv + head) * (2 * D);
+#pragma unroll
+            for (int i0 = 0; i0 < kPairs / 8; i0 += 2) {                 // four elements to a store
+                const int pair = kPairs / 8 * t + i0, j = pair >> 4, e = pair >> 3 & 1, s = pair >> 2 & 1;
+                uint32_t w = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const __half2 two = *reinterpret_cast<const __half2*>(top + i0 + (i >> 1));
+                    const int code = min(__float2int_ru(__fmul_rn(i & 1 ? __high2float(two) : __low2float(two), r)), 127);   // (the negated is rounded up: its negative down)
+                    w |= ((uint32_t)(s ? -code : code) & 255u) << (8 * i);
+                }
+                *reinterpret_cast<uint32_t*>(to + s * D + 64 * j + 32 * e + 8 * c + 2 * (pair & 3)) = w;
+            }
+            if (lane == 0) p.scales[(int64_t)page * bt.h_kv + head] = __fdiv_rn(most, 127.f);
+        }
     }
 }
 
@@ -187,6 +185,7 @@ struct PagedSelectParams {
     int32_t* pages;              // [T, h_kv, budget]
     int64_t q_ld;
     int32_t group, budget, first, recent, share;                         // share: columns of a CTA at most
+    bool gathered;               // the first CTA of a cluster has room for every column's key
 };
 constexpr int kSelectMostColumns = 1 << 18;
 
@@ -206,40 +205,73 @@ __device__ __forceinline__ int cluster_load(const int* p, uint32_t rank)
     return v;
 }
 
-// The pages of a row and KV head by a cluster, each CTA with a contiguous share of the columns: scores as ordered 32-bit keys in shared memory, the budget-th largest of them digit by digit
-// (8 bits, histograms summed through distributed shared memory), then the columns above it, and of those equal to it the first, written down in order.
-// Bound: the chain length -> page -> bounds -> four digits, about 6 us; for many rows the bytes of the bounds (2 d + 4 a page and KV head).
-template <int D>
-__global__ void __launch_bounds__(kBoundsThreads) paged_select_kernel(const PagedSelectParams p)
+constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectGathered = 40 << 10;                                // columns whose keys one CTA holds
+
+__device__ __forceinline__ void cluster_store(uint32_t* p, uint32_t rank, uint32_t v)
 {
-    constexpr int kLanes = D / 8, kPer = 32 / (kLanes < 32 ? kLanes : 32);   // lanes of a page's 2 D bytes, 16 each; pages at once
-    static_assert(kLanes <= 32, "");
-    extern __shared__ uint32_t keys[];                                   // [share]
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+}
+// Exclusive sum over the CTA's kSelectThreads threads, the whole sum in *total.
+__device__ __forceinline__ int select_scan(int v, int* total, int* sums)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int run = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += u;
+    }
+    __syncthreads();
+    if (lane == 31) sums[warp] = run;
+    __syncthreads();
+    const int mine = lane < kSelectWarps ? sums[lane] : 0;
+    *total = (int)__reduce_add_sync(0xffffffffu, (unsigned)mine);
+    return run - v + (int)__reduce_add_sync(0xffffffffu, lane < warp ? (unsigned)mine : 0u);
+}
+
+// The pages of a row and KV head by a cluster.  Each CTA scores a contiguous share of the columns, a warp 32 of them at a time: D / 8 lanes read a page's 2 D bytes, the loads of 8 turns in flight before any is used, and
+// the eight sums of a lane are added over those lanes by halves (each lane keeps the half of the sums that is its own: 8 exchanges for 8 sums, not 8 times log2 of the lanes).  Scores become ordered 32-bit keys in
+// the shared memory of the cluster's first CTA, which finds the budget-th largest digit by digit (8 bits, from the highest bit in which keys differ; rarely more than two rounds) and writes the columns down in order.  Tables
+// too wide for one CTA's shared memory (40960 columns) leave the keys where they are: the CTAs add their histograms through distributed shared memory.
+// Bound: the chain length -> page -> bounds -> meeting -> digits; for many rows the bytes of the bounds (2 d + 4 a page and KV head).
+template <int D>
+__global__ void __launch_bounds__(kSelectThreads, 2) paged_select_kernel(const PagedSelectParams p)
+{
+    constexpr int kLanes = D / 8, kPer = 32 / kLanes, kTurns = 8;        // lanes of a page's 2 D bytes, 16 each; pages at once; loads in flight
+    extern __shared__ uint32_t keys[];                                   // [share], or every column's
     __shared__ __align__(16) int16_t codes[2 * D];
-    __shared__ int hist[2][256], counts[4], sums[kBoundsWarps], found_digit, found_left, found_seq;
-    __shared__ float most[kBoundsWarps];
+    __shared__ int hist[2][256], counts[4], sums[kSelectWarps], found_digit, found_left, found_count, found_seq;
+    __shared__ uint32_t range[2];                                        // the complement of the smallest key, the largest
+    __shared__ float most[kSelectWarps];
     const PagedBatch& bt = p.batch;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, log2_page = bt.log2_blocks + 4;
     const uint32_t rank = cluster_rank(), size = cluster_size();
     const int t = (int)(blockIdx.x / size), head = blockIdx.y;
-    if (tid == 0) found_seq = -1;
+    if (tid == 0) { found_seq = -1; range[0] = range[1] = 0; }
+    if (tid < 4) counts[tid] = 0;
+    if (tid < 256) hist[0][tid] = hist[1][tid] = 0;
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (a CTA's shared memory is written by others once it has started)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __syncthreads();
-    for (int b = tid; b < bt.B; b += kBoundsThreads) {
-        int first;
-        const int rows = paged_rows(bt, b, &first);
-        if (t >= first && t < first + rows) atomicMax(&found_seq, b);    // (the same for every CTA of the cluster, whatever q_start holds: they meet)
-    }
-    // ---- the sums over the heads, in whole numbers
+    // ---- the sums over the heads, in whole numbers; the row's sequence
     float above = 0.f, below = 0.f;
     if (tid < D) {
         const __half* q = p.q + t * p.q_ld + (int64_t)head * p.group * D + tid;
+#pragma unroll 4
         for (int h = 0; h < p.group; ++h) {
             const float x = __half2float(q[(int64_t)h * D]);
             above = __fadd_rn(above, fmaxf(x, 0.f));
             below = __fadd_rn(below, fminf(x, 0.f));
         }
+    }
+    for (int b = tid; b < bt.B; b += kSelectThreads) {
+        int first;
+        const int rows = paged_rows(bt, b, &first);
+        if (t >= first && t < first + rows) atomicMax(&found_seq, b);    // (the same for every CTA of the cluster, whatever q_start holds: they meet)
     }
     float m = fmaxf(above, -below);
 #pragma unroll
@@ -247,124 +279,204 @@ __global__ void __launch_bounds__(kBoundsThreads) paged_select_kernel(const Page
     if (lane == 0) most[warp] = m;
     __syncthreads();
     const int seq = found_seq;
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (seq < 0) return;                                                 // (a row of no sequence: the whole cluster leaves)
     int t0;
     const int rows_all = paged_rows(bt, seq, &t0), pos = (int)max((int64_t)bt.kv_len[seq] - rows_all + (t - t0), (int64_t)-1);
     m = 0.f;
 #pragma unroll
-    for (int w = 0; w < kBoundsWarps; ++w) m = fmaxf(m, most[w]);
+    for (int w = 0; w < D / 32; ++w) m = fmaxf(m, most[w]);
     const float r = m > 0.f ? __fdiv_rn(32767.f, m) : 0.f;
     if (tid < D) {
         codes[tid] = (int16_t)max(min(__float2int_rn(__fmul_rn(above, r)), 32767), -32767);
         codes[D + tid] = (int16_t)max(min(__float2int_rn(__fmul_rn(below, r)), 32767), -32767);
     }
-    hist[0][tid] = hist[1][tid] = 0;
-    if (tid < 4) counts[tid] = 0;
     __syncthreads();
 
     // ---- the keys of this CTA's columns: 0 for those that are no candidates, the largest number for those that are always taken
     const int last = pos < 0 ? -1 : min(pos >> log2_page, bt.table_width - 1), columns = last + 1;
-    const int share = (columns + (int)size - 1) / (int)size, lo = min((int)rank * share, columns), n = min(columns - lo, share);   // (share <= p.share: table_width / size rounded up)
+    const int share = (columns + (int)size - 1) / (int)size, begin = min((int)rank * share, columns), n_mine = min(columns - begin, share);   // (share <= p.share: table_width / size rounded up)
     const bool all = columns <= p.budget;                                // (no scores needed)
-    int4 q[2];
-    q[0] = reinterpret_cast<const int4*>(codes)[2 * (lane % kLanes)];
-    q[1] = reinterpret_cast<const int4*>(codes)[2 * (lane % kLanes) + 1];
-    const int8_t* from = p.bounds + 16 * (lane % kLanes);
-    int candidates = 0;
-    for (int w0 = warp * 32; w0 < n; w0 += kBoundsWarps * 32) {
-        const int at = w0 + lane, column = lo + at;
-        int page = at < n ? bt.table[seq * bt.table_ld + column] : -1;
-        const bool ok = page >= 0 && page < bt.n_pages, always = column < p.first || column > last - p.recent;
-        uint32_t key = ok ? 0xffffffffu : 0u;
-        if (!all) {
-            const int64_t mine = ((int64_t)(ok ? page : 0) * bt.h_kv + head);
-            const float scale = ok && !always ? p.scales[mine] : 0.f;
-            int sum = 0;
-#pragma unroll 8
-            for (int i = 0; i < 32; i += kPer) {
-                const int src = i + lane / kLanes;
-                const int64_t record = __shfl_sync(0xffffffffu, mine, src);
-                const uint4 u = *reinterpret_cast<const uint4*>(from + record * (2 * D));
-                int s = 0;
-                s = __dp2a_lo(q[0].x, (int)u.x, s); s = __dp2a_hi(q[0].y, (int)u.x, s);
-                s = __dp2a_lo(q[0].z, (int)u.y, s); s = __dp2a_hi(q[0].w, (int)u.y, s);
-                s = __dp2a_lo(q[1].x, (int)u.z, s); s = __dp2a_hi(q[1].y, (int)u.z, s);
-                s = __dp2a_lo(q[1].z, (int)u.w, s); s = __dp2a_hi(q[1].w, (int)u.w, s);
+    const int sub = lane % kLanes, turn = (sub & kLanes / 2 ? 4 : 0) + (sub & kLanes / 4 ? 2 : 0) + (sub & kLanes / 8 ? 1 : 0);
+    const int4 q0 = reinterpret_cast<const int4*>(codes)[2 * sub], q1 = reinterpret_cast<const int4*>(codes)[2 * sub + 1];
+    const int8_t* from = p.bounds + 16 * sub;
+    const auto put = [&](int at, uint32_t key) {
+        if (p.gathered && size > 1) cluster_store(keys + begin + at, 0, key);
+        else keys[at] = key;
+    };
+    for (int w0 = warp * 32; w0 < n_mine; w0 += kSelectThreads) {
+        const int at = w0 + lane, column = begin + at;
+        const int page = at < n_mine ? bt.table[seq * bt.table_ld + column] : -1;
+        const bool ok = page >= 0 && page < bt.n_pages, always = all || column < p.first || column > last - p.recent;
+        if (at < n_mine && (!ok || always)) put(at, ok ? 0xffffffffu : 0u);
+        if (all) continue;
+        const int64_t mine = (int64_t)(ok ? page : 0) * bt.h_kv + head;
+        const bool scored = ok && !always;
+        const float scale = scored ? p.scales[mine] : -1.f;
+#pragma unroll 1
+        for (int i0 = 0; i0 < 32; i0 += kTurns * kPer) {
+            uint4 u[kTurns];
 #pragma unroll
-                for (int o = 1; o < kLanes; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                s = __shfl_sync(0xffffffffu, s, (lane % kPer) * kLanes);
-                if (lane / kPer == i / kPer) sum = s;
+            for (int k = 0; k < kTurns; ++k) {
+                const int64_t record = __shfl_sync(0xffffffffu, mine, i0 + k * kPer + lane / kLanes);
+                u[k] = *reinterpret_cast<const uint4*>(from + record * (2 * D));
             }
-            if (ok && !always) {
-                const uint32_t bits = __float_as_uint(__fmul_rn(__int2float_rn(sum), scale) + 0.f);   // (-0 becomes 0: equal scores have equal keys)
-                key = bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+            int s[kTurns];
+#pragma unroll
+            for (int k = 0; k < kTurns; ++k) {
+                s[k] = __dp2a_lo(q0.x, (int)u[k].x, 0);
+                s[k] = __dp2a_hi(q0.y, (int)u[k].x, s[k]);
+                s[k] = __dp2a_lo(q0.z, (int)u[k].y, s[k]); s[k] = __dp2a_hi(q0.w, (int)u[k].y, s[k]);
+                s[k] = __dp2a_lo(q1.x, (int)u[k].z, s[k]); s[k] = __dp2a_hi(q1.y, (int)u[k].z, s[k]);
+                s[k] = __dp2a_lo(q1.z, (int)u[k].w, s[k]); s[k] = __dp2a_hi(q1.w, (int)u[k].w, s[k]);
+            }
+            int held = kTurns;
+#pragma unroll
+            for (int o = kLanes / 2; o >= kLanes / 8; o >>= 1) {         // this lane's half of the sums stays
+                held >>= 1;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k >= held) break;
+                    const bool high = sub & o;
+                    const int send = high ? s[k] : s[k + held], keep = high ? s[k + held] : s[k];
+                    s[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+                }
+            }
+#pragma unroll
+            for (int o = kLanes / 16; o >= 1; o >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
+            const int src = i0 + turn * kPer + lane / kLanes;            // the column (of the 32) whose sum this lane has
+            const float unit = __shfl_sync(0xffffffffu, scale, src);
+            if (unit >= 0.f && sub % (kLanes / 8) == 0) {
+                const uint32_t bits = __float_as_uint(__fadd_rn(__fmul_rn(__int2float_rn(s[0]), unit), 0.f));   // (-0 becomes 0: equal scores have equal keys)
+                put(w0 + src, bits & 0x80000000u ? ~bits : bits | 0x80000000u);
             }
         }
-        if (at < n) keys[at] = key;
+    }
+
+    // ---- who looks for the threshold: the first CTA, which has every key, or, where they do not fit, the cluster
+    const bool together = !p.gathered && size > 1;
+    int n = n_mine, lo = begin;
+    if (p.gathered && size > 1) {
+        cluster_meet();
+        if (rank > 0) return;
+        n = columns;
+        lo = 0;
+    }
+    const uint32_t parts = together ? size : 1;
+    const auto meet = [&]() {
+        if (together) cluster_meet();
+        else __syncthreads();
+    };
+    const auto sum_of = [&](const int* v) {                              // over the parts
+        if (!together) return *v;
+        int x[8], sum = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) x[k] = k < parts ? cluster_load(v, k) : 0;
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) sum += x[k];
+        return sum;
+    };
+    __syncthreads();
+    uint32_t least = 0, largest = 0;                                     // (of the complements; of the keys)
+    int candidates = 0, always = 0;
+    for (int i = tid; i < n; i += kSelectThreads) {
+        const uint32_t key = keys[i];
         candidates += key != 0;
+        always += key == 0xffffffffu;
+        if (key == 0 || key == 0xffffffffu) continue;
+        least = max(least, ~key);
+        largest = max(largest, key);
     }
     candidates = __reduce_add_sync(0xffffffffu, candidates);
-    if (lane == 0) atomicAdd(&counts[0], candidates);
-    __syncthreads();
+    always = __reduce_add_sync(0xffffffffu, always);
+    least = __reduce_max_sync(0xffffffffu, least);
+    largest = __reduce_max_sync(0xffffffffu, largest);
+    if (lane == 0) {
+        atomicAdd(&counts[0], candidates);
+        atomicAdd(&counts[1], always);
+        atomicMax(&range[0], least);
+        atomicMax(&range[1], largest);
+    }
+    meet();
+    candidates = sum_of(&counts[0]);
+    always = sum_of(&counts[1]);
+    least = range[0];
+    largest = range[1];
+    if (together)
+        for (uint32_t k = 0; k < parts; ++k) {
+            least = max(least, (uint32_t)cluster_load(reinterpret_cast<const int*>(&range[0]), k));
+            largest = max(largest, (uint32_t)cluster_load(reinterpret_cast<const int*>(&range[1]), k));
+        }
 
     // ---- the threshold: every key above it is taken, and `left` of those that equal it
     uint32_t threshold = 0;
     int left = 0;
-    if (!all) {
-        uint32_t prefix = 0;
-        for (int digit = 0; digit < 4; ++digit) {
-            int* h = hist[digit & 1];
-            const int shift = 24 - 8 * digit;
-            for (int i = tid; i < n; i += kBoundsThreads) {
+    if (candidates > p.budget) {
+        const uint32_t base = ~least;
+        left = p.budget - always;                                        // (of first + recent <= budget columns)
+        uint32_t prefix = 0;                                             // of key - base
+        int shift = 32 - __clz(largest - base), bits = 0;
+        threshold = left > 0 ? base : 0xfffffffeu;                       // (left 0: those that are always taken are the budget; all keys equal: no rounds)
+        for (int round = 0; left > 0 && shift > 0; ++round) {
+            bits = min(shift, 8);
+            shift -= bits;
+            int* h = hist[round & 1];
+            for (int i = tid; i < n; i += kSelectThreads) {
                 const uint32_t key = keys[i];
-                if (key != 0 && (digit == 0 || key >> (shift + 8) == prefix)) atomicAdd(&h[key >> shift & 255], 1);
+                if (key == 0 || key == 0xffffffffu) continue;
+                const uint32_t x = (key - base) >> shift;
+                if (round == 0 || x >> bits == prefix) atomicAdd(&h[x & ((1u << bits) - 1)], 1);
             }
-            cluster_meet();
-            int sum = 0, total = 0;
-            for (uint32_t k = 0; k < size; ++k) sum += cluster_load(&h[255 - tid], k);   // (thread 0: the largest digit)
-            if (digit == 0) for (uint32_t k = 0; k < size; ++k) total += cluster_load(&counts[0], k);
-            if (digit == 0) left = min(p.budget, total);
-            if (digit == 0 && total <= p.budget) { left = 0; break; }    // (every candidate; the whole cluster agrees)
+            meet();
+            const int sum = tid < 256 ? sum_of(&h[255 - tid]) : 0;       // (thread 0: the largest digit)
             int every;
-            const int before = bounds_scan(sum, &every, sums);
-            if (before < left && before + sum >= left) { found_digit = 255 - tid; found_left = left - before; }
-            hist[(digit + 1) & 1][tid] = 0;                              // (its readers are past the meeting above)
+            const int before = select_scan(sum, &every, sums);
+            if (before < left && before + sum >= left) { found_digit = 255 - tid; found_left = left - before; found_count = sum; }
+            if (tid < 256) hist[(round + 1) & 1][tid] = 0;               // (its readers are past the meeting above)
             __syncthreads();
-            prefix = prefix << 8 | (uint32_t)found_digit;
+            prefix = prefix << bits | (uint32_t)found_digit;
             left = found_left;
+            threshold = base + (prefix << shift);
+            if (left == found_count) {                                   // all of this digit: no need to tell them apart
+                threshold -= 1;
+                left = 0;
+                break;
+            }
         }
-        threshold = prefix;
     }
 
     // ---- the columns, in order: where this CTA's begin
     int over = 0, equal = 0;
-    const int per = (n + kBoundsThreads - 1) / kBoundsThreads, i0 = min(tid * per, n), i1 = min(i0 + per, n);
+    const int per = (n + kSelectThreads - 1) / kSelectThreads, i0 = min(tid * per, n), i1 = min(i0 + per, n);
     for (int i = i0; i < i1; ++i) {
         over += keys[i] > threshold;
-        equal += threshold != 0 && keys[i] == threshold;
+        equal += left > 0 && keys[i] == threshold;
     }
     int all_over, all_equal;
-    int over_at = bounds_scan(over, &all_over, sums), equal_at = bounds_scan(equal, &all_equal, sums);
-    if (tid == 0) { counts[1] = all_over; counts[2] = all_equal; }
-    cluster_meet();
-    int over_before = 0, equal_before = 0, over_all = 0, equal_all = 0;
-    for (uint32_t k = 0; k < size; ++k) {
-        const int a = cluster_load(&counts[1], k), b = cluster_load(&counts[2], k);
-        if (k < rank) { over_before += a; equal_before += b; }
-        over_all += a;
-        equal_all += b;
+    int over_at = select_scan(over, &all_over, sums), equal_at = select_scan(equal, &all_equal, sums);
+    int over_all = all_over, equal_all = all_equal;
+    if (together) {
+        if (tid == 0) { counts[2] = all_over; counts[3] = all_equal; }
+        cluster_meet();
+        over_all = equal_all = 0;
+        for (uint32_t k = 0; k < parts; ++k) {
+            const int a = cluster_load(&counts[2], k), b = cluster_load(&counts[3], k);
+            if (k < rank) { over_at += a; equal_at += b; }
+            over_all += a;
+            equal_all += b;
+        }
     }
-    over_at += over_before;
-    equal_at += equal_before;
     int32_t* to = p.pages + ((int64_t)t * bt.h_kv + head) * p.budget;
     for (int i = i0; i < i1; ++i) {
-        const bool is_over = keys[i] > threshold, is_equal = threshold != 0 && keys[i] == threshold;
+        const uint32_t key = keys[i];
+        const bool is_over = key > threshold, is_equal = left > 0 && key == threshold;
         if (is_over || (is_equal && equal_at < left)) to[over_at + min(equal_at, left)] = lo + i;
         over_at += is_over;
         equal_at += is_equal;
     }
-    for (int i = over_all + min(equal_all, left) + (int)rank * kBoundsThreads + tid; i < p.budget; i += (int)size * kBoundsThreads) to[i] = -1;
-    cluster_meet();                                                      // (nobody leaves while another reads its counts)
+    const int mine = together ? (int)rank : 0;
+    for (int i = over_all + min(equal_all, left) + mine * kSelectThreads + tid; i < p.budget; i += (int)parts * kSelectThreads) to[i] = -1;
+    if (together) cluster_meet();                                        // (nobody leaves while another reads its counts)
 }
 
 }  // namespace ql

@@ -133,7 +133,7 @@ struct SharedPlan {
     bool alone;                                                          // the call is one of qlinear_paged_attention
     bool prefix_tiles, own_tiles;
     int32_t group, tile_rows;
-    size_t own_at, rows_at, ml_at, stretches_at, lengths_at, group_of_at, row_seq_at, bytes;
+    size_t own_at, rows_at, ml_at, stretches_at, lengths_at, row_of_at, bytes;
 };
 bool shared_plan(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t T, int32_t max_q, int32_t n_groups, SharedPlan* a)
 {
@@ -157,9 +157,8 @@ bool shared_plan(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t T, int32_t m
     a->ml_at = a->rows_at + up(cells * d * sizeof(float));
     a->stretches_at = a->ml_at + up(cells * sizeof(float2));
     a->lengths_at = a->stretches_at + up(V * sizeof(AttnStretch));
-    a->group_of_at = a->lengths_at + up((V + 1) * 4);
-    a->row_seq_at = a->group_of_at + up((size_t)B * 4);
-    a->bytes = std::max(a->row_seq_at + up((size_t)T * 4), qlinear_paged_attention_workspace(h, h_q, B, max_q));
+    a->row_of_at = a->lengths_at + up((V + 1) * 4);
+    a->bytes = std::max(a->row_of_at + up((size_t)T * sizeof(int2)), qlinear_paged_attention_workspace(h, h_q, B, max_q));
     return true;
 }
 
@@ -226,13 +225,13 @@ extern "C" ql_status qlinear_paged_attention_shared(qlinear_paged_t h, const voi
     if (!guard.ok) { cudaGetLastError(); return QL_ERR_CUDA; }
     char* w = static_cast<char*>(workspace);
     SharedPlanParams plan{p.batch, group_start, prefix_len, n_groups, a.group, max_q, a.tile_rows, a.prefix_tiles, a.own_tiles, reinterpret_cast<AttnStretch*>(w + a.stretches_at),
-                          reinterpret_cast<int32_t*>(w + a.lengths_at), reinterpret_cast<int32_t*>(w + a.group_of_at), reinterpret_cast<int32_t*>(w + a.row_seq_at)};
+                          reinterpret_cast<int32_t*>(w + a.lengths_at), reinterpret_cast<int2*>(w + a.row_of_at)};
     p.q = static_cast<const __half*>(q); p.q_ld = q_ld;
     p.h_q = h_q; p.group = a.group; p.max_q = max_q; p.n_groups = n_groups;
     p.stretches = plan.stretches; p.lengths = plan.lengths;
     p.row_o = reinterpret_cast<float*>(w + a.rows_at); p.row_ml = reinterpret_cast<float2*>(w + a.ml_at);
     const int32_t few = few_ctas(h, V), sms = h->shared.sms;
-    const SharedJoinParams j{plan.stretches, plan.lengths, plan.group_of, plan.row_seq, p.row_o, p.row_ml, static_cast<__half*>(out), out_ld, T, h_q, a.group, h->d.h_kv, n_groups, a.tile_rows,
+    const SharedJoinParams j{plan.stretches, plan.lengths, plan.row_of, p.row_o, p.row_ml, static_cast<__half*>(out), out_ld, T, h_q, a.group, h->d.h_kv, n_groups, a.tile_rows,
                              {reinterpret_cast<const float*>(w), 0, n_groups, a.prefix_tiles ? sms : few, a.prefix_tiles},
                              {reinterpret_cast<const float*>(w + a.own_at), n_groups, V, a.own_tiles ? sms : few, a.own_tiles}};
     cudaStream_t st = static_cast<cudaStream_t>(stream);

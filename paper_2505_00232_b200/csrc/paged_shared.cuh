@@ -20,6 +20,12 @@ constexpr int kSharedThreads = 1024, kMostStretches = QL_PAGED_MAX_SEQUENCES;
 constexpr int kStretchUnit = 64;
 constexpr int kMostPrefix = 1 << 30;                                     // (positions and rows add up below 2^31)
 
+// A launch of one of the two kernels over the stretches v0 .. v1 - 1.
+struct SharedLaunch {
+    const float* partial;
+    int32_t v0, v1, grid;
+    bool tiles;
+};
 struct SharedPlanParams {
     PagedBatch batch;
     const int32_t* group_start;
@@ -28,8 +34,7 @@ struct SharedPlanParams {
     bool prefix_tiles, own_tiles;
     AttnStretch* stretches;      // [n_groups + B]
     int32_t* lengths;            // [n_groups + B + 1]
-    int32_t* group_of;           // [B] the group whose beginning a sequence shares, -1: none
-    int32_t* row_seq;            // [T] the sequence of a served row, -1: none
+    int2* row_of;                // [T] the stretches of a served row: its sequence's own, its group's (-1: none); -1: not served
 };
 
 template <int kRows>
@@ -45,39 +50,38 @@ __device__ __forceinline__ int stretch_length(const AttnStretch& v, int group, b
 
 __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const SharedPlanParams p)
 {
-    __shared__ int group_of[kMostStretches], prefix[kMostStretches], sums[32];
+    __shared__ int start[kMostStretches + 1], len_of[kMostStretches], group_of[kMostStretches], prefix[kMostStretches], sums[32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const PagedBatch& bt = p.batch;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = p.n_groups, V = G + bt.B;
     const int64_t held = min((int64_t)bt.table_width << (bt.log2_blocks + 4), (int64_t)INT32_MAX);
-    for (int b = tid; b < bt.B; b += kSharedThreads) group_of[b] = -1;
-    for (int t = tid; t < bt.T; t += kSharedThreads) p.row_seq[t] = -1;
+    for (int b = tid; b <= bt.B; b += kSharedThreads) start[b] = bt.q_start[b];
+    for (int b = tid; b < bt.B; b += kSharedThreads) { len_of[b] = bt.kv_len[b]; group_of[b] = -1; }
+    for (int t = tid; t < bt.T; t += kSharedThreads) p.row_of[t] = make_int2(-1, -1);
+    int s = 0, e = 0, wanted = 0;                                        // (of this warp's first group, on its way meanwhile)
+    if (warp < G) { s = p.group_start[warp]; e = p.group_start[warp + 1]; wanted = p.prefix_len[warp]; }
     __syncthreads();
     for (int g = warp; g < G; g += kSharedThreads / 32) {
-        const int s = p.group_start[g], e = p.group_start[g + 1];
+        if (g != warp) { s = p.group_start[g]; e = p.group_start[g + 1]; wanted = p.prefix_len[g]; }
         const bool some = s >= 0 && e <= bt.B && (int64_t)e - s >= 2;
         int64_t least = min(held, (int64_t)kMostPrefix);
         int first = INT32_MAX;                                           // the first sequence with rows
         bool ok = some;
         for (int b = s + lane; some && b < e; b += 32) {
-            const int t0 = bt.q_start[b], t1 = bt.q_start[b + 1];
+            const int t0 = start[b], t1 = start[b + 1];
             ok = ok && t0 >= 0 && t1 >= t0 && t1 <= bt.T;
-            if (t1 <= t0 || bt.kv_len[b] <= 0) continue;                 // (a request that is done keeps the others' beginning as it is)
+            if (t1 <= t0 || len_of[b] <= 0) continue;                    // (a request that is done keeps the others' beginning as it is)
             first = min(first, b);
-            least = min(least, (int64_t)bt.kv_len[b] - ((int64_t)t1 - t0) + 1);   // what its first row sees
+            least = min(least, (int64_t)len_of[b] - ((int64_t)t1 - t0) + 1);   // what its first row sees
         }
         first = __reduce_min_sync(0xffffffffu, first);
         int sees = __reduce_min_sync(0xffffffffu, (int)max(least, (int64_t)0));
         ok = __all_sync(0xffffffffu, ok) && first != INT32_MAX;
-        sees = ok ? max(min(sees, p.prefix_len[g]), 0) / kStretchUnit * kStretchUnit : 0;
+        sees = ok ? max(min(sees, wanted), 0) / kStretchUnit * kStretchUnit : 0;
         for (int b = s + lane; sees > 0 && b < e; b += 32)
-            if (bt.kv_len[b] > 0) atomicMax(&group_of[b], g);
-        if (lane == 0) {
-            prefix[g] = sees;
-            const int t0 = sees > 0 ? bt.q_start[s] : 0, rows = sees > 0 ? bt.q_start[e] - t0 : 0;
-            p.stretches[g] = AttnStretch{t0, rows, sees - 1, 0, sees, sees > 0 ? first : 0, sees / kPagedBlock, (rows * p.group + kAttnCols - 1) / kAttnCols};
-        }
+            if (len_of[b] > 0) atomicMax(&group_of[b], g);
+        if (lane == 0) prefix[g] = sees;
     }
     __syncthreads();
     int before = 0;
@@ -86,10 +90,24 @@ __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const
         int n = 0;
         if (v < V) {
             AttnStretch st{};
-            if (v < G) st = p.stretches[v];                              // (written by this CTA, before its threads met)
-            else {
-                const int b = v - G, g = group_of[b], rows_all = paged_rows(bt, b, &st.t0), len = bt.kv_len[b];
-                p.group_of[b] = g;
+            if (v < G) {
+                const int sees = prefix[v];
+                if (sees > 0) {                                          // (a group of sequences in [0, B))
+                    const int s0 = p.group_start[v], e0 = p.group_start[v + 1];
+                    int first = s0;
+                    while (first + 1 < e0 && (start[first + 1] <= start[first] || len_of[first] <= 0)) ++first;   // the first sequence with rows: its pages
+                    st.t0 = start[s0];
+                    st.rows = start[e0] - st.t0;
+                    st.pos0 = sees - 1;
+                    st.end = sees;
+                    st.seq = first;
+                    st.blocks = sees / kPagedBlock;
+                    st.row_blocks = (st.rows * p.group + kAttnCols - 1) / kAttnCols;
+                }
+            } else {
+                const int b = v - G, g = group_of[b], t1 = start[b + 1], len = len_of[b];
+                st.t0 = start[b];
+                const int rows_all = st.t0 < 0 || t1 > bt.T || t1 < st.t0 ? 0 : t1 - st.t0;
                 st.rows = len > 0 ? min(rows_all, p.max_q) : 0;
                 st.first = g >= 0 ? prefix[g] : 0;
                 st.end = (int)held;
@@ -100,9 +118,9 @@ __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const
                     st.blocks = max((int)(((unsigned)max(end, 0) + kPagedBlock - 1) / kPagedBlock) - st.first / kPagedBlock, 0);
                     st.row_blocks = (st.rows * p.group + kAttnCols - 1) / kAttnCols;
                 }
-                for (int i = 0; i < min(rows_all, p.max_q); ++i) p.row_seq[st.t0 + i] = b;
-                p.stretches[v] = st;
+                for (int i = 0; i < min(rows_all, p.max_q); ++i) p.row_of[st.t0 + i] = make_int2(v, g);
             }
+            p.stretches[v] = st;
             const bool tiles = v < G ? p.prefix_tiles : p.own_tiles;
             n = st.rows <= 0 ? 0 : p.tile_rows == 128 ? stretch_length<128>(st, p.group, tiles) : stretch_length<256>(st, p.group, tiles);
         }
@@ -115,28 +133,18 @@ __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const
         __syncthreads();
         if (lane == 31) sums[warp] = run;
         __syncthreads();
-        int mine = sums[lane], all = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int u = __shfl_up_sync(0xffffffffu, all, o);
-            if (lane >= o) all += u;
-        }
-        run += before + __shfl_sync(0xffffffffu, all - mine, warp);
+        const int mine = sums[lane];
+        run += before + (int)__reduce_add_sync(0xffffffffu, lane < warp ? (unsigned)mine : 0u);
         if (v < V) p.lengths[v + 1] = run;
-        before += __shfl_sync(0xffffffffu, all, 31);
+        before += (int)__reduce_add_sync(0xffffffffu, (unsigned)mine);
     }
     if (tid == 0) p.lengths[0] = 0;
 }
 
-// One launch of a kernel over stretches, as the join finds its parts.
-struct SharedLaunch {
-    const float* partial;
-    int32_t v0, v1, grid;
-    bool tiles;
-};
 struct SharedJoinParams {
-    AttnStretch const* stretches;
-    const int32_t *lengths, *group_of, *row_seq;
+    const AttnStretch* stretches;
+    const int32_t* lengths;
+    const int2* row_of;
     const float* row_o;
     const float2* row_ml;
     __half* out;
@@ -145,22 +153,17 @@ struct SharedJoinParams {
     SharedLaunch prefix, own;
 };
 
-// The parts of a row in one of its stretches: n of them, part i with o at o + (i == 0 ? first : i * stride), and its m and l.
-struct SharedParts {
-    const float *first, *others;                                         // of part 0, and where part 1 would lie with the others' stride (their slots 0)
-    const float *ml_first, *ml_others;
-    int64_t stride;
-    int ml_step, n;                                                      // from m to l
-};
-template <int D>
-__device__ __forceinline__ SharedParts shared_parts(const SharedJoinParams& p, const SharedLaunch& at, int part, int v, int t, int head, int in_group)
+// The parts of a row in one of its stretches: n of them, in the slots of neighbouring CTAs from c0 on (the first part in slot 1, later ones in slot 0), or, n = 1, in a place of its own.
+struct SharedParts { int32_t n, c0, row; };
+__device__ __forceinline__ SharedParts shared_parts(const SharedJoinParams& p, const SharedLaunch& at, int v, int t, int head, int in_group)
 {
     const AttnStretch st = p.stretches[v];
-    SharedParts r{};
-    const int row = (t - st.t0) * p.group + in_group, block_rows = at.tiles ? p.tile_rows : kAttnCols, block = row / block_rows;
-    int64_t begin = (int64_t)(p.lengths[v] - p.lengths[at.v0]) * p.h_kv;
-    int length, overhead = kAttnOverhead, end;
+    const int32_t lengths_v = p.lengths[v], lengths_0 = p.lengths[at.v0], lengths_1 = p.lengths[at.v1];
+    SharedParts r{0, 0, 0};
     if (st.rows <= 0) return r;
+    const int row = (t - st.t0) * p.group + in_group, block_rows = at.tiles ? p.tile_rows : kAttnCols, block = row / block_rows;
+    int64_t begin = (int64_t)(lengths_v - lengths_0) * p.h_kv;
+    int length, overhead = kAttnOverhead, end;
     if (at.tiles) {
         overhead = kTileOverhead;
         const auto steps = [&](int k) { return p.tile_rows == 128 ? stretch_steps<64, 128>(st, k * 128, p.group, &end) : stretch_steps<64, 256>(st, k * 256, p.group, &end); };
@@ -174,22 +177,19 @@ __device__ __forceinline__ SharedParts shared_parts(const SharedJoinParams& p, c
         length = st.blocks + kAttnOverhead;
         begin += ((int64_t)head * st.row_blocks + block) * length;
     }
-    const int64_t total = (int64_t)(p.lengths[at.v1] - p.lengths[at.v0]) * p.h_kv, span = max((total + at.grid - 1) / at.grid, (int64_t)(at.tiles ? 1 : kAttnSpan));
-    const int c0 = (int)((begin + overhead) / span), c1 = (int)((begin + length - 1) / span);   // the CTAs with something of it
-    r.n = c1 - c0 + 1;
-    if (r.n == 1) {
-        const int64_t at_row = ((int64_t)part * p.T + t) * p.h_q + head * p.group + in_group;
-        r.first = p.row_o + at_row * D;
-        r.ml_first = reinterpret_cast<const float*>(p.row_ml + at_row);
-        r.ml_step = 1;
-        return r;
+    const int64_t total = (int64_t)(lengths_1 - lengths_0) * p.h_kv;
+    int c1;                                                              // the CTAs with something of it
+    if (total <= INT32_MAX - at.grid) {                                  // (32 bits: a sixth of the time)
+        const unsigned span = max(((unsigned)total + at.grid - 1) / (unsigned)at.grid, (unsigned)(at.tiles ? 1 : kAttnSpan));
+        r.c0 = ((unsigned)begin + overhead) / span;
+        c1 = ((unsigned)begin + length - 1) / span;
+    } else {
+        const int64_t span = max((total + at.grid - 1) / at.grid, (int64_t)(at.tiles ? 1 : kAttnSpan));
+        r.c0 = (int)((begin + overhead) / span);
+        c1 = (int)((begin + length - 1) / span);
     }
-    r.stride = 2ll * block_rows * (D + 2);                               // (slots 0 of neighbouring CTAs; the first part lies in slot 1)
-    r.others = at.partial + c0 * r.stride + (row - block * block_rows) * D;
-    r.first = r.others + block_rows * (D + 2);
-    r.ml_others = at.partial + c0 * r.stride + block_rows * D + (row - block * block_rows);
-    r.ml_first = r.ml_others + block_rows * (D + 2);
-    r.ml_step = block_rows;
+    r.n = c1 - r.c0 + 1;
+    r.row = row - block * block_rows;
     return r;
 }
 
@@ -203,44 +203,55 @@ __global__ void __launch_bounds__(256) paged_shared_join_kernel(const SharedJoin
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int t = blockIdx.x, head = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % W;
-    const int b = p.row_seq[t];
-    if (b < 0) return;
-    const int g = p.group_of[b];
+    const int2 of = p.row_of[t];
+    if (of.x < 0) return;
     for (int r0 = 0; r0 < p.group; r0 += 8 / W) {
         const int r = r0 + warp / W;
         float acc[V], l = 0.f, m = -1e30f;
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] = 0.f;
         if (r < p.group) {
-            SharedParts parts[2] = {};
-            if (g >= 0) parts[0] = shared_parts<D>(p, p.prefix, 0, g, t, head, r);
-            parts[1] = shared_parts<D>(p, p.own, 1, p.n_groups + b, t, head, r);
-            const int n = parts[0].n + parts[1].n;
-            const auto ml_of = [&](int i) {
-                const bool one = i >= parts[0].n;
-                const SharedParts& s = parts[one];
-                const int k = one ? i - parts[0].n : i;
-                return k == 0 ? s.ml_first : s.ml_others + k * s.stride;
+            SharedParts pre{0, 0, 0};
+            if (of.y >= 0) pre = shared_parts(p, p.prefix, of.y, t, head, r);
+            const SharedParts own = shared_parts(p, p.own, of.x, t, head, r);
+            const int n = pre.n + own.n;
+            // part i: where its o lies, and its m and l
+            const auto find = [&](int i, const float** o, const float** ml, int* to_l) {
+                const bool first = i < pre.n;
+                const SharedParts s = first ? pre : own;
+                const SharedLaunch& at = first ? p.prefix : p.own;
+                if (s.n == 1) {
+                    const int64_t cell = ((int64_t)(first ? 0 : 1) * p.T + t) * p.h_q + head * p.group + r;
+                    *o = p.row_o + cell * D;
+                    *ml = reinterpret_cast<const float*>(p.row_ml + cell);
+                    *to_l = 1;
+                    return;
+                }
+                const int k = first ? i : i - pre.n, block_rows = at.tiles ? p.tile_rows : kAttnCols;
+                const float* slot = at.partial + (int64_t)(2 * (s.c0 + k) + (k == 0 ? 1 : 0)) * (block_rows * (D + 2));
+                *o = slot + s.row * D;
+                *ml = slot + block_rows * D + s.row;
+                *to_l = block_rows;
             };
-            const auto step_of = [&](int i) { return parts[i >= parts[0].n].ml_step; };
-            for (int i = lane; i < n; i += 32) m = fmaxf(m, *ml_of(i));
+            const float *o = nullptr, *ml = nullptr;
+            int to_l = 0;
+            for (int i = lane; i < n; i += 32) {
+                find(i, &o, &ml, &to_l);
+                m = fmaxf(m, *ml);
+            }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
             for (int at = sub; at < n; at += 32 * W) {                   // 32 parts' weights side by side, then their values
                 const int mine = at + lane * W, here = min(32, (n - at + W - 1) / W);
                 float f = 0.f;
                 if (mine < n) {
-                    const float* ml = ml_of(mine);
+                    find(mine, &o, &ml, &to_l);
                     f = exp2_fast(ml[0] - m);
-                    l += ml[step_of(mine)] * f;
+                    l += ml[to_l] * f;
                 }
-#pragma unroll 8
+#pragma unroll 4
                 for (int j = 0; j < here; ++j) {
-                    const int i = at + j * W;
-                    const bool one = i >= parts[0].n;
-                    const SharedParts& s = parts[one];
-                    const int k = one ? i - parts[0].n : i;
-                    const float* from = (k == 0 ? s.first : s.others + k * s.stride) + V * lane;
+                    const float* from = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(o), j)) + V * lane;
                     const float fj = __shfl_sync(0xffffffffu, f, j);
                     float y[V];
                     if constexpr (V == 2) *reinterpret_cast<float2*>(y) = *reinterpret_cast<const float2*>(from);
@@ -252,7 +263,7 @@ __global__ void __launch_bounds__(256) paged_shared_join_kernel(const SharedJoin
                 }
             }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+            for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
         }
         if (W > 1) {
             __syncthreads();

@@ -121,9 +121,9 @@ extern "C" ql_status qlinear_paged_summarise(qlinear_paged_t h, const int32_t* t
     p.scales = scales;
     // T rows of B sequences lie in T / page_size + 2 B pages at most
     const int64_t pages = std::min<int64_t>(((int64_t)T >> (h->log2_blocks + 4)) + 2ll * B, T);
-    const unsigned grid = (unsigned)std::min<int64_t>((pages * h->d.h_kv + kBoundsWarps - 1) / kBoundsWarps, 8ll * h->shared.sms);
+    const unsigned grid = (unsigned)std::min<int64_t>(pages, 4ll * h->shared.sms);
     const auto kernel = h->d.d_h == 64 ? paged_bounds_kernel<64> : h->d.d_h == 128 ? paged_bounds_kernel<128> : paged_bounds_kernel<256>;
-    return launched(launch(kernel, p, dim3(grid), dim3(kBoundsThreads), (B + 1) * 4, static_cast<cudaStream_t>(stream), 1, h->pdl));
+    return launched(launch(kernel, p, dim3(grid), dim3(kBoundsThreads), (2 * B + 1) * 4, static_cast<cudaStream_t>(stream), 1, h->pdl));
 }
 
 namespace {
@@ -132,11 +132,11 @@ cudaError_t launch_select(const PagedSelectParams& p, dim3 grid, int cluster, in
 {
     static std::atomic<bool> flags[64];
     if (!flags[device].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(paged_select_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelectMostColumns / 8 * 4);
+        const cudaError_t e = cudaFuncSetAttribute(paged_select_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, std::max(kSelectMostColumns / 8, kSelectGathered) * 4);
         if (e != cudaSuccess) return e;
         flags[device].store(true, std::memory_order_release);
     }
-    return launch(paged_select_kernel<D>, p, grid, dim3(kBoundsThreads), p.share * 4, st, cluster, pdl);
+    return launch(paged_select_kernel<D>, p, grid, dim3(kSelectThreads), (p.gathered ? p.batch.table_width : p.share) * 4, st, cluster, pdl);
 }
 }  // namespace
 
@@ -155,10 +155,11 @@ extern "C" ql_status qlinear_paged_select(qlinear_paged_t h, const void* q, int6
     p.q = static_cast<const __half*>(q); p.q_ld = q_ld;
     p.bounds = static_cast<const int8_t*>(bounds); p.scales = scales; p.pages = pages;
     p.group = h_q / h->d.h_kv; p.budget = budget; p.first = first; p.recent = recent;
-    // CTAs of a row and KV head: more while they would not fill the SMs and have 128 columns left each, and as many as hold the keys
+    // CTAs of a row and KV head: more while they would not fill the SMs and have 64 columns left each, and as many as hold the keys
     int cluster = 1;
-    while (cluster < 8 && (int64_t)T * h->d.h_kv * cluster <= h->shared.sms && table_width / (2 * cluster) >= 128) cluster *= 2;
-    while ((table_width + cluster - 1) / cluster > kSelectMostColumns / 8) cluster *= 2;
+    while (cluster < 8 && (int64_t)T * h->d.h_kv * cluster <= h->shared.sms && table_width / (2 * cluster) >= 64) cluster *= 2;
+    p.gathered = table_width <= kSelectGathered;
+    while (!p.gathered && (table_width + cluster - 1) / cluster > kSelectMostColumns / 8) cluster *= 2;
     p.share = std::max((table_width + cluster - 1) / cluster, 1);
     if ((int64_t)T * cluster > INT32_MAX) return QL_ERR_INVALID_ARG;
     const auto go = h->d.d_h == 64 ? launch_select<64> : h->d.d_h == 128 ? launch_select<128> : launch_select<256>;
