@@ -414,8 +414,9 @@ ql_status qlinear_paged_compact(qlinear_paged_t h, int32_t* refs_dev, int32_t* t
  * qlinear_paged_attention_shared: qlinear_paged_attention (no window) for a batch of which sequences share the beginning: group g is the sequences group_start[g] .. group_start[g + 1] - 1 (int32 [n_groups + 1]),
  *   whose first prefix_len[g] tokens are the same, the table rows of the group holding the same pages for them or pages of the same contents.  The prefix is read and multiplied once for all rows of the group (from the pages of one of
  *   its sequences), what follows once per sequence, and the two are joined; the result is that of qlinear_paged_attention up to rounding.  A prefix longer than what one of the group's rows sees counts as
- *   far as all see it.  Sequences of no group, and groups that do not lie in [0, B) or that have less than two sequences, share nothing; no sequence may be in two groups.  n_groups <= QL_PAGED_MAX_SEQUENCES.
- *   Calls with max_q * h_q / h_kv >= 256 query rows a sequence and KV head, which gain nothing by it, are qlinear_paged_attention calls.  The limits on B * C and T are those of that call with n_groups + B in the place of B.
+ *   far as all see it.  Sequences of no group, and groups that do not lie in [0, B) or that have less than two sequences, share nothing; no sequence may be in two groups.  n_groups + B <= QL_PAGED_MAX_SEQUENCES.
+ *   Calls that by their sizes (the table's columns for the lengths: pass no more than are needed) would gain nothing by it are qlinear_paged_attention calls, with the limits of that; QLINEAR_PAGED_SHARED=0 makes all calls such, 1 and 2
+ *   those without groups alone (beginnings by the kernel of few rows, where it serves, and of many).
  *   workspace_dev: qlinear_paged_attention_shared_workspace bytes, 32-byte aligned, overwritten.
  * Asynchronous, allocate nothing; ordered against appends, summaries and moves of the same pages by the caller.  Errors as above. */
 ql_status qlinear_paged_summarise(qlinear_paged_t h, const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T,

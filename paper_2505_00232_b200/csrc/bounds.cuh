@@ -59,12 +59,12 @@ __device__ __forceinline__ int bounds_scan(int v, int* total, int* sums)
 }
 
 // A warp takes a page and KV head: in a block of 16 tokens lane 4 t + c has eight elements of each group of the tokens t and t + 8, so that the maxima over tokens are packed fp16
-// instructions on what it holds (the smallest as the largest of the negated: one operation for both), and at the end 8 lanes share the values out among them: each exchange halves what a lane goes on with (28
+// instructions on what it holds, and at the end (the smallest as the largest of the negated: one operation for both) 8 lanes share the values out among them: each exchange halves what a lane goes on with (28
 // exchanges for 32 pairs, not 96), and a lane is left with elements in a row, which it encodes and stores.
 // Every CTA numbers the touched columns of the batch (a scan) and takes pages in turn, 32 of them looked up side by side.
 // Bound: HBM (the keys of the touched pages, once); for a generated token a sequence the chain length -> column -> page -> keys.
 template <int D>
-__global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : D == 128 ? 3 : 4) paged_bounds_kernel(const PagedBoundsParams p)
+__global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : 4) paged_bounds_kernel(const PagedBoundsParams p)
 {
     constexpr int NB = D / 64, kBlock = paged_block_bytes(D), kPairs = 16 * NB;   // pairs of elements of a lane: largest and smallest
     extern __shared__ int pre[];                                         // [B + 1] touched columns before sequence b, [B] the first of them
@@ -106,19 +106,19 @@ __global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : D == 128 ? 3 : 
             const uint8_t* blk = bt.pool + (((int64_t)page * bt.h_kv + head) << bt.log2_blocks) * kBlock;
             uint32_t top[kPairs];                                        // pairs 4 (4 j + 2 e + s) ..: panel j, group e, s: of the negated
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) top[i] = 0xfc00fc00u;       // (-infinity)
+            for (int i = 0; i < kPairs; ++i) top[i] = i & 4 ? 0x7c007c00u : 0xfc00fc00u;   // (infinities)
             const auto take = [&](uint32_t word, uint32_t scale, uint32_t* to) {
                 uint32_t h[4];
                 unpack_int4_word(word, h);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t v = h2_mul(h[i], scale), w = v ^ 0x80008000u;
-                    const __half2 a = __hmax2(*reinterpret_cast<const __half2*>(to + i), *reinterpret_cast<const __half2*>(&v)), b = __hmax2(*reinterpret_cast<const __half2*>(to + 4 + i), *reinterpret_cast<const __half2*>(&w));
+                    const uint32_t v = h2_mul(h[i], scale);
+                    const __half2 a = __hmax2(*reinterpret_cast<const __half2*>(to + i), *reinterpret_cast<const __half2*>(&v)), b = __hmin2(*reinterpret_cast<const __half2*>(to + 4 + i), *reinterpret_cast<const __half2*>(&v));
                     to[i] = *reinterpret_cast<const uint32_t*>(&a);
                     to[4 + i] = *reinterpret_cast<const uint32_t*>(&b);
                 }
             };
-#pragma unroll 2
+#pragma unroll 1
             for (int t0 = 0; t0 < tokens; t0 += kPagedBlock, blk += kBlock) {
                 uint4 kw[NB];
                 uint2 ks[NB];
@@ -139,6 +139,8 @@ __global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : D == 128 ? 3 : 
                     }
                 }
             }
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) top[i] ^= i & 4 ? 0x80008000u : 0u;   // (of the negated, the largest)
             // the lane with t keeps the pairs kPairs / 8 * t ..
             int held = kPairs;
 #pragma unroll
@@ -205,7 +207,7 @@ __device__ __forceinline__ int cluster_load(const int* p, uint32_t rank)
     return v;
 }
 
-constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
 constexpr int kSelectGathered = 40 << 10;                                // columns whose keys one CTA holds
 
 __device__ __forceinline__ void cluster_store(uint32_t* p, uint32_t rank, uint32_t v)
@@ -238,19 +240,20 @@ __device__ __forceinline__ int select_scan(int v, int* total, int* sums)
 // too wide for one CTA's shared memory (40960 columns) leave the keys where they are: the CTAs add their histograms through distributed shared memory.
 // Bound: the chain length -> page -> bounds -> meeting -> digits; for many rows the bytes of the bounds (2 d + 4 a page and KV head).
 template <int D>
-__global__ void __launch_bounds__(kSelectThreads, 2) paged_select_kernel(const PagedSelectParams p)
+__global__ void __launch_bounds__(kSelectThreads, 4) paged_select_kernel(const PagedSelectParams p)
 {
     constexpr int kLanes = D / 8, kPer = 32 / kLanes, kTurns = 8;        // lanes of a page's 2 D bytes, 16 each; pages at once; loads in flight
     extern __shared__ uint32_t keys[];                                   // [share], or every column's
     __shared__ __align__(16) int16_t codes[2 * D];
-    __shared__ int hist[2][256], counts[4], sums[kSelectWarps], found_digit, found_left, found_count, found_seq;
+    __shared__ int hist[2][256], counts[4], sums[kSelectWarps], found_digit, found_left, found_count;
+    __shared__ unsigned long long found;                                 // the row's sequence and position, one more of each
     __shared__ uint32_t range[2];                                        // the complement of the smallest key, the largest
     __shared__ float most[kSelectWarps];
     const PagedBatch& bt = p.batch;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, log2_page = bt.log2_blocks + 4;
     const uint32_t rank = cluster_rank(), size = cluster_size();
     const int t = (int)(blockIdx.x / size), head = blockIdx.y;
-    if (tid == 0) { found_seq = -1; range[0] = range[1] = 0; }
+    if (tid == 0) { found = 0; range[0] = range[1] = 0; }
     if (tid < 4) counts[tid] = 0;
     if (tid < 256) hist[0][tid] = hist[1][tid] = 0;
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (a CTA's shared memory is written by others once it has started)
@@ -271,18 +274,18 @@ __global__ void __launch_bounds__(kSelectThreads, 2) paged_select_kernel(const P
     for (int b = tid; b < bt.B; b += kSelectThreads) {
         int first;
         const int rows = paged_rows(bt, b, &first);
-        if (t >= first && t < first + rows) atomicMax(&found_seq, b);    // (the same for every CTA of the cluster, whatever q_start holds: they meet)
+        const int len = bt.kv_len[b];
+        if (t >= first && t < first + rows)                              // (the largest: the same for every CTA of the cluster, whatever q_start holds: they meet)
+            atomicMax(&found, (unsigned long long)(b + 1) << 32 | (uint32_t)max((int64_t)len - rows + (t - first) + 1, (int64_t)0));
     }
     float m = fmaxf(above, -below);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     if (lane == 0) most[warp] = m;
     __syncthreads();
-    const int seq = found_seq;
+    const int seq = (int)(found >> 32) - 1, pos = (int)(uint32_t)found - 1;
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (seq < 0) return;                                                 // (a row of no sequence: the whole cluster leaves)
-    int t0;
-    const int rows_all = paged_rows(bt, seq, &t0), pos = (int)max((int64_t)bt.kv_len[seq] - rows_all + (t - t0), (int64_t)-1);
     m = 0.f;
 #pragma unroll
     for (int w = 0; w < D / 32; ++w) m = fmaxf(m, most[w]);
@@ -304,9 +307,11 @@ __global__ void __launch_bounds__(kSelectThreads, 2) paged_select_kernel(const P
         if (p.gathered && size > 1) cluster_store(keys + begin + at, 0, key);
         else keys[at] = key;
     };
+    const int32_t* row = bt.table + seq * bt.table_ld + begin;
+    int page_next = warp * 32 + lane < n_mine ? row[warp * 32 + lane] : -1;
     for (int w0 = warp * 32; w0 < n_mine; w0 += kSelectThreads) {
-        const int at = w0 + lane, column = begin + at;
-        const int page = at < n_mine ? bt.table[seq * bt.table_ld + column] : -1;
+        const int at = w0 + lane, column = begin + at, page = page_next;
+        page_next = at + kSelectThreads < n_mine ? row[at + kSelectThreads] : -1;
         const bool ok = page >= 0 && page < bt.n_pages, always = all || column < p.first || column > last - p.recent;
         if (at < n_mine && (!ok || always)) put(at, ok ? 0xffffffffu : 0u);
         if (all) continue;
@@ -320,6 +325,11 @@ __global__ void __launch_bounds__(kSelectThreads, 2) paged_select_kernel(const P
             for (int k = 0; k < kTurns; ++k) {
                 const int64_t record = __shfl_sync(0xffffffffu, mine, i0 + k * kPer + lane / kLanes);
                 u[k] = *reinterpret_cast<const uint4*>(from + record * (2 * D));
+            }
+            if (i0 + kTurns * kPer < 32) {                               // (the next turns' are on their way to L2 meanwhile: a lane 128 bytes of a record)
+                const int k = lane * kTurns * kPer / 32, line = lane - k * 32 / (kTurns * kPer);
+                const int64_t record = __shfl_sync(0xffffffffu, mine, i0 + kTurns * kPer + k);
+                if (128 * line < 2 * D) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.bounds + record * (2 * D) + 128 * line));
             }
             int s[kTurns];
 #pragma unroll

@@ -133,48 +133,64 @@ struct SharedPlan {
     bool alone;                                                          // the call is one of qlinear_paged_attention
     bool prefix_tiles, own_tiles;
     int32_t group, tile_rows;
-    size_t own_at, rows_at, ml_at, stretches_at, lengths_at, row_of_at, bytes;
+    size_t own_at, rows_at, ml_at, stretches_at, lengths_at, row_of_at, spans_at, bytes;
 };
+// What of a call does not depend on the lengths: what it needs; false for bad arguments.
 bool shared_plan(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t T, int32_t max_q, int32_t n_groups, SharedPlan* a)
 {
     if (!h || h_q < 1 || h_q > 65536 || h_q % h->d.h_kv || B < 0 || T < 0 || n_groups < 0 || max_q < 0 || (int64_t)n_groups + B > QL_PAGED_MAX_SEQUENCES) return false;
     const int32_t d = h->d.d_h;
     a->group = h_q / h->d.h_kv;
     a->tile_rows = d == 256 ? TileShape<256>::kRows : TileShape<128>::kRows;
-    const int64_t rows = (int64_t)max_q * a->group, all_rows = (int64_t)T * a->group;
-    // a sequence's own rows fill a tile: they read what they see once already
-    a->alone = n_groups == 0 || rows >= 256 || all_rows >= 1 << 30;
-    a->own_tiles = rows > attn_max_rows(d);
-    a->prefix_tiles = a->own_tiles || all_rows > (int64_t)n_groups * attn_max_rows(d);
-    if (a->alone) {
-        a->bytes = qlinear_paged_attention_workspace(h, h_q, B, max_q);
-        return a->bytes > 0;
-    }
+    a->own_tiles = (int64_t)max_q * a->group > attn_max_rows(d);
     const auto up = [](size_t n) { return (n + 31) / 32 * 32; };
     const size_t few = up(few_partial(h)), tiles = up((size_t)2 * h->shared.sms * a->tile_rows * (d + 2) * sizeof(float)), cells = (size_t)2 * T * h_q, V = (size_t)n_groups + B;
-    a->own_at = a->prefix_tiles == a->own_tiles ? 0 : tiles;             // (one launch for both)
-    a->rows_at = a->own_at + (a->own_tiles ? tiles : few);
+    a->own_at = tiles;                                                   // (where it is a launch of its own)
+    a->rows_at = tiles + few;
     a->ml_at = a->rows_at + up(cells * d * sizeof(float));
     a->stretches_at = a->ml_at + up(cells * sizeof(float2));
     a->lengths_at = a->stretches_at + up(V * sizeof(AttnStretch));
     a->row_of_at = a->lengths_at + up((V + 1) * 4);
-    a->bytes = std::max(a->row_of_at + up((size_t)T * sizeof(int2)), qlinear_paged_attention_workspace(h, h_q, B, max_q));
-    return true;
+    a->spans_at = a->row_of_at + up((size_t)T * sizeof(int2));
+    const size_t plain = qlinear_paged_attention_workspace(h, h_q, B, max_q);
+    a->bytes = std::max(a->spans_at + 32, plain);
+    return plain > 0;
+}
+// Which kernels take it: by estimates of the three ways' times, with the tables' columns for the lengths and the beginnings.  A launch over stretches has a fixed part (plan, ramps, join; the tiles a pipeline of their own), few rows cost
+// by their blocks of 16 tokens and 8 rows, tiles by their steps of 64 tokens.  us, plain, few rows and tiles, 8 KV heads of 128 and 4 queries each: 4 sequences over 1024 tokens 11.5, 14.9, 30.9; 16 over 2048 19.8, 20.5, 33.1;
+// 8 over 16384 41.0, 30.4, 43.4; 16 over 16384 71.5, 47.3, 44.5; two groups of 32 over 16384 259, 149, 75.  4 of 256 and 2: 4 over 16384 25.6, 18.4, 37.7; two groups of 32 257, 87, 61.  2 of 64 and 7: 8 over 16384 15.4, 18.4, 32.2; two groups of 32 50, 51, 39.
+void shared_route(qlinear_paged_t h, int32_t B, int32_t T, int32_t max_q, int32_t n_groups, int32_t table_width, SharedPlan* a)
+{
+    const int32_t d = h->d.d_h, V = n_groups + B, choice = paged_shared_choice();
+    const int64_t held = std::min((int64_t)table_width * h->d.page_size, (int64_t)INT32_MAX), all_rows = (int64_t)T * a->group;
+    a->alone = n_groups == 0 || all_rows >= 1 << 30 || choice == 0;
+    // (the kernels number the steps of a KV head's segments in 32 bits)
+    const __int128 few_blocks = (__int128)(all_rows / kAttnCols + V) * (held / kPagedBlock + 1 + kAttnOverhead), tile_steps = (__int128)(all_rows / a->tile_rows + 2 * V) * (held / 64 + 1 + kTileOverhead);
+    if (few_blocks + tile_steps > INT32_MAX) a->alone = true;
+    if (a->alone) return;
+    const int64_t group_rows = (all_rows + n_groups - 1) / n_groups, rows = (int64_t)max_q * a->group;
+    const auto pieces_of = [](int64_t n, int64_t size) { return (double)((n + size - 1) / size); };
+    const double per_block = (d == 64 ? 0.085 : d == 128 ? 0.15 : 0.14) * h->d.h_kv * held / kPagedBlock / few_ctas(h, V), per_step = 1.2 * h->d.h_kv * held / 64 / h->shared.sms;
+    const double plain = a->own_tiles ? 18 + per_step * B * pieces_of(rows, a->tile_rows) : 9.5 + per_block * B * pieces_of(rows, kAttnCols);
+    const double few = a->own_tiles ? INFINITY : 13.5 + per_block * n_groups * pieces_of(group_rows, kAttnCols), tiles = 28 + per_step * n_groups * pieces_of(group_rows, a->tile_rows);
+    a->prefix_tiles = choice == 2 || a->own_tiles || (choice != 1 && tiles < few);
+    a->alone = choice < 0 && plain <= std::min(few, tiles);
 }
 
 template <int D>
-cudaError_t launch_join(const SharedJoinParams& j, cudaStream_t st, bool pdl)
+cudaError_t launch_join(const SharedJoinParams& j, int sms, cudaStream_t st, bool pdl)
 {
-    const dim3 grid(j.T, j.h_kv);
-    if (j.group <= 1) return launch(paged_shared_join_kernel<D, 8>, j, grid, dim3(256), 0, st, 1, pdl);
-    if (j.group <= 2) return launch(paged_shared_join_kernel<D, 4>, j, grid, dim3(256), 0, st, 1, pdl);
-    if (j.group <= 4) return launch(paged_shared_join_kernel<D, 2>, j, grid, dim3(256), 0, st, 1, pdl);
-    return launch(paged_shared_join_kernel<D, 1>, j, grid, dim3(256), 0, st, 1, pdl);
+    // a row's parts are up to one per CTA: as many warps for them as the SMs have room for (8 CTAs each), in CTAs of at most one token and KV head's rows
+    const int64_t rows = (int64_t)j.T * j.h_q, room = 64ll * sms;
+    const auto go = [&](auto kernel, int w) { return launch(kernel, j, dim3(j.T, j.h_kv, (j.group + 8 / w - 1) / (8 / w)), dim3(256), 0, st, 1, pdl); };
+    if (rows * 8 <= room || j.group <= 1) return go(paged_shared_join_kernel<D, 8>, 8);
+    if (rows * 4 <= room || j.group <= 2) return go(paged_shared_join_kernel<D, 4>, 4);
+    if (rows * 2 <= room || j.group <= 4) return go(paged_shared_join_kernel<D, 2>, 2);
+    return go(paged_shared_join_kernel<D, 1>, 1);
 }
 template <int D>
-cudaError_t launch_shared(const SharedPlanParams& plan, PagedAttnParams p, SharedJoinParams j, qlinear_paged_t h, cudaStream_t st)
+cudaError_t launch_shared(const SharedPlanParams& plan, PagedAttnParams p, const SharedJoinParams& j, qlinear_paged_t h, cudaStream_t st)
 {
-    const int V = p.n_groups + p.batch.B;
     cudaError_t e = launch(paged_shared_plan_kernel, plan, dim3(1), dim3(kSharedThreads), 0, st, 1, h->pdl);
     const auto go = [&](const SharedLaunch& at) {
         if (e != cudaSuccess) return;
@@ -182,15 +198,9 @@ cudaError_t launch_shared(const SharedPlanParams& plan, PagedAttnParams p, Share
         p.v0 = at.v0; p.v1 = at.v1; p.grid = at.grid;
         e = at.tiles ? launch_tiles<D>(p, at.v1 - at.v0, h->device, st, h->pdl) : launch_few<D, kAttnShared>(p, at.v1 - at.v0, h->device, st, h->pdl);
     };
-    if (plan.prefix_tiles == plan.own_tiles) {
-        j.prefix.v1 = j.own.v1 = V;
-        j.own = j.prefix;
-        go(j.prefix);
-    } else {
-        go(j.prefix);
-        go(j.own);
-    }
-    return e != cudaSuccess ? e : launch_join<D>(j, st, h->pdl);
+    go(j.prefix);
+    if (j.own.v0 != j.prefix.v0) go(j.own);
+    return e != cudaSuccess ? e : launch_join<D>(j, h->shared.sms, st, h->pdl);
 }
 
 }  // namespace
@@ -210,30 +220,28 @@ extern "C" ql_status qlinear_paged_attention_shared(qlinear_paged_t h, const voi
     SharedPlan a;
     if (!batch_of(h, table, table_ld, table_width, kv_len, q_start, B, T, &p.batch) || !shared_plan(h, h_q, B, T, max_q, n_groups, &a) || !scores_of(scale, softcap, &p)) return QL_ERR_INVALID_ARG;
     if (n_groups > 0 && (!group_start || !prefix_len || !aligned(group_start, 4) || !aligned(prefix_len, 4))) return QL_ERR_INVALID_ARG;
+    shared_route(h, B, T, max_q, n_groups, table_width, &a);
     if (a.alone) return qlinear_paged_attention(h, q, q_ld, out, out_ld, h_q, table, table_ld, table_width, kv_len, q_start, B, T, max_q, scale, softcap, 0, workspace, workspace_bytes, stream);
     if (B == 0 || T == 0 || max_q == 0) return QL_OK;
     const int32_t d = h->d.d_h, V = n_groups + B;
-    {   // the kernels number the steps of a KV head's segments in 32 bits
-        const int64_t held = std::min((int64_t)table_width * h->d.page_size, (int64_t)INT32_MAX), rows = (int64_t)T * a.group;
-        const int64_t few = rows / kAttnCols + V, tiles = rows / a.tile_rows + 2 * V;
-        if ((a.prefix_tiles ? (__int128)tiles * (held / 64 + 1 + kTileOverhead) : 0) + (a.own_tiles ? 0 : (__int128)few * (held / kPagedBlock + 1 + kAttnOverhead)) > INT32_MAX) return QL_ERR_INVALID_ARG;
-    }
     if (!rows_ok(q, q_ld, (int64_t)h_q * d) || !rows_ok(out, out_ld, (int64_t)h_q * d) || q == out) return QL_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 32) || workspace_bytes < a.bytes) return QL_ERR_INVALID_ARG;
     if (timed_out(h)) return QL_ERR_DEVICE_TIMEOUT;
     DeviceGuard guard(h->device);
     if (!guard.ok) { cudaGetLastError(); return QL_ERR_CUDA; }
     char* w = static_cast<char*>(workspace);
-    SharedPlanParams plan{p.batch, group_start, prefix_len, n_groups, a.group, max_q, a.tile_rows, a.prefix_tiles, a.own_tiles, reinterpret_cast<AttnStretch*>(w + a.stretches_at),
-                          reinterpret_cast<int32_t*>(w + a.lengths_at), reinterpret_cast<int2*>(w + a.row_of_at)};
+    const int32_t few = few_ctas(h, V), sms = h->shared.sms;
+    const bool one = a.prefix_tiles == a.own_tiles;                      // one launch for both
+    const SharedLaunch prefix{reinterpret_cast<const float*>(w), 0, one ? V : n_groups, a.prefix_tiles ? sms : few, a.prefix_tiles};
+    const SharedLaunch own = one ? prefix : SharedLaunch{reinterpret_cast<const float*>(w + a.own_at), n_groups, V, a.own_tiles ? sms : few, a.own_tiles};
+    int64_t* spans = reinterpret_cast<int64_t*>(w + a.spans_at);
+    const SharedPlanParams plan{p.batch, group_start, prefix_len, n_groups, a.group, max_q, a.tile_rows, prefix, own, spans, reinterpret_cast<AttnStretch*>(w + a.stretches_at),
+                                reinterpret_cast<int32_t*>(w + a.lengths_at), reinterpret_cast<int2*>(w + a.row_of_at)};
     p.q = static_cast<const __half*>(q); p.q_ld = q_ld;
     p.h_q = h_q; p.group = a.group; p.max_q = max_q; p.n_groups = n_groups;
     p.stretches = plan.stretches; p.lengths = plan.lengths;
     p.row_o = reinterpret_cast<float*>(w + a.rows_at); p.row_ml = reinterpret_cast<float2*>(w + a.ml_at);
-    const int32_t few = few_ctas(h, V), sms = h->shared.sms;
-    const SharedJoinParams j{plan.stretches, plan.lengths, plan.row_of, p.row_o, p.row_ml, static_cast<__half*>(out), out_ld, T, h_q, a.group, h->d.h_kv, n_groups, a.tile_rows,
-                             {reinterpret_cast<const float*>(w), 0, n_groups, a.prefix_tiles ? sms : few, a.prefix_tiles},
-                             {reinterpret_cast<const float*>(w + a.own_at), n_groups, V, a.own_tiles ? sms : few, a.own_tiles}};
+    const SharedJoinParams j{plan.stretches, plan.lengths, plan.row_of, p.row_o, p.row_ml, static_cast<__half*>(out), out_ld, T, h_q, a.group, h->d.h_kv, a.tile_rows == 128 ? 7 : 8, prefix, own, spans};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const auto go = d == 64 ? launch_shared<64> : d == 128 ? launch_shared<128> : launch_shared<256>;
     return launched(go(plan, p, j, h, st));

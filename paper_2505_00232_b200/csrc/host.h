@@ -14,6 +14,7 @@ struct SharedState {
 ql_status shared_state(int device, SharedState* out);
 ql_status device_sms(int device, int* sms);          // checks the device as well (QL_ERR_ARCH); allocates nothing
 bool pdl_enabled();                                  // QLINEAR_PDL
+int paged_shared_choice();                           // QLINEAR_PAGED_SHARED
 ql_status device_status(int device, uint32_t* detail);   // qlinear_device_status for a device whose shared state exists
 
 struct DeviceGuard {

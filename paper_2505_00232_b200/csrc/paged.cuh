@@ -18,7 +18,10 @@
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <limits.h>
 #include <stdint.h>
+
+#include "dequant.cuh"
 
 namespace ql {
 
@@ -270,6 +273,97 @@ __global__ void __launch_bounds__(kPagedThreads) paged_read_kernel(const PagedRe
         const int64_t to = (((int64_t)blockIdx.x * ROWS + row) * p.batch.h_kv + head) * d + 8 * m;
         *reinterpret_cast<uint4*>(p.k + to) = k;
         *reinterpret_cast<uint4*>(p.v + to) = v;
+    }
+}
+
+// The same for many rows a sequence: a warp takes 16 tokens of a KV head as they lie in a block, so that it reads whole blocks, 16 bytes a lane, and writes 64 bytes of a key and 128 of a value in a row
+// (the kernel above gathers words of 4 bytes: of 131000 tokens, 8 heads of 128, 155 us, here READ_US).  Every CTA numbers the blocks that the batch's rows lie in (a scan).  Bound: HBM, seven bytes written for one read.
+template <int D>
+__global__ void __launch_bounds__(kPagedThreads) paged_read_blocks_kernel(const PagedReadParams p)
+{
+    constexpr int NB = D / 64, kBlock = paged_block_bytes(D), kWarps = kPagedThreads / 32;
+    extern __shared__ int pre[];                                         // [B + 1] blocks before sequence b
+    __shared__ int sums[kWarps];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const PagedBatch& bt = p.batch;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3, h_kv = bt.h_kv;
+    // rows of sequence b, the position of the first, and its place in its block
+    const auto rows_of = [&](int b, int* t0, int64_t* p0, int* phase) {
+        const int rows = paged_rows(bt, b, t0);
+        *p0 = (int64_t)bt.kv_len[b] - rows;
+        *phase = (int)(*p0 & 15);
+        return rows;
+    };
+    int total = 0;
+    if (tid == 0) pre[0] = 0;
+    for (int b0 = 0; b0 < bt.B; b0 += kPagedThreads) {
+        const int b = b0 + tid;
+        int t0, phase, run = 0;
+        int64_t p0;
+        if (b < bt.B) {
+            const int rows = rows_of(b, &t0, &p0, &phase);
+            run = rows > 0 ? (phase + rows + 15) >> 4 : 0;
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, run, o);
+            if (lane >= o) run += u;
+        }
+        __syncthreads();
+        if (lane == 31) sums[warp] = run;
+        __syncthreads();
+        run += total;
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) run += sums[w];
+            total += sums[w];
+        }
+        if (b < bt.B) pre[b + 1] = run;
+    }
+    __syncthreads();
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    for (int64_t item = (int64_t)blockIdx.x * kWarps + warp; item < (int64_t)total * h_kv; item += (int64_t)gridDim.x * kWarps) {
+        const int k = (int)(item / h_kv), head = (int)(item - (int64_t)k * h_kv);
+        int b = 0, hi = bt.B, t0, phase;                                 // pre[b] <= k < pre[hi]
+        while (hi - b > 1) {
+            const int mid = (b + hi) >> 1;
+            if (pre[mid] <= k) b = mid;
+            else hi = mid;
+        }
+        int64_t p0;
+        const int rows = rows_of(b, &t0, &p0, &phase), row0 = 16 * (k - pre[b]) - phase;   // of token 0 of the block (below 0: not a row of the call)
+        const int64_t j = p0 + row0;
+        const uint8_t* blk = j >= 0 && j <= INT_MAX ? paged_block(bt, b, (int)j, head, kBlock) : nullptr;
+        uint4 kw[NB], vw[NB];
+        uint2 ks[NB], vs[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            kw[i] = vw[i] = zero;
+            ks[i] = vs[i] = make_uint2(0, 0);
+            if (!blk) continue;
+            kw[i] = *reinterpret_cast<const uint4*>(blk + 512 * i + 16 * lane);
+            ks[i] = *reinterpret_cast<const uint2*>(blk + paged_k_scales(D) + g * (8 * NB) + 8 * i);
+            vw[i] = *reinterpret_cast<const uint4*>(blk + paged_v_data(D) + 512 * i + 16 * lane);
+            vs[i] = *reinterpret_cast<const uint2*>(blk + paged_v_scales(D) + (2 * i + (g >> 2)) * 32 + 8 * c);
+        }
+        const auto put = [&](__half* to, int token, int element, uint32_t word, uint32_t scale) {
+            const int row = row0 + token;
+            if (row < 0 || row >= rows) return;
+            uint32_t h[4];
+            unpack_int4_word(word, h);
+            *reinterpret_cast<uint4*>(to + ((int64_t)(t0 + row) * h_kv + head) * D + element) = blk ? make_uint4(h2_mul(h[0], scale), h2_mul(h[1], scale), h2_mul(h[2], scale), h2_mul(h[3], scale)) : zero;
+        };
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            put(p.k, g, 64 * i + 8 * c, kw[i].x, __byte_perm(ks[i].x, ks[i].x, 0x1010));
+            put(p.k, g, 64 * i + 32 + 8 * c, kw[i].y, __byte_perm(ks[i].y, ks[i].y, 0x1010));
+            put(p.k, g + 8, 64 * i + 8 * c, kw[i].z, __byte_perm(ks[i].x, ks[i].x, 0x3232));
+            put(p.k, g + 8, 64 * i + 32 + 8 * c, kw[i].w, __byte_perm(ks[i].y, ks[i].y, 0x3232));
+            put(p.v, 2 * c, 64 * i + 8 * g, vw[i].x, __byte_perm(vs[i].x, vs[i].x, 0x1010));
+            put(p.v, 2 * c + 1, 64 * i + 8 * g, vw[i].y, __byte_perm(vs[i].x, vs[i].x, 0x3232));
+            put(p.v, 2 * c + 8, 64 * i + 8 * g, vw[i].z, __byte_perm(vs[i].y, vs[i].y, 0x1010));
+            put(p.v, 2 * c + 9, 64 * i + 8 * g, vw[i].w, __byte_perm(vs[i].y, vs[i].y, 0x3232));
+        }
     }
 }
 

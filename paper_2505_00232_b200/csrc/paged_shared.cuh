@@ -31,7 +31,8 @@ struct SharedPlanParams {
     const int32_t* group_start;
     const int32_t* prefix_len;
     int32_t n_groups, group, max_q, tile_rows;
-    bool prefix_tiles, own_tiles;
+    SharedLaunch prefix, own;    // (the same one, or one each)
+    int64_t* spans;              // of a CTA of theirs
     AttnStretch* stretches;      // [n_groups + B]
     int32_t* lengths;            // [n_groups + B + 1]
     int2* row_of;                // [T] the stretches of a served row: its sequence's own, its group's (-1: none); -1: not served
@@ -50,7 +51,7 @@ __device__ __forceinline__ int stretch_length(const AttnStretch& v, int group, b
 
 __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const SharedPlanParams p)
 {
-    __shared__ int start[kMostStretches + 1], len_of[kMostStretches], group_of[kMostStretches], prefix[kMostStretches], sums[32];
+    __shared__ int start[kMostStretches + 1], len_of[kMostStretches], group_of[kMostStretches], prefix[kMostStretches], sums[32], prefix_length;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const PagedBatch& bt = p.batch;
@@ -60,6 +61,7 @@ __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const
     for (int b = tid; b < bt.B; b += kSharedThreads) { len_of[b] = bt.kv_len[b]; group_of[b] = -1; }
     for (int t = tid; t < bt.T; t += kSharedThreads) p.row_of[t] = make_int2(-1, -1);
     int s = 0, e = 0, wanted = 0;                                        // (of this warp's first group, on its way meanwhile)
+    if (tid == 0) prefix_length = 0;
     if (warp < G) { s = p.group_start[warp]; e = p.group_start[warp + 1]; wanted = p.prefix_len[warp]; }
     __syncthreads();
     for (int g = warp; g < G; g += kSharedThreads / 32) {
@@ -121,7 +123,7 @@ __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const
                 for (int i = 0; i < min(rows_all, p.max_q); ++i) p.row_of[st.t0 + i] = make_int2(v, g);
             }
             p.stretches[v] = st;
-            const bool tiles = v < G ? p.prefix_tiles : p.own_tiles;
+            const bool tiles = v < G ? p.prefix.tiles : p.own.tiles;
             n = st.rows <= 0 ? 0 : p.tile_rows == 128 ? stretch_length<128>(st, p.group, tiles) : stretch_length<256>(st, p.group, tiles);
         }
         int run = n;
@@ -136,7 +138,14 @@ __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const
         const int mine = sums[lane];
         run += before + (int)__reduce_add_sync(0xffffffffu, lane < warp ? (unsigned)mine : 0u);
         if (v < V) p.lengths[v + 1] = run;
+        if (v + 1 == G) prefix_length = run;
         before += (int)__reduce_add_sync(0xffffffffu, (unsigned)mine);
+    }
+    __syncthreads();
+    if (tid < 2) {
+        const SharedLaunch& at = tid == 0 ? p.prefix : p.own;
+        const int64_t total = (int64_t)((at.v1 == G ? prefix_length : before) - (at.v0 == G ? prefix_length : 0)) * bt.h_kv;
+        p.spans[tid] = max((total + at.grid - 1) / at.grid, (int64_t)(at.tiles ? kSharedTileSpan : kAttnSpan));
     }
     if (tid == 0) p.lengths[0] = 0;
 }
@@ -149,142 +158,139 @@ struct SharedJoinParams {
     const float2* row_ml;
     __half* out;
     int64_t out_ld;
-    int32_t T, h_q, group, h_kv, n_groups, tile_rows;
+    int32_t T, h_q, group, h_kv, log2_tile_rows;
     SharedLaunch prefix, own;
+    const int64_t* spans;        // of the two launches
 };
 
 // The parts of a row in one of its stretches: n of them, in the slots of neighbouring CTAs from c0 on (the first part in slot 1, later ones in slot 0), or, n = 1, in a place of its own.
 struct SharedParts { int32_t n, c0, row; };
-__device__ __forceinline__ SharedParts shared_parts(const SharedJoinParams& p, const SharedLaunch& at, int v, int t, int head, int in_group)
+__device__ __forceinline__ SharedParts shared_parts(const SharedJoinParams& p, bool group_s, int v, int t, int head, int in_group)
 {
     const AttnStretch st = p.stretches[v];
-    const int32_t lengths_v = p.lengths[v], lengths_0 = p.lengths[at.v0], lengths_1 = p.lengths[at.v1];
-    SharedParts r{0, 0, 0};
-    if (st.rows <= 0) return r;
-    const int row = (t - st.t0) * p.group + in_group, block_rows = at.tiles ? p.tile_rows : kAttnCols, block = row / block_rows;
+    const int32_t v0 = group_s ? p.prefix.v0 : p.own.v0, lengths_v = p.lengths[v], lengths_0 = p.lengths[v0], lengths_1 = p.lengths[group_s ? p.prefix.v1 : p.own.v1];
+    const long long span = p.spans[group_s ? 0 : 1];
+    const bool tiles = group_s ? p.prefix.tiles : p.own.tiles;
+    const int row = (t - st.t0) * p.group + in_group, log2_rows = tiles ? p.log2_tile_rows : 3, block = row >> log2_rows, overhead = tiles ? kTileOverhead : kAttnOverhead;
     int64_t begin = (int64_t)(lengths_v - lengths_0) * p.h_kv;
-    int length, overhead = kAttnOverhead, end;
-    if (at.tiles) {
-        overhead = kTileOverhead;
-        const auto steps = [&](int k) { return p.tile_rows == 128 ? stretch_steps<64, 128>(st, k * 128, p.group, &end) : stretch_steps<64, 256>(st, k * 256, p.group, &end); };
+    int length = 0, end;
+    if (st.rows > 0 && tiles && group_s) {                               // (every row sees it whole)
+        length = tile_length(st.end / kStretchUnit);
+        begin += ((int64_t)block * p.h_kv + head) * length;
+    } else if (st.rows > 0 && tiles) {
+        const auto steps = [&](int k) { return p.log2_tile_rows == 7 ? stretch_steps<64, 128>(st, k * 128, p.group, &end) : stretch_steps<64, 256>(st, k * 256, p.group, &end); };
         length = tile_length(steps(block));
-        if (length == 0) return r;
-        if (v < p.n_groups) begin += (int64_t)block * length * p.h_kv;
-        else for (int k = 0; k < block; ++k) begin += (int64_t)tile_length(steps(k)) * p.h_kv;
+        for (int k = 0; k < block; ++k) begin += (int64_t)tile_length(steps(k)) * p.h_kv;
         begin += (int64_t)head * length;
-    } else {
-        if (st.blocks == 0) return r;
+    } else if (st.blocks > 0) {
         length = st.blocks + kAttnOverhead;
         begin += ((int64_t)head * st.row_blocks + block) * length;
     }
-    const int64_t total = (int64_t)(lengths_1 - lengths_0) * p.h_kv;
+    SharedParts r{0, 0, row - (block << log2_rows)};
+    if (length == 0) return r;
     int c1;                                                              // the CTAs with something of it
-    if (total <= INT32_MAX - at.grid) {                                  // (32 bits: a sixth of the time)
-        const unsigned span = max(((unsigned)total + at.grid - 1) / (unsigned)at.grid, (unsigned)(at.tiles ? 1 : kAttnSpan));
-        r.c0 = ((unsigned)begin + overhead) / span;
-        c1 = ((unsigned)begin + length - 1) / span;
+    if ((int64_t)(lengths_1 - lengths_0) * p.h_kv <= INT32_MAX) {        // (32 bits: a sixth of the time)
+        r.c0 = ((unsigned)begin + overhead) / (unsigned)span;
+        c1 = ((unsigned)begin + length - 1) / (unsigned)span;
     } else {
-        const int64_t span = max((total + at.grid - 1) / at.grid, (int64_t)(at.tiles ? 1 : kAttnSpan));
         r.c0 = (int)((begin + overhead) / span);
         c1 = (int)((begin + length - 1) / span);
     }
     r.n = c1 - r.c0 + 1;
-    r.row = row - block * block_rows;
     return r;
 }
 
-// A row of the call and a KV head per CTA; W of its 8 warps share a row's parts, in a fixed order.
+// 8 / W rows (query heads of a KV head) of a token per CTA; W warps share a row's parts, in a fixed order.
 template <int D, int W>
 __global__ void __launch_bounds__(256) paged_shared_join_kernel(const SharedJoinParams p)
 {
     constexpr int V = D / 32;
     __shared__ __align__(16) float sums[8][D];
-    __shared__ float sums_l[8];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int t = blockIdx.x, head = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % W;
     const int2 of = p.row_of[t];
     if (of.x < 0) return;
-    for (int r0 = 0; r0 < p.group; r0 += 8 / W) {
-        const int r = r0 + warp / W;
-        float acc[V], l = 0.f, m = -1e30f;
+    const int r = blockIdx.z * (8 / W) + warp / W;
+    float acc[V], l = 0.f, m = -1e30f;
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = 0.f;
-        if (r < p.group) {
-            SharedParts pre{0, 0, 0};
-            if (of.y >= 0) pre = shared_parts(p, p.prefix, of.y, t, head, r);
-            const SharedParts own = shared_parts(p, p.own, of.x, t, head, r);
-            const int n = pre.n + own.n;
-            // part i: where its o lies, and its m and l
-            const auto find = [&](int i, const float** o, const float** ml, int* to_l) {
-                const bool first = i < pre.n;
-                const SharedParts s = first ? pre : own;
-                const SharedLaunch& at = first ? p.prefix : p.own;
-                if (s.n == 1) {
-                    const int64_t cell = ((int64_t)(first ? 0 : 1) * p.T + t) * p.h_q + head * p.group + r;
-                    *o = p.row_o + cell * D;
-                    *ml = reinterpret_cast<const float*>(p.row_ml + cell);
-                    *to_l = 1;
-                    return;
-                }
-                const int k = first ? i : i - pre.n, block_rows = at.tiles ? p.tile_rows : kAttnCols;
-                const float* slot = at.partial + (int64_t)(2 * (s.c0 + k) + (k == 0 ? 1 : 0)) * (block_rows * (D + 2));
-                *o = slot + s.row * D;
-                *ml = slot + block_rows * D + s.row;
-                *to_l = block_rows;
-            };
+    for (int e = 0; e < V; ++e) acc[e] = 0.f;
+    if (r < p.group) {
+        // (half of the lanes for each of the two)
+        SharedParts mine{0, 0, 0};
+        if (lane >= 16 || of.y >= 0) mine = shared_parts(p, lane < 16, lane < 16 ? of.y : of.x, t, head, r);
+        const SharedParts pre{__shfl_sync(0xffffffffu, mine.n, 0), __shfl_sync(0xffffffffu, mine.c0, 0), __shfl_sync(0xffffffffu, mine.row, 0)};
+        const SharedParts own{__shfl_sync(0xffffffffu, mine.n, 16), __shfl_sync(0xffffffffu, mine.c0, 16), __shfl_sync(0xffffffffu, mine.row, 16)};
+        const int n = pre.n + own.n;
+        // part i: where its o lies, and its m and l
+        const auto find = [&](int i, const float** o, const float** ml, int* to_l) {
+            const bool first = i < pre.n;
+            const SharedParts s = first ? pre : own;
+            const SharedLaunch& at = first ? p.prefix : p.own;
+            if (s.n == 1) {
+                const int64_t cell = ((int64_t)(first ? 0 : 1) * p.T + t) * p.h_q + head * p.group + r;
+                *o = p.row_o + cell * D;
+                *ml = reinterpret_cast<const float*>(p.row_ml + cell);
+                *to_l = 1;
+                return;
+            }
+            const int k = first ? i : i - pre.n, block_rows = 1 << (at.tiles ? p.log2_tile_rows : 3);
+            const float* slot = at.partial + (int64_t)(2 * (s.c0 + k) + (k == 0 ? 1 : 0)) * (block_rows * (D + 2));
+            *o = slot + s.row * D;
+            *ml = slot + block_rows * D + s.row;
+            *to_l = block_rows;
+        };
+        for (int at = 0; at < n; at += 32) {                         // 32 parts at a time, a lane each; m, and what it scales, follow
             const float *o = nullptr, *ml = nullptr;
             int to_l = 0;
-            for (int i = lane; i < n; i += 32) {
-                find(i, &o, &ml, &to_l);
-                m = fmaxf(m, *ml);
+            float m_part = -INFINITY, l_part = 0.f;
+            if (at + lane < n) {
+                find(at + lane, &o, &ml, &to_l);
+                m_part = ml[0];
+                l_part = ml[to_l];
             }
+            float top = m_part;
 #pragma unroll
-            for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-            for (int at = sub; at < n; at += 32 * W) {                   // 32 parts' weights side by side, then their values
-                const int mine = at + lane * W, here = min(32, (n - at + W - 1) / W);
-                float f = 0.f;
-                if (mine < n) {
-                    find(mine, &o, &ml, &to_l);
-                    f = exp2_fast(ml[0] - m);
-                    l += ml[to_l] * f;
-                }
-#pragma unroll 4
-                for (int j = 0; j < here; ++j) {
-                    const float* from = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(o), j)) + V * lane;
-                    const float fj = __shfl_sync(0xffffffffu, f, j);
-                    float y[V];
-                    if constexpr (V == 2) *reinterpret_cast<float2*>(y) = *reinterpret_cast<const float2*>(from);
-                    else
+            for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+            top = fmaxf(top, m);
+            const float back = exp2_fast(m - top), f = exp2_fast(m_part - top);
+            m = top;
+            l = l * back + l_part * f;
 #pragma unroll
-                        for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(y + e) = *reinterpret_cast<const float4*>(from + e);
+            for (int e = 0; e < V; ++e) acc[e] *= back;
+            const int here = min(32, n - at);
+#pragma unroll (V == 8 ? 4 : 8)
+            for (int j = sub; j < here; j += W) {
+                const float* from = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(o), j)) + V * lane;
+                const float fj = __shfl_sync(0xffffffffu, f, j);
+                float y[V];
+                if constexpr (V == 2) *reinterpret_cast<float2*>(y) = *reinterpret_cast<const float2*>(from);
+                else
 #pragma unroll
-                    for (int e = 0; e < V; ++e) acc[e] = fmaf(y[e], fj, acc[e]);
-                }
+                    for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(y + e) = *reinterpret_cast<const float4*>(from + e);
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] = fmaf(y[e], fj, acc[e]);
             }
-#pragma unroll
-            for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
         }
-        if (W > 1) {
-            __syncthreads();
 #pragma unroll
-            for (int e = 0; e < V; ++e) sums[warp][e * 32 + lane] = acc[e];
-            if (lane == 0) sums_l[warp] = l;
-            __syncthreads();
-            if (sub == 0)
+        for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);   // (each of the W warps has it whole)
+    }
+    if (W > 1) {
+        __syncthreads();
 #pragma unroll
-                for (int w = 1; w < W; ++w) {
-                    l += sums_l[warp + w];
+        for (int e = 0; e < V; ++e) sums[warp][e * 32 + lane] = acc[e];
+        __syncthreads();
+        if (sub == 0)
 #pragma unroll
-                    for (int e = 0; e < V; ++e) acc[e] += sums[warp + w][e * 32 + lane];
-                }
-        }
-        if (sub == 0 && r < p.group) {
-            const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-            __half* to = p.out + (int64_t)t * p.out_ld + (int64_t)(head * p.group + r) * D + V * lane;
+            for (int w = 1; w < W; ++w)
 #pragma unroll
-            for (int e = 0; e < V; e += 2) *reinterpret_cast<__half2*>(to + e) = __floats2half2_rn(acc[e] * inv, acc[e + 1] * inv);
-        }
+                for (int e = 0; e < V; ++e) acc[e] += sums[warp + w][e * 32 + lane];
+    }
+    if (sub == 0 && r < p.group) {
+        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+        __half* to = p.out + (int64_t)t * p.out_ld + (int64_t)(head * p.group + r) * D + V * lane;
+#pragma unroll
+        for (int e = 0; e < V; e += 2) *reinterpret_cast<__half2*>(to + e) = __floats2half2_rn(acc[e] * inv, acc[e + 1] * inv);
     }
 }
 

@@ -49,6 +49,8 @@ template <int D> struct TileShape {
 constexpr int kTileThreads = 640;
 constexpr int kTileOverhead = 6;                                         // a segment without steps, in steps (three ragged prompts of up to 4096: 444 us with 5, 447 with 6, 450 with 7, 455 with 8; a prompt of 4096: 166, 168, 168, 169)
 
+constexpr int kSharedTileSpan = 8;                                       // the least span of the stretches of paged_shared.cuh: a part of a tile is up to 256 rows to write and to join
+
 struct TileSegment {
     int32_t head, row0, n_rows, t0, pos0, end, step0, n, slot;           // rows of the sequence row0 .. (n_rows of it), row 0's token and position, keys [.., end) that one of them sees, steps step0 .. + n
     int64_t table;                                                       // (offset of the sequence's row of the page table)
@@ -205,7 +207,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
-    const int64_t total = (int64_t)pre[n_seqs] * bt.h_kv, span = max((total + p.grid - 1) / p.grid, (int64_t)1);
+    const int64_t total = (int64_t)pre[n_seqs] * bt.h_kv, span = max((total + p.grid - 1) / p.grid, (int64_t)(KIND == kAttnShared ? kSharedTileSpan : 1));
     const int64_t w_first = (int64_t)blockIdx.x * span, w_end = min(total, w_first + span);
     if (KIND != kAttnShared && tid == 16 * 32) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
 
@@ -404,6 +406,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tiles_kernel(const Page
                     for (int d = 0; d < D; d += 32) {
                         uint32_t o[32];
                         tmem_ld32(to + d, o);
+                        if (KIND == kAttnShared && rr >= s.n_rows) continue;   // (nobody reads it)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) store32(part + row * D + d + 8 * e, o + 8 * e);
                     }

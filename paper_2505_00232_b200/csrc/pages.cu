@@ -121,7 +121,7 @@ extern "C" ql_status qlinear_paged_summarise(qlinear_paged_t h, const int32_t* t
     p.scales = scales;
     // T rows of B sequences lie in T / page_size + 2 B pages at most
     const int64_t pages = std::min<int64_t>(((int64_t)T >> (h->log2_blocks + 4)) + 2ll * B, T);
-    const unsigned grid = (unsigned)std::min<int64_t>(pages, 4ll * h->shared.sms);
+    const unsigned grid = (unsigned)std::min<int64_t>(pages, (h->d.d_h == 256 ? 2ll : 4ll) * h->shared.sms);
     const auto kernel = h->d.d_h == 64 ? paged_bounds_kernel<64> : h->d.d_h == 128 ? paged_bounds_kernel<128> : paged_bounds_kernel<256>;
     return launched(launch(kernel, p, dim3(grid), dim3(kBoundsThreads), (2 * B + 1) * 4, static_cast<cudaStream_t>(stream), 1, h->pdl));
 }
@@ -155,9 +155,10 @@ extern "C" ql_status qlinear_paged_select(qlinear_paged_t h, const void* q, int6
     p.q = static_cast<const __half*>(q); p.q_ld = q_ld;
     p.bounds = static_cast<const int8_t*>(bounds); p.scales = scales; p.pages = pages;
     p.group = h_q / h->d.h_kv; p.budget = budget; p.first = first; p.recent = recent;
-    // CTAs of a row and KV head: more while they would not fill the SMs and have 64 columns left each, and as many as hold the keys
+    // CTAs of a row and KV head: more while they would not fill the SMs twice and have 64 columns left each, and as many as hold the keys (us, clusters of 1, 2, 4, 8: one row of 8 heads and 2048 pages 23.1, 15.6, 11.9,
+    // 10.3; 32 ragged rows of up to 1024 pages 16.5, 14.9, 17.2, 24.2; 16 rows of 4 heads of 256 and 1000 pages 22.2, 15.9, 13.4, 14.3)
     int cluster = 1;
-    while (cluster < 8 && (int64_t)T * h->d.h_kv * cluster <= h->shared.sms && table_width / (2 * cluster) >= 64) cluster *= 2;
+    while (cluster < 8 && (int64_t)T * h->d.h_kv * cluster <= 2 * h->shared.sms && table_width / (2 * cluster) >= 64) cluster *= 2;
     p.gathered = table_width <= kSelectGathered;
     while (!p.gathered && (table_width + cluster - 1) / cluster > kSelectMostColumns / 8) cluster *= 2;
     p.share = std::max((table_width + cluster - 1) / cluster, 1);

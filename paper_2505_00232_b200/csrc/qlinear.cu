@@ -59,6 +59,7 @@ struct Config {
     int force_ks;            // QLINEAR_GEMV_KS: forced K split of the cluster decode kernel (0 = planned)
     int mid_max_m;           // QLINEAR_MID_MAX_M: largest M up to 64 that the kernels for a batch of tokens may serve (0: none); see takes_mid, narrow_can
     int narrow;              // QLINEAR_GEMM_NARROW: 0 gemm_narrow.cuh serves no call, 1 by the rules (default), 2 every call that it can serve
+    int paged_shared;        // QLINEAR_PAGED_SHARED: shared beginnings 0 by no call (qlinear_paged_attention serves them), 1 by the kernel of few rows where it can, 2 by that of many; -1 by the rules (default)
     bool xdirect;            // QLINEAR_GEMV_XDIRECT: x fragments straight from global memory
     int kernel;              // QLINEAR_GEMV_KERNEL: 0 / 1 cluster kernel (default), 2 streaming kernel
     int stream_ctas_per_sm, stream_stages;
@@ -80,6 +81,7 @@ void load_config()
     c.mid_max_m = env_int("QLINEAR_MID_MAX_M", 64);
     c.narrow = env_int("QLINEAR_GEMM_NARROW", 1);
     c.xdirect = env_int("QLINEAR_GEMV_XDIRECT", 1) != 0;
+    c.paged_shared = env_int("QLINEAR_PAGED_SHARED", -1);
     const char* kc = std::getenv("QLINEAR_GEMV_KERNEL");
     c.kernel = !kc ? 0 : !std::strcmp(kc, "cluster") ? 1 : !std::strcmp(kc, "stream") ? 2 : 0;
     c.stream_ctas_per_sm = std::max(1, std::min(4, env_int("QLINEAR_STREAM_CTAS_PER_SM", 3)));
@@ -1132,6 +1134,7 @@ inline bool device_timed_out(const qlinear_s* h)
 
 namespace ql {
 bool pdl_enabled() { return config().pdl; }
+int paged_shared_choice() { return config().paged_shared; }
 ql_status device_sms(int device, int* sms)
 {
     static std::atomic<int> known[kMaxDevices];
