@@ -428,7 +428,7 @@ size_t qlinear_paged_attention_selected_workspace(qlinear_paged_t h, int32_t h_q
 ql_status qlinear_paged_attention_selected(qlinear_paged_t h, const void* q_dev, int64_t q_ld, void* out_dev, int64_t out_ld, int32_t h_q, const int32_t* pages_dev, int32_t budget,
                                            const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T,
                                            float scale, float softcap, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
-size_t qlinear_paged_attention_shared_workspace(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t T, int32_t max_q, int32_t n_groups);
+size_t qlinear_paged_attention_shared_workspace(qlinear_paged_t h, int32_t h_q, int32_t table_width, int32_t B, int32_t T, int32_t max_q, int32_t n_groups);
 ql_status qlinear_paged_attention_shared(qlinear_paged_t h, const void* q_dev, int64_t q_ld, void* out_dev, int64_t out_ld, int32_t h_q,
                                          const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T, int32_t max_q,
                                          const int32_t* group_start, const int32_t* prefix_len, int32_t n_groups, float scale, float softcap,

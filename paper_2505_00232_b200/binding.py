@@ -155,7 +155,7 @@ def _load() -> ctypes.CDLL:
     lib.qlinear_paged_attention_shared.argtypes = [vp, vp, i64, vp, i64, i32, *batch, i32, vp, vp, i32, f32, f32, vp, size, vp]
     lib.qlinear_paged_pages_workspace.argtypes = [vp]
     lib.qlinear_paged_attention_selected_workspace.argtypes = [vp, i32]
-    lib.qlinear_paged_attention_shared_workspace.argtypes = [vp, i32, i32, i32, i32, i32]
+    lib.qlinear_paged_attention_shared_workspace.argtypes = [vp, i32, i32, i32, i32, i32, i32]
     for f in ("qlinear_paged_pages_workspace", "qlinear_paged_attention_selected_workspace", "qlinear_paged_attention_shared_workspace"):
         getattr(lib, f).restype = size
     for f in ("qlinear_rope_tables", "qlinear_paged_create", "qlinear_paged_destroy", "qlinear_paged_device_status", "qlinear_paged_append", "qlinear_paged_read", "qlinear_paged_attention", "qlinear_adjust_logits",
@@ -837,7 +837,7 @@ class PagedKV:
         if h_q % self.h_kv or max_q < 0:
             raise QLinearError(QL_ERR_INVALID_ARG, where + " (query heads a multiple of the KV heads, max_q >= 0)")
         st, here = _on_stream(self.device, stream)
-        size = lib.qlinear_paged_attention_shared_workspace(self._h, h_q, batch[5], T, max_q, G)
+        size = lib.qlinear_paged_attention_shared_workspace(self._h, h_q, batch[2], batch[5], T, max_q, G)
         with here:
             if out is None:
                 out = torch.empty((T, h_q, self.d_h), dtype=torch.float16, device=self.device)

@@ -135,27 +135,6 @@ struct SharedPlan {
     int32_t group, tile_rows;
     size_t own_at, rows_at, ml_at, stretches_at, lengths_at, row_of_at, spans_at, bytes;
 };
-// What of a call does not depend on the lengths: what it needs; false for bad arguments.
-bool shared_plan(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t T, int32_t max_q, int32_t n_groups, SharedPlan* a)
-{
-    if (!h || h_q < 1 || h_q > 65536 || h_q % h->d.h_kv || B < 0 || T < 0 || n_groups < 0 || max_q < 0 || (int64_t)n_groups + B > QL_PAGED_MAX_SEQUENCES) return false;
-    const int32_t d = h->d.d_h;
-    a->group = h_q / h->d.h_kv;
-    a->tile_rows = d == 256 ? TileShape<256>::kRows : TileShape<128>::kRows;
-    a->own_tiles = (int64_t)max_q * a->group > attn_max_rows(d);
-    const auto up = [](size_t n) { return (n + 31) / 32 * 32; };
-    const size_t few = up(few_partial(h)), tiles = up((size_t)2 * h->shared.sms * a->tile_rows * (d + 2) * sizeof(float)), cells = (size_t)2 * T * h_q, V = (size_t)n_groups + B;
-    a->own_at = tiles;                                                   // (where it is a launch of its own)
-    a->rows_at = tiles + few;
-    a->ml_at = a->rows_at + up(cells * d * sizeof(float));
-    a->stretches_at = a->ml_at + up(cells * sizeof(float2));
-    a->lengths_at = a->stretches_at + up(V * sizeof(AttnStretch));
-    a->row_of_at = a->lengths_at + up((V + 1) * 4);
-    a->spans_at = a->row_of_at + up((size_t)T * sizeof(int2));
-    const size_t plain = qlinear_paged_attention_workspace(h, h_q, B, max_q);
-    a->bytes = std::max(a->spans_at + 32, plain);
-    return plain > 0;
-}
 // Which kernels take it: by estimates of the three ways' times, with the tables' columns for the lengths and the beginnings.  A launch over stretches has a fixed part (plan, ramps, join; the tiles a pipeline of their own), few rows cost
 // by their blocks of 16 tokens and 8 rows, tiles by their steps of 64 tokens.  us, plain, few rows and tiles, 8 KV heads of 128 and 4 queries each: 4 sequences over 1024 tokens 11.5, 14.9, 30.9; 16 over 2048 19.8, 20.5, 33.1;
 // 8 over 16384 41.0, 30.4, 43.4; 16 over 16384 71.5, 47.3, 44.5; two groups of 32 over 16384 259, 149, 75.  4 of 256 and 2: 4 over 16384 25.6, 18.4, 37.7; two groups of 32 257, 87, 61.  2 of 64 and 7: 8 over 16384 15.4, 18.4, 32.2; two groups of 32 50, 51, 39.
@@ -177,6 +156,29 @@ void shared_route(qlinear_paged_t h, int32_t B, int32_t T, int32_t max_q, int32_
     a->alone = choice < 0 && plain <= std::min(few, tiles);
 }
 
+// The launches of a call, from what the host knows of it; false for bad arguments.
+bool shared_plan(qlinear_paged_t h, int32_t h_q, int32_t table_width, int32_t B, int32_t T, int32_t max_q, int32_t n_groups, SharedPlan* a)
+{
+    if (!h || h_q < 1 || h_q > 65536 || h_q % h->d.h_kv || table_width < 0 || B < 0 || T < 0 || n_groups < 0 || max_q < 0 || (int64_t)n_groups + B > QL_PAGED_MAX_SEQUENCES) return false;
+    const int32_t d = h->d.d_h;
+    a->group = h_q / h->d.h_kv;
+    a->tile_rows = d == 256 ? TileShape<256>::kRows : TileShape<128>::kRows;
+    a->own_tiles = (int64_t)max_q * a->group > attn_max_rows(d);
+    a->bytes = qlinear_paged_attention_workspace(h, h_q, B, max_q);
+    shared_route(h, B, T, max_q, n_groups, table_width, a);
+    if (a->alone) return a->bytes > 0;
+    const auto up = [](size_t n) { return (n + 31) / 32 * 32; };
+    const size_t few = up(few_partial(h)), tiles = up((size_t)2 * h->shared.sms * a->tile_rows * (d + 2) * sizeof(float)), cells = (size_t)2 * T * h_q, V = (size_t)n_groups + B;
+    a->own_at = a->prefix_tiles ? tiles : 0;                             // (where it is a launch of its own)
+    a->rows_at = a->own_at + (a->own_tiles ? 0 : few);
+    a->ml_at = a->rows_at + up(cells * d * sizeof(float));
+    a->stretches_at = a->ml_at + up(cells * sizeof(float2));
+    a->lengths_at = a->stretches_at + up(V * sizeof(AttnStretch));
+    a->row_of_at = a->lengths_at + up((V + 1) * 4);
+    a->spans_at = a->row_of_at + up((size_t)T * sizeof(int2));
+    a->bytes = a->spans_at + 32;
+    return true;
+}
 template <int D>
 cudaError_t launch_join(const SharedJoinParams& j, int sms, cudaStream_t st, bool pdl)
 {
@@ -205,10 +207,10 @@ cudaError_t launch_shared(const SharedPlanParams& plan, PagedAttnParams p, const
 
 }  // namespace
 
-extern "C" size_t qlinear_paged_attention_shared_workspace(qlinear_paged_t h, int32_t h_q, int32_t B, int32_t T, int32_t max_q, int32_t n_groups)
+extern "C" size_t qlinear_paged_attention_shared_workspace(qlinear_paged_t h, int32_t h_q, int32_t table_width, int32_t B, int32_t T, int32_t max_q, int32_t n_groups)
 {
     SharedPlan a;
-    return shared_plan(h, h_q, B, T, max_q, n_groups, &a) ? a.bytes : 0;
+    return shared_plan(h, h_q, table_width, B, T, max_q, n_groups, &a) ? a.bytes : 0;
 }
 
 extern "C" ql_status qlinear_paged_attention_shared(qlinear_paged_t h, const void* q, int64_t q_ld, void* out, int64_t out_ld, int32_t h_q,
@@ -218,9 +220,8 @@ extern "C" ql_status qlinear_paged_attention_shared(qlinear_paged_t h, const voi
 {
     PagedAttnParams p{};
     SharedPlan a;
-    if (!batch_of(h, table, table_ld, table_width, kv_len, q_start, B, T, &p.batch) || !shared_plan(h, h_q, B, T, max_q, n_groups, &a) || !scores_of(scale, softcap, &p)) return QL_ERR_INVALID_ARG;
+    if (!batch_of(h, table, table_ld, table_width, kv_len, q_start, B, T, &p.batch) || !shared_plan(h, h_q, table_width, B, T, max_q, n_groups, &a) || !scores_of(scale, softcap, &p)) return QL_ERR_INVALID_ARG;
     if (n_groups > 0 && (!group_start || !prefix_len || !aligned(group_start, 4) || !aligned(prefix_len, 4))) return QL_ERR_INVALID_ARG;
-    shared_route(h, B, T, max_q, n_groups, table_width, &a);
     if (a.alone) return qlinear_paged_attention(h, q, q_ld, out, out_ld, h_q, table, table_ld, table_width, kv_len, q_start, B, T, max_q, scale, softcap, 0, workspace, workspace_bytes, stream);
     if (B == 0 || T == 0 || max_q == 0) return QL_OK;
     const int32_t d = h->d.d_h, V = n_groups + B;

@@ -723,7 +723,7 @@ PyObject* paged_attention_shared(PyObject*, PyObject* const* a, Py_ssize_t)   //
         at::Tensor made, work;
         const void* qp = q.t->data_ptr();
         void* st = stream_on(p.device);
-        const size_t bytes = serving.shared_workspace(p.h, (int32_t)q.heads, b.B, (int32_t)q.T, (int32_t)max_q, (int32_t)G);
+        const size_t bytes = serving.shared_workspace(p.h, (int32_t)q.heads, b.width, b.B, (int32_t)q.T, (int32_t)max_q, (int32_t)G);
         if (!done([&] {
                 if (make) { made = half_like(*q.t, {q.T, q.heads, p.d}); o.t = &made; o.ld = q.heads * p.d; }
                 work = made_bytes(bytes, p);

@@ -15,7 +15,7 @@ BATCH = (AT, 4, 4, AT, AT, 1, 1)
 def test_no_handle():
     assert lib.qlinear_paged_pages_workspace(None) == 0
     assert lib.qlinear_paged_attention_selected_workspace(None, 8) == 0
-    assert lib.qlinear_paged_attention_shared_workspace(None, 8, 1, 1, 1, 1) == 0
+    assert lib.qlinear_paged_attention_shared_workspace(None, 8, 1, 1, 1, 1, 1) == 0
     assert lib.qlinear_paged_fork(None, AT, AT, 4, 4, 1, AT, AT, 1, AT + 1024, 4, None) == BAD
     assert lib.qlinear_paged_release(None, AT, AT, 4, 4, 1, AT, AT, 1, None) == BAD
     assert lib.qlinear_paged_reserve(None, AT, *BATCH, AT, AT, 4096, None) == BAD

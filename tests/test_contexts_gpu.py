@@ -485,6 +485,16 @@ def test_other_streams_and_two_at_once(P, torch):
         assert torch.equal(a[0], want[0]) and torch.equal(a[1], want[1])
 
 
+def test_workspaces_by_what_a_call_needs(P, torch):
+    """Prompts, which do not share, take what attention takes; a batch over a long table more."""
+    lib = P.lib
+    cache = P.PagedKV(8, 16, 8, 128)
+    plain = lib.qlinear_paged_attention_workspace(cache._h, 32, 4, 4000)
+    assert lib.qlinear_paged_attention_shared_workspace(cache._h, 32, 300, 4, 16000, 4000, 0) == plain > 0
+    assert lib.qlinear_paged_attention_shared_workspace(cache._h, 32, 4096, 64, 64, 1, 1) > 2 * 64 * 32 * 130 * 4
+    assert lib.qlinear_paged_attention_shared_workspace(cache._h, 31, 300, 4, 4, 1, 1) == 0
+
+
 # ---------------------------------------------------------------------------- refusals
 def test_refused(P, torch):
     cache = P.PagedKV(8, 16, 2, 64)
