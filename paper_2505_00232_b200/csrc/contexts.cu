@@ -182,8 +182,8 @@ bool shared_plan(qlinear_paged_t h, int32_t h_q, int32_t table_width, int32_t B,
 template <int D>
 cudaError_t launch_join(const SharedJoinParams& j, int sms, cudaStream_t st, bool pdl)
 {
-    // a row's parts are up to one per CTA: warps for them while the SMs have room, 32 each (us, 1, 2, 4, 8 warps a row: 2048 rows of 128 with 20 parts 10.5, 7.1, 10.2, 13.2; 1536 of 256 with 13 10.9, 9.1, 8.5, 11.6; one of 128
-    // with 128 parts by the row 40 and more, by eight warps 4)
+    // a row's parts are up to one per CTA: warps for them while the SMs have room, 32 each (us, 1, 2, 4, 8 warps a row: 2048 rows of 128 with 20 parts 10.5, 7.1, 10.2, 13.2; 1536 of 256 with 13 10.9, 9.1, 8.5, 11.6; 48 rows
+    // with 131 parts: the whole call 76 with one, 33 with eight and parts of 8 steps at least)
     const int64_t rows = (int64_t)j.T * j.h_q, room = 32ll * sms;
     const auto go = [&](auto kernel, int w) { return launch(kernel, j, dim3(j.T, j.h_kv, (j.group + 8 / w - 1) / (8 / w)), dim3(256), 0, st, 1, pdl); };
     if (rows * 8 <= room || j.group <= 1) return go(paged_shared_join_kernel<D, 8>, 8);

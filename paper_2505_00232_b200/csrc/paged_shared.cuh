@@ -5,6 +5,9 @@
 //
 // The plan is a kernel of its own, one CTA: stretches, their lengths as the kernels number their segments, and each row's sequence, from the arrays on the device.  The length of a shared beginning is cut to a
 // multiple of 64 tokens (a step of the tiles) and to what all rows of the group see, so that nothing of it needs a mask; what is cut off belongs to what follows, from each sequence's own pages.
+//
+// 64 sequences of up to 1500 tokens of their own over 32768, 8 KV heads of 128 and 4 queries each: plan 4.8 us, tiles 52 (10 until the first scores are weighed, 28 steps of 1.28, 5 for the sums to leave), few rows 21, join 7;
+// qlinear_paged_attention of the same 480.  The sums of cut tiles are 21 MB: laid with eight elements of all rows side by side they leave in 1.7 us less and take the join 1 to 4 more.
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
