@@ -62,7 +62,7 @@ __device__ __forceinline__ int bounds_scan(int v, int* total, int* sums)
 // instructions on what it holds, and at the end (the smallest as the largest of the negated: one operation for both) 8 lanes share the values out among them: each exchange halves what a lane goes on with (28
 // exchanges for 32 pairs, not 96), and a lane is left with elements in a row, which it encodes and stores.
 // Every CTA numbers the touched columns of the batch (a scan) and takes pages in turn, 32 of them looked up side by side.
-// Bound: instruction issue (68 % of the slots: 22 instructions for eight elements, half of them the unpack): the keys of 27000 tokens, 8 heads of 128, in 12.7 us (15 MB read, 2.6 at the copy rate), 14 with two blocks' loads
+// Bound: instruction issue (68 % of the slots: 22 instructions for eight elements, half of them the unpack): the keys of 29500 tokens, 8 heads of 128, in 12.7 us (17 MB read, 2.6 at the copy rate), 14 with two blocks' loads
 // in flight or their lines prefetched; for a generated token a sequence (7.3 us) the chain length -> column -> page -> keys.
 template <int D>
 __global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : 4) paged_bounds_kernel(const PagedBoundsParams p)

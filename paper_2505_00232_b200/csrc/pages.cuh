@@ -5,7 +5,7 @@
 // come: needs are numbered in the order of sequences and columns, free pages in their own, and need j gets free page j.
 //
 // Bound: latencies.  The decisions are one CTA's (a scan over refs and a scan over the columns that new tokens touch; what they read is a few hundred kilobytes), the
-// copying of bytes, bound by HBM, is a second launch's over all SMs (us, a pool of 16000 pages: 4.5 to decide what moves, 5 to 6 what 256 sequences get, 2 the launch behind it).
+// copying of bytes, bound by HBM, is a second launch's over all SMs (us: 4.5 to decide what moves of 4000 pages, 6 what 256 sequences get of 3300, 2 the launch behind it).
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
