@@ -159,7 +159,7 @@ def test_release(P, torch, W):
 
 # ---------------------------------------------------------------------------- reserve
 CASES = [  # heads, d, page, sequences, pages, new tokens
-    (2, 128, 16, 5, 60, 1), (1, 64, 64, 40, 300, 1), (4, 256, 32, 3, 40, 70), (3, 64, 128, 7, 60, 129), (1, 64, 16, 200, 9000, 40), (1, 64, 16, 2, 40000, 9000)]
+    (2, 128, 16, 5, 60, 1), (1, 64, 64, 40, 300, 1), (4, 256, 32, 3, 40, 70), (3, 64, 128, 7, 60, 129), (1, 64, 16, 200, 9000, 40), (1, 64, 16, 2, 40000, 9000), (8, 128, 64, 60, 600, 30)]
 
 
 @pytest.mark.parametrize("h_kv,d,page,B,n_pages,new", CASES)
