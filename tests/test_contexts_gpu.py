@@ -495,6 +495,99 @@ def test_workspaces_by_what_a_call_needs(P, torch):
     assert lib.qlinear_paged_attention_shared_workspace(cache._h, 31, 300, 4, 4, 1, 1) == 0
 
 
+# ---------------------------------------------------------------------------- large numbers
+def test_two_thousand_sequences_that_share(P, torch):
+    """As many sequences as a call takes (with its groups), all of the calls on them; a sample of the rows against 64 bits."""
+    rng = np.random.default_rng(21)
+    h_q, h_kv, d, page = 4, 2, 64, 16
+    groups = [(96, [int(n) for n in rng.integers(1, 40, 20)]) for _ in range(96)]
+    cache, batch, kv, start, prefix = sharing(P, torch, groups, page, h_kv, d, [1 + b % 2 for b in range(1952)], seed=22, alone=[int(n) for n in rng.integers(1, 90, 32)])
+    assert len(batch.lens) + len(groups) == 2048
+    q = f16(rng, batch.T, h_q, d)
+    dq = torch.from_numpy(q).cuda()
+    rows = [r for r in batch.rows() if r[1] % 37 == 0 or r[1] > 1940]
+    want, tol = attention64(q, kv, batch, d ** -0.5, rows=rows, max_q=10 ** 6)
+    check(cache.attention_shared(dq, *batch.args, batch.max_q, start, prefix).cpu().numpy(), want, tol, rows)
+    b = cache.key_bounds()
+    cache.summarise(b, *batch.whole, sum(batch.lens))
+    W = batch.table.shape[1]
+    pages = cache.select(dq, b, *batch.args, W)                          # (every page)
+    check(cache.attention_selected(dq, pages, *batch.args).cpu().numpy(), want, tol, rows)
+    few = cache.select(dq, b, *batch.args, 3).cpu().numpy()
+    bounds, scales = (x.cpu().numpy() for x in b)
+    for t, s, pos in rows:
+        assert (few[t] == chosen64(q[t], h_kv, bounds, scales, batch.table[s], pos, page, batch.n_pages, 3, 1, 1)).all()
+
+
+@pytest.mark.parametrize("h_q,h_kv,d,page", [(64, 1, 128, 1024), (40, 40, 64, 16), (96, 2, 256, 64)])
+def test_many_heads_that_share(P, torch, h_q, h_kv, d, page):
+    """Many query heads a KV head, many KV heads, large pages: shared beginnings, lists, choices."""
+    rng = np.random.default_rng(h_q)
+    cache, batch, kv, start, prefix = sharing(P, torch, [(1100, [5, 90, 700]), (70, [3, 4])], page, h_kv, d, 1, seed=h_q, before=1, behind=1)
+    q = f16(rng, batch.T, h_q, d)
+    dq = torch.from_numpy(q).cuda()
+    want, tol = attention64(q, kv, batch, d ** -0.5, max_q=10 ** 6)
+    check(cache.attention_shared(dq, *batch.args, 1, start, prefix).cpu().numpy(), want, tol, batch.rows())
+    b = cache.key_bounds()
+    cache.summarise(b, *batch.whole, sum(batch.lens))
+    bounds, scales = (x.cpu().numpy() for x in b)
+    pages = cache.select(dq, b, *batch.args, 2, 1, 0)
+    got, g = cache.attention_selected(dq, pages, *batch.args).cpu().numpy().astype(np.float64), h_q // h_kv
+    pages = pages.cpu().numpy()
+    for t, s, pos in batch.rows():
+        assert (pages[t] == chosen64(q[t], h_kv, bounds, scales, batch.table[s], pos, page, batch.n_pages, 2, 1, 0)).all()
+        for h in range(h_kv):
+            tokens = [j for c in pages[t, h] if c >= 0 for j in range(c * page, min((c + 1) * page, pos + 1))]
+            y, e = attended64(q[t, g * h:g * h + g], kv[s][0][tokens, h], kv[s][1][tokens, h], d ** -0.5)
+            assert (np.abs(got[t, g * h:g * h + g] - y) <= e).all()
+
+
+def test_a_prompt_over_listed_pages(P, torch):
+    """Every row of a prompt with a list of its own: more segments than CTAs by far."""
+    rng = np.random.default_rng(31)
+    h_q, h_kv, d, page, n = 4, 2, 128, 32, 2500
+    batch = Batch(torch, [n, 300], [n, 300], page)
+    cache, kv = filled(P, torch, batch, h_kv, d)
+    b = cache.key_bounds()
+    cache.summarise(b, *batch.args, batch.T)
+    q = f16(rng, batch.T, h_q, d)
+    dq = torch.from_numpy(q).cuda()
+    pages = cache.select(dq, b, *batch.args, 5, 1, 2)
+    got, listed = cache.attention_selected(dq, pages, *batch.args).cpu().numpy().astype(np.float64), pages.cpu().numpy()
+    for t, s, pos in batch.rows()[::29]:
+        for h in range(h_kv):
+            tokens = [j for c in listed[t, h] if c >= 0 for j in range(c * page, min((c + 1) * page, pos + 1))]
+            y, e = attended64(q[t, 2 * h:2 * h + 2], kv[s][0][tokens, h], kv[s][1][tokens, h], d ** -0.5)
+            assert (np.abs(got[t, 2 * h:2 * h + 2] - y) <= e).all()
+
+
+def test_scores_of_millions(P, torch):
+    """Large queries and scales: differences of scores are taken before they are scaled, in the join as well (weights of one token, the others vanish)."""
+    rng = np.random.default_rng(32)
+    cache, batch, kv, start, prefix = sharing(P, torch, [(900, [100, 40, 300])], 16, 2, 128, 1, seed=7)
+    q = (f16(rng, batch.T, 8, 128).astype(np.float32) * 100).astype(np.float16)
+    W = batch.table.shape[1]
+    pages = dev(torch, np.broadcast_to(np.arange(W), (batch.T, 2, W)))
+    apart = np.zeros((batch.T, 8), bool)                                 # heads whose largest score stays the largest whatever the keys' rounding (2^-11 of each product) does to two of them
+    best = np.zeros((batch.T, 8, 128))
+    for r, s, pos in batch.rows():
+        for h in range(8):
+            k = kv[s][0][:pos + 1, h // 4]
+            x = k @ q[r, h].astype(np.float64)
+            top = np.sort(x)[-2:]
+            apart[r, h] = top[1] - top[0] > 2 * 2.0 ** -11 * (np.abs(k) @ np.abs(q[r, h]).astype(np.float64)).max() + 1
+            best[r, h] = kv[s][1][x.argmax(), h // 4]
+    assert apart.mean() > 0.5
+    calls = lambda scale: (cache.attention_selected(torch.from_numpy(q).cuda(), pages, *batch.args, scale=scale), cache.attention_shared(torch.from_numpy(q).cuda(), *batch.args, 1, start, prefix, scale=scale))
+    for scale in (1e3, 1e15):                                            # one token's weight is left: its value, rounded to fp16 with the weight's own rounding on the way
+        for y in calls(scale):
+            y = y.cpu().numpy().astype(np.float64)
+            assert (np.abs(y - best) <= 4 * 2.0 ** -11 * np.abs(best))[apart].all() and np.isfinite(y).all()
+    want, tol = attention64(q, kv, batch, 0.0, max_q=10 ** 6)
+    for y in calls(0.0):
+        check(y.cpu().numpy(), want, tol, batch.rows())
+
+
 # ---------------------------------------------------------------------------- refusals
 def test_refused(P, torch):
     cache = P.PagedKV(8, 16, 2, 64)

@@ -240,6 +240,40 @@ def test_compact(P, torch, h_kv, d, page, n_pages, live):
     assert again.tolist() == [x if c > 0 else -1 for x, c in enumerate(new_refs)] and t.tolist() == new_table and torch.equal(cache.pool[new], before[old])
 
 
+def test_two_thousand_sequences(P, torch):
+    """As many sequences as the calls take: forked from 7, written apart, given back."""
+    rng = np.random.default_rng(8)
+    n_pages, page, W = 9000, 16, 6
+    refs, table = np.zeros(n_pages, np.int64), np.full((7, W), -1, np.int64)
+    lens = [1, 16, 40, 17, 64, 33, 80]
+    order = rng.permutation(n_pages)
+    for b, n in enumerate(lens):
+        k = -(-n // page)
+        table[b, :k] = order[10 * b:10 * b + k]
+        refs[table[b, :k]] = 1
+    parents = rng.integers(0, 7, 2048)
+    held = [lens[p] for p in parents]
+    want, want_refs = forked(refs, table, parents, held, page)
+    cache, before = full(P, torch, n_pages, page, 1, 64)
+    r = dev(torch, refs)
+    t = cache.fork(r, dev(torch, table), dev(torch, parents), dev(torch, held))
+    assert t.tolist() == want and r.tolist() == want_refs
+    kv_len = [n + 1 + i % 3 for i, n in enumerate(held)]
+    starts = np.concatenate([[0], np.cumsum([1 + i % 3 for i in range(2048)])]).tolist()
+    want, want_refs, missing, copies = reserved(want_refs, want, kv_len, starts, starts[-1], page)
+    assert missing == 0 and len(copies) > 1000
+    assert cache.reserve(r, t, dev(torch, kv_len), dev(torch, starts), starts[-1]).tolist() == [0]
+    assert t.tolist() == want and r.tolist() == want_refs
+    assert all(torch.equal(cache.pool[to], before[x]) for x, to, _ in copies[::41])
+    rows = rng.permutation(2048)[:2000]
+    cache.release(r, t, dev(torch, rows))
+    for b in rows:
+        for x in want[b]:
+            if x >= 0:
+                want_refs[x] -= 1
+    assert r.tolist() == want_refs
+
+
 # ---------------------------------------------------------------------------- refusals
 def test_refused(P, torch):
     cache = P.PagedKV(8, 16, 2, 64)
