@@ -135,9 +135,10 @@ struct SharedPlan {
     int32_t group, tile_rows;
     size_t own_at, rows_at, ml_at, stretches_at, lengths_at, row_of_at, spans_at, bytes;
 };
-// Which kernels take it: by estimates of the three ways' times, with the tables' columns for the lengths and the beginnings.  A launch over stretches has a fixed part (plan, ramps, join; the tiles a pipeline of their own), few rows cost
-// by their blocks of 16 tokens and 8 rows, tiles by their steps of 64 tokens.  us, plain, few rows and tiles, 8 KV heads of 128 and 4 queries each: 4 sequences over 1024 tokens 11.5, 14.9, 30.9; 16 over 2048 19.8, 20.5, 33.1;
-// 8 over 16384 41.0, 30.4, 43.4; 16 over 16384 71.5, 47.3, 44.5; two groups of 32 over 16384 259, 149, 75.  4 of 256 and 2: 4 over 16384 25.6, 18.4, 37.7; two groups of 32 257, 87, 61.  2 of 64 and 7: 8 over 16384 15.4, 18.4, 32.2; two groups of 32 50, 51, 39.
+// Which kernels take it: by estimates of the three ways' times, with the table's columns for the lengths and three quarters of them for the beginnings.  A launch over stretches has a fixed part (plan, ramps, join; the tiles a pipeline of their
+// own), few rows cost by their blocks of 16 tokens and 8 rows, tiles by their steps of 64 tokens.  us, plain, few rows and tiles, 8 KV heads of 128 and 4 queries each: 4 sequences over 1024 tokens 11.5, 14.9, 30.9; 16 over 2048 19.8, 20.5, 33.1;
+// 8 over 16384 41.0, 30.4, 43.4; 16 over 16384 71.5, 47.3, 44.5; two groups of 32 over 16384 259, 149, 75; 16 drafted tokens each, 4 over 16384 81.9, -, 43.6.  4 of 256 and 2: 4 over 16384 25.6, 18.4, 37.7; two groups of 32 257, 87, 61.
+// 2 of 64 and 7: 8 over 16384 15.4, 18.4, 32.2; two groups of 32 50, 51, 39.  What the estimate does not know is how long the beginnings are: 64 sequences of 2000 tokens of their own over 512 take 58.6 by its choice and 54.5 plain.
 void shared_route(qlinear_paged_t h, int32_t B, int32_t T, int32_t max_q, int32_t n_groups, int32_t table_width, SharedPlan* a)
 {
     const int32_t d = h->d.d_h, V = n_groups + B, choice = paged_shared_choice();
@@ -149,9 +150,11 @@ void shared_route(qlinear_paged_t h, int32_t B, int32_t T, int32_t max_q, int32_
     if (a->alone) return;
     const int64_t group_rows = (all_rows + n_groups - 1) / n_groups, rows = (int64_t)max_q * a->group;
     const auto pieces_of = [](int64_t n, int64_t size) { return (double)((n + size - 1) / size); };
-    const double per_block = (d == 64 ? 0.085 : d == 128 ? 0.15 : 0.14) * h->d.h_kv * held / kPagedBlock / few_ctas(h, V), per_step = 1.2 * h->d.h_kv * held / 64 / h->shared.sms;
-    const double plain = a->own_tiles ? 18 + per_step * B * pieces_of(rows, a->tile_rows) : 9.5 + per_block * B * pieces_of(rows, kAttnCols);
-    const double few = a->own_tiles ? INFINITY : 13.5 + per_block * n_groups * pieces_of(group_rows, kAttnCols), tiles = 28 + per_step * n_groups * pieces_of(group_rows, a->tile_rows);
+    const double per_block = (d == 64 ? 0.085 : d == 128 ? 0.15 : 0.14) * h->d.h_kv * held / kPagedBlock / few_ctas(h, V), per_step = (d == 256 ? 1.4 : 1.1) * h->d.h_kv * held / 64 / h->shared.sms;
+    const double beginning = 0.75, each = a->own_tiles ? per_step * B * pieces_of(rows, a->tile_rows) : per_block * B * pieces_of(rows, kAttnCols);   // (of every sequence's whole length)
+    const double plain = (a->own_tiles ? 23 : 9.5) + each;
+    const double few = a->own_tiles ? INFINITY : 13.5 + (1 - beginning) * each + beginning * per_block * n_groups * pieces_of(group_rows, kAttnCols);
+    const double tiles = 28 + (1 - beginning) * each + beginning * per_step * n_groups * pieces_of(group_rows, a->tile_rows);
     a->prefix_tiles = choice == 2 || a->own_tiles || (choice != 1 && tiles < few);
     a->alone = choice < 0 && plain <= std::min(few, tiles);
 }
