@@ -10,6 +10,7 @@
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include "dequant.cuh"
@@ -36,19 +37,19 @@ __device__ __forceinline__ int touched_columns(const PagedBatch& p, int b, int* 
     return max(min(((len - 1) >> log2_page) + 1, p.table_width) - *first, 0);
 }
 // Exclusive sum over the CTA's kBoundsThreads threads, the whole sum in *total.
-__device__ __forceinline__ int bounds_scan(int v, int* total, int* sums)
+__device__ __forceinline__ long long bounds_scan(long long v, long long* total, long long* sums)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int run = v;
+    long long run = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, run, o);
+        const long long u = __shfl_up_sync(0xffffffffu, run, o);
         if (lane >= o) run += u;
     }
     __syncthreads();
     if (lane == 31) sums[warp] = run;
     __syncthreads();
-    int before = 0, all = 0;
+    long long before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < kBoundsWarps; ++w) {
         if (w == warp) before = all;
@@ -69,21 +70,25 @@ __global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : 4) paged_bounds
 {
     constexpr int NB = D / 64, kBlock = paged_block_bytes(D), kPairs = 16 * NB;   // pairs of elements of a lane: largest and smallest
     extern __shared__ int pre[];                                         // [B + 1] touched columns before sequence b, [B] the first of them
-    __shared__ int sums[kBoundsWarps];
+    __shared__ long long sums[kBoundsWarps];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const PagedBatch& bt = p.batch;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t = lane >> 2, c = lane & 3, log2_page = bt.log2_blocks + 4;
     int* first_of = pre + bt.B + 1;
-    int total = 0;
+    long long columns = 0;
     if (tid == 0) pre[0] = 0;
     for (int b0 = 0; b0 < bt.B; b0 += kBoundsThreads) {
         const int b = b0 + tid;
-        int first = 0, all;
-        const int n = b < bt.B ? touched_columns(bt, b, &first) : 0, before = bounds_scan(n, &all, sums);
-        if (b < bt.B) { pre[b + 1] = total + before + n; first_of[b] = first; }
-        total += all;
+        int first = 0;
+        long long all;
+        const int n = b < bt.B ? touched_columns(bt, b, &first) : 0;
+        const long long before = bounds_scan(n, &all, sums);
+        if (b < bt.B) { pre[b + 1] = (int)(columns + before + n); first_of[b] = first; }
+        columns += all;
     }
+    if (columns > INT_MAX) return;                                       // (rows named more than once, against the rules: they lie in T / page_size + 2 B columns at most)
+    const int total = (int)columns;
     __syncthreads();
     const int mine = total > (int)blockIdx.x ? (total - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;   // pages of this CTA: blockIdx.x, + gridDim.x, ...
     for (int base = 0; base < mine; base += 32) {

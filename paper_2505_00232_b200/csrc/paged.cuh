@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_read_blocks_kernel(const 
 {
     constexpr int NB = D / 64, kBlock = paged_block_bytes(D), kWarps = kPagedThreads / 32;
     extern __shared__ int pre[];                                         // [B + 1] blocks before sequence b
-    __shared__ int sums[kWarps];
+    __shared__ long long sums[kWarps];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const PagedBatch& bt = p.batch;
@@ -295,19 +295,20 @@ __global__ void __launch_bounds__(kPagedThreads) paged_read_blocks_kernel(const 
         *phase = (int)(*p0 & 15);
         return rows;
     };
-    int total = 0;
+    long long total = 0;
     if (tid == 0) pre[0] = 0;
     for (int b0 = 0; b0 < bt.B; b0 += kPagedThreads) {
         const int b = b0 + tid;
-        int t0, phase, run = 0;
+        int t0, phase;
         int64_t p0;
+        long long run = 0;
         if (b < bt.B) {
             const int rows = rows_of(b, &t0, &p0, &phase);
             run = rows > 0 ? (phase + rows + 15) >> 4 : 0;
         }
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int u = __shfl_up_sync(0xffffffffu, run, o);
+            const long long u = __shfl_up_sync(0xffffffffu, run, o);
             if (lane >= o) run += u;
         }
         __syncthreads();
@@ -318,11 +319,12 @@ __global__ void __launch_bounds__(kPagedThreads) paged_read_blocks_kernel(const 
             if (w < warp) run += sums[w];
             total += sums[w];
         }
-        if (b < bt.B) pre[b + 1] = run;
+        if (b < bt.B) pre[b + 1] = (int)run;
     }
+    if (total > INT_MAX) return;                                         // (rows named more than once, against the rules: they lie in T / 16 + 2 B blocks at most)
     __syncthreads();
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    for (int64_t item = (int64_t)blockIdx.x * kWarps + warp; item < (int64_t)total * h_kv; item += (int64_t)gridDim.x * kWarps) {
+    for (int64_t item = (int64_t)blockIdx.x * kWarps + warp; item < total * h_kv; item += (int64_t)gridDim.x * kWarps) {
         const int k = (int)(item / h_kv), head = (int)(item - (int64_t)k * h_kv);
         int b = 0, hi = bt.B, t0, phase;                                 // pre[b] <= k < pre[hi]
         while (hi - b > 1) {

@@ -193,10 +193,15 @@ __device__ __forceinline__ void attn_scan(const PagedAttnParams& p, int* pre)
     __shared__ int warp_sum[kAttnWarps];
     const int B = p.batch.B, tid = threadIdx.x, per = (B + 255) / 256, lo = min(B, tid * per), hi = min(B, lo + per);
     int sum = 0, first;
+    unsigned long long wide = 0;
     for (int b = lo; b < hi; ++b) {
         const int blocks = KIND == kAttnListed ? listed_blocks(p, b) : attn_blocks(p, b, &first);
         int n = blocks > 0 ? blocks + kAttnOverhead : 0;
-        if (KIND == kAttnListed) n *= paged_rows(p.batch, b, &first);    // (a segment per row)
+        if (KIND == kAttnListed) {                                       // (a segment per row)
+            const int rows = paged_rows(p.batch, b, &first);
+            wide += (unsigned long long)n * rows;
+            n *= rows;
+        }
         pre[b + 1] = n;
         sum += n;
     }
@@ -213,6 +218,17 @@ __device__ __forceinline__ void attn_scan(const PagedAttnParams& p, int* pre)
     for (int b = lo; b < hi; ++b) { run += pre[b + 1]; pre[b + 1] = run; }
     if (tid == 0) pre[0] = 0;
     __syncthreads();
+    if constexpr (KIND == kAttnListed)                                   // rows named more than once, against the rules, may add up beyond 32 bits: nothing is done for them
+        if (__syncthreads_or(wide > INT32_MAX / (kAttnWarps * 32))) {
+            __shared__ unsigned long long all;
+            if (tid == 0) all = 0;
+            __syncthreads();
+            atomicAdd(&all, wide);
+            __syncthreads();
+            if (all > INT32_MAX)
+                for (int b = tid; b <= B; b += kAttnWarps * 32) pre[b] = 0;
+            __syncthreads();
+        }
 }
 
 // What a CTA does of a segment: blocks first .. first + n - 1 of its sequence.

@@ -55,6 +55,7 @@ __device__ __forceinline__ int stretch_length(const AttnStretch& v, int group, b
 __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const SharedPlanParams p)
 {
     __shared__ int start[kMostStretches + 1], len_of[kMostStretches], group_of[kMostStretches], prefix[kMostStretches], sums[32], prefix_length;
+    __shared__ unsigned long long every_length;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const PagedBatch& bt = p.batch;
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const
     for (int b = tid; b < bt.B; b += kSharedThreads) { len_of[b] = bt.kv_len[b]; group_of[b] = -1; }
     for (int t = tid; t < bt.T; t += kSharedThreads) p.row_of[t] = make_int2(-1, -1);
     int s = 0, e = 0, wanted = 0;                                        // (of this warp's first group, on its way meanwhile)
-    if (tid == 0) prefix_length = 0;
+    if (tid == 0) { prefix_length = 0; every_length = 0; }
     if (warp < G) { s = p.group_start[warp]; e = p.group_start[warp + 1]; wanted = p.prefix_len[warp]; }
     __syncthreads();
     for (int g = warp; g < G; g += kSharedThreads / 32) {
@@ -128,6 +129,7 @@ __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const
             p.stretches[v] = st;
             const bool tiles = v < G ? p.prefix.tiles : p.own.tiles;
             n = st.rows <= 0 ? 0 : p.tile_rows == 128 ? stretch_length<128>(st, p.group, tiles) : stretch_length<256>(st, p.group, tiles);
+            if (n > 0) atomicAdd(&every_length, (unsigned long long)n);
         }
         int run = n;
 #pragma unroll
@@ -145,6 +147,12 @@ __global__ void __launch_bounds__(kSharedThreads) paged_shared_plan_kernel(const
         before += (int)__reduce_add_sync(0xffffffffu, (unsigned)mine);
     }
     __syncthreads();
+    if (every_length > INT32_MAX) {                                      // rows or sequences named more than once, against the rules: nothing is done
+        for (int v = tid; v <= V; v += kSharedThreads) p.lengths[v] = 0;
+        for (int t = tid; t < bt.T; t += kSharedThreads) p.row_of[t] = make_int2(-1, -1);
+        before = prefix_length = 0;
+        __syncthreads();
+    }
     if (tid < 2) {
         const SharedLaunch& at = tid == 0 ? p.prefix : p.own;
         const int64_t total = (int64_t)((at.v1 == G ? prefix_length : before) - (at.v0 == G ? prefix_length : 0)) * bt.h_kv;

@@ -8,6 +8,7 @@
 // copying of bytes, bound by HBM, is a second launch's over all SMs (us: 4.5 to decide what moves of 4000 pages, 6 what 256 sequences get of 3300, 2 the launch behind it).
 #pragma once
 #include <cuda_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include "paged.cuh"
@@ -64,24 +65,25 @@ __global__ void __launch_bounds__(256) paged_release_kernel(const PagedReleasePa
     if (in_pool(page, p.n_pages)) atomicSub(p.refs + page, 1);
 }
 
-// Exclusive sum over the CTA's threads and, in *total, the whole sum.  Every thread takes part; `sums` may be used again by the next call.
-__device__ __forceinline__ int plan_scan(int v, int* total, int* sums)
+// Exclusive sum over the CTA's threads and, in *total, the whole sum (64 bits where q_start may name rows more than once, against the rules).  Every thread takes part; `sums` may be used again by the next call.
+template <typename T>
+__device__ __forceinline__ T plan_scan(T v, T* total, T* sums)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int run = v;
+    T run = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, run, o);
+        const T u = __shfl_up_sync(0xffffffffu, run, o);
         if (lane >= o) run += u;
     }
     __syncthreads();
     if (lane == 31) sums[warp] = run;
     __syncthreads();
-    int before = lane < kPlanWarps ? sums[lane] : 0;
-    int all = before;
+    T before = lane < kPlanWarps ? sums[lane] : 0;
+    T all = before;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, all, o);
+        const T u = __shfl_up_sync(0xffffffffu, all, o);
         if (lane >= o) all += u;
     }
     *total = __shfl_sync(0xffffffffu, all, 31);
@@ -124,6 +126,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_reserve_kernel(const Paged
 {
     extern __shared__ int pre[];                                         // [B + 1] columns before sequence b, [B] the first column of it
     __shared__ int sums[kPlanWarps], copied;
+    __shared__ long long wide_sums[kPlanWarps];
     const PagedBatch& bt = p.batch;
     const int tid = threadIdx.x, lane = tid & 31, B = bt.B, log2_page = bt.log2_blocks + 4, n_pages = bt.n_pages;
     int* first = pre + B + 1;
@@ -131,10 +134,11 @@ __global__ void __launch_bounds__(kPlanThreads) paged_reserve_kernel(const Paged
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (tid == 0) { copied = 0; pre[0] = 0; }
     // ---- the columns that new tokens come to
-    int columns = 0;
+    long long columns = 0;
     for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
         const int b = b0 + tid;
-        int n = 0, t0, all;
+        int n = 0, t0;
+        long long all;
         if (b < B) {
             const int rows = paged_rows(bt, b, &t0), len = bt.kv_len[b];
             if (rows > 0 && len > 0) {
@@ -143,15 +147,19 @@ __global__ void __launch_bounds__(kPlanThreads) paged_reserve_kernel(const Paged
                 n = max(pages_of(len, log2_page, bt.table_width) - c0, 0);
             }
         }
-        const int before = plan_scan(n, &all, sums);
-        if (b < B) pre[b + 1] = columns + before + n;
+        const long long before = plan_scan((long long)n, &all, wide_sums);
+        if (b < B) pre[b + 1] = (int)(columns + before + n);
         columns += all;
+    }
+    if (columns > INT_MAX) {                                             // (rows named more than once: they lie in T / page_size + 2 B columns at most)
+        if (tid == 0) { *p.missing = INT_MAX; *p.n_copies = 0; }
+        return;
     }
     __syncthreads();
     // ---- those without a page of their own, in order
     int needs = 0;
-    for (int k0 = 0; k0 < columns; k0 += kPlanThreads) {
-        const int k = k0 + tid;
+    for (int64_t k0 = 0; k0 < columns; k0 += kPlanThreads) {
+        const int k = (int)min(k0 + tid, (int64_t)INT_MAX);
         int b = 0, c = 0, page = -1, blocks = 0, all;
         bool fresh = false;
         if (k < columns) {
@@ -171,7 +179,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_reserve_kernel(const Paged
                 blocks = (older + kPagedBlock - 1) / kPagedBlock;
             }
         }
-        const int at = needs + plan_scan(fresh, &all, sums);
+        const int at = needs + plan_scan((int)fresh, &all, sums);
         if (fresh && at < n_pages) p.need[at] = make_int4(b, c, page, blocks);
         needs += all;
     }

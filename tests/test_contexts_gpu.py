@@ -588,6 +588,27 @@ def test_scores_of_millions(P, torch):
         check(y.cpu().numpy(), want, tol, batch.rows())
 
 
+def test_rows_named_a_thousand_times_in_lists(P, torch):
+    """q_start against the rules, so that the segments pass 32 bits: the kernel sees it and does nothing but zeros."""
+    cache = P.PagedKV(8, 16, 1, 64)
+    T, B = 70000, 2047
+    q = torch.randn(T, 64, device="cuda").half()
+    out = torch.full((T, 1, 64), 7.5, dtype=torch.float16, device="cuda")
+    start = dev(torch, [0, T] * (B // 2) + [0, T])
+    assert start.shape == (B + 1,)
+    cache.attention_selected(q, torch.zeros((T, 1, 1), dtype=torch.int32, device="cuda"), torch.zeros((B, 1), dtype=torch.int32, device="cuda"), dev(torch, [16] * B), start, out=out)
+    assert (out == 0).all() and cache.device_status() == (0, 0)
+
+
+def test_sequences_named_a_thousand_times_that_share(P, torch):
+    """group_start against the rules: a call that ends."""
+    cache = P.PagedKV(8, 16, 1, 64)
+    T, G = 1000000, 1023
+    q = torch.randn(T, 64, device="cuda").half()
+    out = cache.attention_shared(q, dev(torch, [list(range(8))] * 2), dev(torch, [600000] * 2), dev(torch, [0, T // 2, T]), 1, dev(torch, [0, 2] * (G // 2) + [0, 2]), dev(torch, [64] * G))
+    assert out.shape == (T, 1, 64) and cache.device_status() == (0, 0)
+
+
 # ---------------------------------------------------------------------------- refusals
 def test_refused(P, torch):
     cache = P.PagedKV(8, 16, 2, 64)
