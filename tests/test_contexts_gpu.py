@@ -495,6 +495,34 @@ def test_workspaces_by_what_a_call_needs(P, torch):
     assert lib.qlinear_paged_attention_shared_workspace(cache._h, 31, 300, 4, 4, 1, 1) == 0
 
 
+# ---------------------------------------------------------------------------- read back by blocks
+@pytest.mark.parametrize("h_kv,d,page", [(3, 128, 16), (2, 64, 64), (1, 256, 32)])
+def test_read_of_many_rows(P, torch, h_kv, d, page):
+    """Rows at every place of a block, before the first token, without a page, of no sequence; equal to the rows read a few at a time, bit for bit."""
+    rng = np.random.default_rng(page)
+    lens, new = [700, 33, 5, 901, 16], [695, 33, 40, 300, 16]
+    batch = Batch(torch, lens, lens, page, seed=page)
+    cache, kv = filled(P, torch, batch, h_kv, d)
+    table = batch.table.copy()
+    table[3, 700 // page], table[0, 1] = -1, batch.n_pages + 7
+    starts = [4]
+    for n in new:
+        starts.append(starts[-1] + n)
+    T = starts[-1] + 9
+    args = dev(torch, table), dev(torch, lens), dev(torch, starts)
+    got = [x.cpu().numpy() for x in cache.read(*args, T)]
+    for b, (n, m) in enumerate(zip(lens, new)):
+        for c in range(m):
+            pos, t = n - m + c, starts[b] + c
+            x = table[b, pos // page] if pos >= 0 else -1
+            for y, whole in zip(got, kv[b]):
+                want = whole[pos].astype(np.float16) if 0 <= x < batch.n_pages else np.zeros((h_kv, d), np.float16)
+                assert (y[t] == want).all(), (b, pos)
+        few = min(m, 20)
+        for a, y in zip(cache.read(args[0][b:b + 1], args[1][b:b + 1], dev(torch, [0, few]), few), got):
+            assert (a.cpu().numpy() == y[starts[b] + m - few:starts[b] + m]).all()
+
+
 # ---------------------------------------------------------------------------- large numbers
 def test_two_thousand_sequences_that_share(P, torch):
     """As many sequences as a call takes (with its groups), all of the calls on them; a sample of the rows against 64 bits."""
