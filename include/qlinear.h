@@ -403,7 +403,8 @@ ql_status qlinear_paged_compact(qlinear_paged_t h, int32_t* refs_dev, int32_t* t
  * qlinear_paged_select: for row t at position p and KV head k the candidates are the columns c <= min(p / page_size, table_width - 1) of its sequence's table row whose entry lies in the pool.  With Q+ and Q- the sums over
  *   the query heads that read k, in their order, of max(q, 0) and min(q, 0), a = the largest magnitude of both and r = 32767 / a (a 0: all zero), in IEEE fp32, their codes rint(Q r), and of the page
  *       score = fp32(sum_c code+_c hi_c + code-_c lo_c) * scale            (the sum exact; it bounds the sum of the heads' scores from above, but for the codes' rounding)
- *   the `first` first and the `recent` last candidate columns' places (columns c < first, c > the last column - recent) come before all others, then the largest scores, of equal ones the lowest columns.
+ *   the `first` first and the `recent` last candidate columns' places (columns c < first, c > the last column - recent) come before all others, then the largest scores, of equal ones the lowest columns;
+ *   a score that is no number comes behind all others (scales_dev may hold any bits: pages that have never been summarised give an arbitrary choice among the candidates, nothing else).
  *   pages_dev[t, k, :] := the min(budget, candidates) columns so chosen, ascending, -1 behind them.  first + recent <= budget.  table_width <= 262144.  Queries must be finite (others choose some of the candidates).
  *   Rows of no sequence are left as they are; a row at a negative position has no candidates.  No row may be two sequences'.
  * qlinear_paged_attention_selected: qlinear_paged_attention (no window) over those visible tokens of the row's sequence that lie in the listed pages of each KV head: pages_dev as select leaves it, or columns

@@ -6,7 +6,7 @@
 // this is one product of 2 d numbers, whatever the group.  So for a row and KV head: Q+ and Q- the sums over the heads of max(q, 0) and min(q, 0) (fp32, in the heads' order),
 // in whole numbers of 1 / 32767 of the largest magnitude, r' = 32767 / top', rint(Q r'); the score of a page is
 //     fp32(sum_c Q+_c hi_c + Q-_c lo_c) * scale                                                         (the sum exact: below 2^31 for 512 products)
-// and every number on the way is defined to the bit, so the choice is, ties included.
+// and every number on the way is defined to the bit, so the choice is, ties included.  A score that is no number (keys beyond fp16 leave an infinite scale: 0 * inf) comes behind all others.
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -196,6 +196,15 @@ struct PagedSelectParams {
     bool gathered;               // the first CTA of a cluster has room for every column's key
 };
 constexpr int kSelectMostColumns = 1 << 18;
+// Keys of columns: 0, no candidate; kNoNumber, a candidate whose score is no number; from 0x007fffff (-inf) to 0xff800000 (inf), scores; kAlways, taken whatever the scores.  No scale, whatever it holds, makes a key
+// of another kind, so the kAlways are the first and the recent columns alone, budget of them at most.
+constexpr uint32_t kNoNumber = 1, kAlways = 0xffffffffu;
+__device__ __forceinline__ uint32_t select_key(int sum, float scale)
+{
+    const float score = __fadd_rn(__fmul_rn(__int2float_rn(sum), scale), 0.f);   // (-0 becomes 0: equal scores have equal keys)
+    const uint32_t bits = __float_as_uint(score);
+    return score != score ? kNoNumber : bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
@@ -320,11 +329,11 @@ __global__ void __launch_bounds__(kSelectThreads, 4) paged_select_kernel(const P
         const int at = w0 + lane, column = begin + at, page = page_next;
         page_next = at + kSelectThreads < n_mine ? row[at + kSelectThreads] : -1;
         const bool ok = page >= 0 && page < bt.n_pages, always = all || column < p.first || column > last - p.recent;
-        if (at < n_mine && (!ok || always)) put(at, ok ? 0xffffffffu : 0u);
+        if (at < n_mine && (!ok || always)) put(at, ok ? kAlways : 0u);
         if (all) continue;
         const int64_t mine = (int64_t)(ok ? page : 0) * bt.h_kv + head;
-        const bool scored = ok && !always;
-        const float scale = scored ? p.scales[mine] : -1.f;
+        const uint32_t scored = __ballot_sync(0xffffffffu, ok && !always);
+        const float scale = scored >> lane & 1 ? p.scales[mine] : 0.f;
 #pragma unroll 1
         for (int i0 = 0; i0 < 32; i0 += kTurns * kPer) {
             uint4 u[kTurns];
@@ -363,10 +372,7 @@ __global__ void __launch_bounds__(kSelectThreads, 4) paged_select_kernel(const P
             for (int o = kLanes / 16; o >= 1; o >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
             const int src = i0 + turn * kPer + lane / kLanes;            // the column (of the 32) whose sum this lane has
             const float unit = __shfl_sync(0xffffffffu, scale, src);
-            if (unit >= 0.f && sub % (kLanes / 8) == 0) {
-                const uint32_t bits = __float_as_uint(__fadd_rn(__fmul_rn(__int2float_rn(s[0]), unit), 0.f));   // (-0 becomes 0: equal scores have equal keys)
-                put(w0 + src, bits & 0x80000000u ? ~bits : bits | 0x80000000u);
-            }
+            if ((scored >> src & 1) && sub % (kLanes / 8) == 0) put(w0 + src, select_key(s[0], unit));
         }
     }
 
@@ -399,8 +405,8 @@ __global__ void __launch_bounds__(kSelectThreads, 4) paged_select_kernel(const P
     for (int i = tid; i < n; i += kSelectThreads) {
         const uint32_t key = keys[i];
         candidates += key != 0;
-        always += key == 0xffffffffu;
-        if (key == 0 || key == 0xffffffffu) continue;
+        always += key == kAlways;
+        if (key == 0 || key == kAlways) continue;
         least = max(least, ~key);
         largest = max(largest, key);
     }
@@ -430,17 +436,17 @@ __global__ void __launch_bounds__(kSelectThreads, 4) paged_select_kernel(const P
     int left = 0;
     if (candidates > p.budget) {
         const uint32_t base = ~least;
-        left = p.budget - always;                                        // (of first + recent <= budget columns)
+        left = p.budget - always;                                        // (not below 0: first + recent <= budget)
         uint32_t prefix = 0;                                             // of key - base
         int shift = 32 - __clz(largest - base), bits = 0;
-        threshold = left > 0 ? base : 0xfffffffeu;                       // (left 0: those that are always taken are the budget; all keys equal: no rounds)
+        threshold = left > 0 ? base : kAlways - 1;                       // (left 0: those that are always taken are the budget; all keys equal: no rounds)
         for (int round = 0; left > 0 && shift > 0; ++round) {
             bits = min(shift, 8);
             shift -= bits;
             int* h = hist[round & 1];
             for (int i = tid; i < n; i += kSelectThreads) {
                 const uint32_t key = keys[i];
-                if (key == 0 || key == 0xffffffffu) continue;
+                if (key == 0 || key == kAlways) continue;
                 const uint32_t x = (key - base) >> shift;
                 if (round == 0 || x >> bits == prefix) atomicAdd(&h[x & ((1u << bits) - 1)], 1);
             }

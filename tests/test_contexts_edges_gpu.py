@@ -1,0 +1,118 @@
+"""Shared and sparse contexts at the edges of what their arrays may hold: summaries whose scales are no ordinary numbers."""
+import numpy as np
+import pytest
+
+from test_contexts_gpu import dev
+from test_paged_gpu import HEADS, f16
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def P(_built_library):
+    import paper_2505_00232_b200 as P
+    return P
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available(), "these tests need a CUDA device"
+    return torch
+
+
+# ---------------------------------------------------------------------------- the choice of pages
+def chosen_by_any_score(q, h_kv, bounds, scales, row, n_pages, budget, first, recent):
+    """The columns chosen for a row's queries [h_q, d] that all of the table's row is open to, [h_kv, budget]: by the definition, scores that are no numbers behind all others."""
+    h_q, d = q.shape
+    c = np.arange(len(row))
+    ok = (row >= 0) & (row < n_pages)
+    out = np.full((h_kv, budget), -1)
+    for h in range(h_kv):
+        up, down = np.zeros(d, np.float32), np.zeros(d, np.float32)
+        for x in q[h * (h_q // h_kv):(h + 1) * (h_q // h_kv)].astype(np.float32):
+            up, down = up + np.maximum(x, 0), down + np.minimum(x, 0)
+        top = max(up.max(), -down.min())
+        r = np.float32(32767) / top if top > 0 else np.float32(0)
+        at = np.where(ok, row, 0)
+        total = bounds[at, h, 0].astype(np.int64) @ np.rint(up * r).astype(np.int64) + bounds[at, h, 1].astype(np.int64) @ np.rint(down * r).astype(np.int64)
+        with np.errstate(invalid="ignore", over="ignore"):
+            score = total.astype(np.float32) * scales[at, h]
+        always = (c < first) | (c >= len(row) - recent)
+        kind = np.where(always, 0, np.where(np.isnan(score), 2, 1))
+        order = np.lexsort((c, np.where(kind == 1, -score.astype(np.float64), 0.0), kind))
+        order = order[ok[order]][:budget]
+        out[h, :len(order)] = np.sort(order)
+    return out
+
+
+def rows_between_guards(torch, T, h_kv, budget):
+    """Rows for lists, and the tensor that they lie in the middle of."""
+    around = torch.full((T + 2 * 64, h_kv, budget), 77, dtype=torch.int32, device="cuda")
+    return around, around[64:-64]
+
+
+@pytest.mark.parametrize("W,T", [(40, 300), (700, 2), (30001, 1), (60000, 1)])      # (one CTA a row; clusters whose first CTA has every key, and that look for the threshold together)
+@pytest.mark.parametrize("budget,first,recent", [(1, 0, 0), (1, 1, 0), (5, 1, 1), (6, 3, 3), (33, 0, 2)])
+def test_select_whatever_the_scales_hold(P, torch, W, T, budget, first, recent):
+    """Infinite and negative scales, scales that are no numbers, sums of zero: nothing is written behind a row's list, and the choice is the definition's."""
+    rng = np.random.default_rng(W + budget)
+    h_q, h_kv, d, page, n_pages = 4, 2, 64, 16, 3000
+    cache = P.PagedKV(n_pages, page, h_kv, d)
+    bounds = np.sort(rng.integers(-127, 128, (n_pages, h_kv, 2, d)), 2)[:, :, ::-1].astype(np.int8)
+    bounds[rng.random(n_pages) < 0.5] = 0                                # (0 * inf)
+    scales = rng.random((n_pages, h_kv)).astype(np.float32)
+    patterns = np.array([0x7f800000, 0xff800000, 0x7fffffff, 0xffffffff, 0x7fc00000, 0xffc00000, 0x7f800001, 0xbf800000, 0x80000000, 0x00000001, 0x7f7fffff], np.uint32).view(np.float32)
+    odd = rng.random((n_pages, h_kv)) < 0.6
+    scales[odd] = rng.choice(patterns, odd.sum())
+    table = rng.integers(-1, n_pages + 1, (1, W))
+    q = f16(rng, T, h_q, d)
+    args = dev(torch, table), dev(torch, [W * page + T - 1]), dev(torch, [0, T])      # (every row's last column is the table's last)
+    db = torch.from_numpy(bounds.copy()).cuda(), torch.from_numpy(scales).cuda()
+    around, out = rows_between_guards(torch, T, h_kv, budget)
+    cache.select(torch.from_numpy(q).cuda(), db, *args, budget, first, recent, out=out)
+    got = around.cpu().numpy()
+    assert (got[:64] == 77).all() and (got[-64:] == 77).all()
+    for t in range(0, T, 37):
+        assert (got[64 + t] == chosen_by_any_score(q[t], h_kv, bounds, scales, table[0], n_pages, budget, first, recent)).all()
+
+
+@pytest.mark.parametrize("bits", [0x7f800000, 0xff800000, 0x7fffffff, 0xffffffff, 0xbf800000])
+def test_select_where_every_scale_is_the_same(P, torch, bits):
+    """As a buffer that nothing has been written to may hold it: the lists stay lists."""
+    rng = np.random.default_rng(5)
+    h_kv, d, n_pages, W, T, budget = 3, 128, 200, 150, 64, 4
+    cache = P.PagedKV(n_pages, 16, h_kv, d)
+    bounds = np.where(rng.random((n_pages, h_kv, 2, d)) < 0.5, 0, -1).astype(np.int8)
+    bounds[::2] = 0
+    scales = np.full((n_pages, h_kv), bits, np.uint32).view(np.float32)
+    table = np.stack([rng.permutation(n_pages)[:W] for _ in range(T)])
+    q = f16(rng, T, h_kv, d)
+    db = torch.from_numpy(bounds).cuda(), torch.from_numpy(scales).cuda()
+    around, out = rows_between_guards(torch, T, h_kv, budget)
+    for _ in range(3):                                                   # (whatever the calls before have left in shared memory)
+        cache.select(torch.from_numpy(q).cuda(), db, dev(torch, table), dev(torch, [W * 16] * T), dev(torch, range(T + 1)), budget, 1, 2, out=out)
+        got = around.cpu().numpy()
+        assert (got[:64] == 77).all() and (got[-64:] == 77).all()
+        for t in range(T):
+            assert (got[64 + t] == chosen_by_any_score(q[t], h_kv, bounds, scales, table[t], n_pages, budget, 1, 2)).all()
+
+
+@pytest.mark.parametrize("h_q,h_kv,d", HEADS)
+def test_select_by_summaries_of_any_bytes(P, torch, h_q, h_kv, d):
+    """A pool of random bytes: scales of keys that are infinite or no numbers, summarised and chosen from."""
+    rng = np.random.default_rng(d)
+    page, n_pages, W, T, budget = 16, 300, 280, 5, 7
+    cache = P.PagedKV(n_pages, page, h_kv, d)
+    cache.pool.copy_(torch.randint(0, 256, cache.pool.shape, dtype=torch.uint8, generator=torch.Generator().manual_seed(d)))
+    b = cache.key_bounds()
+    table = np.stack([rng.permutation(n_pages)[:W] for _ in range(T)])
+    lens = dev(torch, [W * page] * T)
+    cache.summarise(b, dev(torch, table), lens, dev(torch, [W * page * i for i in range(T + 1)]), T * W * page)
+    q = f16(rng, T, h_q, d)
+    around, out = rows_between_guards(torch, T, h_kv, budget)
+    cache.select(torch.from_numpy(q).cuda(), b, dev(torch, table), lens, dev(torch, range(T + 1)), budget, 1, 1, out=out)
+    got, bounds, scales = around.cpu().numpy(), b[0].cpu().numpy(), b[1].cpu().numpy()
+    assert (got[:64] == 77).all() and (got[-64:] == 77).all()
+    for t in range(T):
+        assert (got[64 + t] == chosen_by_any_score(q[t], h_kv, bounds, scales, table[t], n_pages, budget, 1, 1)).all()
