@@ -400,6 +400,7 @@ ql_status qlinear_paged_compact(qlinear_paged_t h, int32_t* refs_dev, int32_t* t
  *   bounds_dev int8 [n_pages, h_kv, 2, d_h], 16-byte aligned, and scales_dev fp32 [n_pages, h_kv]: the caller's, what the summaries of the pool's pages are held in.
  * qlinear_paged_summarise: for every page that one of the batch's rows lies in (after they have been appended), over its tokens j < kv_len, with hi_c and lo_c the largest and the smallest key element fp16(q s) of channel c of a
  *   KV head and top = max_c max(hi_c, -lo_c):  scale = top / 127,  r = 127 / top,  bounds = min(127, ceil(hi_c r)) and max(-127, floor(lo_c r))     (IEEE fp32 operations; top 0: zeros).
+ *   A page that rows of several sequences lie in, in the same column (as fork leaves it): over the tokens of the one that has the most in it.  In different columns a page may not be, unless it is full.
  * qlinear_paged_select: for row t at position p and KV head k the candidates are the columns c <= min(p / page_size, table_width - 1) of its sequence's table row whose entry lies in the pool.  With Q+ and Q- the sums over
  *   the query heads that read k, in their order, of max(q, 0) and min(q, 0), a = the largest magnitude of both and r = 32767 / a (a 0: all zero), in IEEE fp32, their codes rint(Q r), and of the page
  *       score = fp32(sum_c code+_c hi_c + code-_c lo_c) * scale            (the sum exact; it bounds the sum of the heads' scores from above, but for the codes' rounding)

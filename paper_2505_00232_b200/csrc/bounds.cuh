@@ -69,13 +69,15 @@ template <int D>
 __global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : 4) paged_bounds_kernel(const PagedBoundsParams p)
 {
     constexpr int NB = D / 64, kBlock = paged_block_bytes(D), kPairs = 16 * NB;   // pairs of elements of a lane: largest and smallest
-    extern __shared__ int pre[];                                         // [B + 1] touched columns before sequence b, [B] the first of them
+    extern __shared__ int pre[];                                         // [B + 1] touched columns before sequence b, [B] the first of them, [B] its length
     __shared__ long long sums[kBoundsWarps];
+    __shared__ int theirs[kBoundsWarps][32];
+    __shared__ int3 looked_up[kBoundsWarps][32];                         // page, column, tokens in it: of 32 pages of the CTA (in registers beside the maxima they would spill)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const PagedBatch& bt = p.batch;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t = lane >> 2, c = lane & 3, log2_page = bt.log2_blocks + 4;
-    int* first_of = pre + bt.B + 1;
+    int *first_of = pre + bt.B + 1, *len_of = first_of + bt.B;
     long long columns = 0;
     if (tid == 0) pre[0] = 0;
     for (int b0 = 0; b0 < bt.B; b0 += kBoundsThreads) {
@@ -84,15 +86,16 @@ __global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : 4) paged_bounds
         long long all;
         const int n = b < bt.B ? touched_columns(bt, b, &first) : 0;
         const long long before = bounds_scan(n, &all, sums);
-        if (b < bt.B) { pre[b + 1] = (int)(columns + before + n); first_of[b] = first; }
+        if (b < bt.B) { pre[b + 1] = (int)(columns + before + n); first_of[b] = first; len_of[b] = bt.kv_len[b]; }
         columns += all;
     }
     if (columns > INT_MAX) return;                                       // (rows named more than once, against the rules: they lie in T / page_size + 2 B columns at most)
     const int total = (int)columns;
     __syncthreads();
+    const auto tokens_in = [&](int len, int column) { return (int)min((int64_t)len - ((int64_t)column << log2_page), (int64_t)1 << log2_page); };
     const int mine = total > (int)blockIdx.x ? (total - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;   // pages of this CTA: blockIdx.x, + gridDim.x, ...
     for (int base = 0; base < mine; base += 32) {
-        int page_of = -1, tokens_of = 0;                                 // of page base + lane
+        __syncwarp();
         if (base + lane < mine) {
             const int k = (int)blockIdx.x + (base + lane) * (int)gridDim.x;
             int b = 0, hi_b = bt.B;                                      // pre[b] <= k < pre[hi_b]
@@ -102,14 +105,31 @@ __global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : 4) paged_bounds
                 else hi_b = mid;
             }
             const int column = first_of[b] + k - pre[b];
-            page_of = bt.table[b * bt.table_ld + column];
-            tokens_of = (int)min((int64_t)bt.kv_len[b] - ((int64_t)column << log2_page), (int64_t)1 << log2_page);
+            looked_up[warp][lane] = make_int3(bt.table[b * bt.table_ld + column], column, tokens_in(len_of[b], column));
         }
+        __syncwarp();
         const int tasks = min(32, mine - base) * bt.h_kv;
         for (int task = warp; task < tasks; task += kBoundsWarps) {
-            const int at = task / bt.h_kv, head = task - at * bt.h_kv, page = __shfl_sync(0xffffffffu, page_of, at), tokens = __shfl_sync(0xffffffffu, tokens_of, at);
+            const int at = task / bt.h_kv, head = task - at * bt.h_kv, page = looked_up[warp][at].x, tokens = looked_up[warp][at].z;
             if (page < 0 || page >= bt.n_pages) continue;
             const uint8_t* blk = bt.pool + (((int64_t)page * bt.h_kv + head) << bt.log2_blocks) * kBlock;
+            // Of the sequences that end in a page the one with the most tokens there speaks for it (those with as many say the same).  A lane's last entry of one with more in this column is on its way until the keys are done, to
+            // shared memory: waited for before them a generated token a sequence takes 1.8 us more, in a register prompts do, which spill then.
+            const bool partly = tokens < 1 << log2_page;
+            if (partly) {
+                const int column = looked_up[warp][at].y;
+                bool requested = false;
+                for (int b = lane; b < bt.B; b += 32) {
+                    if (column < first_of[b] || column - first_of[b] >= pre[b + 1] - pre[b] || tokens_in(len_of[b], column) <= tokens) continue;
+                    if (requested) {
+                        asm volatile("cp.async.wait_all;" ::: "memory");
+                        if (theirs[warp][lane] == page) break;
+                    }
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(&theirs[warp][lane])), "l"(bt.table + b * bt.table_ld + column) : "memory");
+                    requested = true;
+                }
+                if (!requested) theirs[warp][lane] = -1;
+            }
             uint32_t top[kPairs];                                        // pairs 4 (4 j + 2 e + s) ..: panel j, group e, s: of the negated
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) top[i] = i & 4 ? 0x7c007c00u : 0xfc00fc00u;   // (infinities)
@@ -166,6 +186,10 @@ __global__ void __launch_bounds__(kBoundsThreads, D == 256 ? 2 : 4) paged_bounds
             for (int i = 0; i < kPairs / 8; ++i) most = fmaxf(most, fmaxf(__low2float(*reinterpret_cast<const __half2*>(top + i)), __high2float(*reinterpret_cast<const __half2*>(top + i))));
 #pragma unroll
             for (int o = 16; o >= 1; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            if (partly) {
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                if (__any_sync(0xffffffffu, theirs[warp][lane] == page)) continue;
+            }
             const float r = most > 0.f ? __fdiv_rn(127.f, most) : 0.f;
             int8_t* to = p.bounds + ((int64_t)page * bt.h_kv + head) * (2 * D);
 #pragma unroll

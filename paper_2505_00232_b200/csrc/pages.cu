@@ -123,7 +123,7 @@ extern "C" ql_status qlinear_paged_summarise(qlinear_paged_t h, const int32_t* t
     const int64_t pages = std::min<int64_t>(((int64_t)T >> (h->log2_blocks + 4)) + 2ll * B, T);
     const unsigned grid = (unsigned)std::min<int64_t>(pages, (h->d.d_h == 256 ? 2ll : 4ll) * h->shared.sms);
     const auto kernel = h->d.d_h == 64 ? paged_bounds_kernel<64> : h->d.d_h == 128 ? paged_bounds_kernel<128> : paged_bounds_kernel<256>;
-    return launched(launch(kernel, p, dim3(grid), dim3(kBoundsThreads), (2 * B + 1) * 4, static_cast<cudaStream_t>(stream), 1, h->pdl));
+    return launched(launch(kernel, p, dim3(grid), dim3(kBoundsThreads), (3 * B + 1) * 4, static_cast<cudaStream_t>(stream), 1, h->pdl));
 }
 
 namespace {

@@ -1,8 +1,8 @@
-"""Shared and sparse contexts at the edges of what their arrays may hold: summaries whose scales are no ordinary numbers."""
+"""Shared and sparse contexts at the edges of what their arrays may hold: summaries whose scales are no ordinary numbers, pages in which several sequences end."""
 import numpy as np
 import pytest
 
-from test_contexts_gpu import dev
+from test_contexts_gpu import bounds64, dev
 from test_paged_gpu import HEADS, f16
 
 pytestmark = pytest.mark.gpu
@@ -116,3 +116,31 @@ def test_select_by_summaries_of_any_bytes(P, torch, h_q, h_kv, d):
     assert (got[:64] == 77).all() and (got[-64:] == 77).all()
     for t in range(T):
         assert (got[64 + t] == chosen_by_any_score(q[t], h_kv, bounds, scales, table[t], n_pages, budget, 1, 1)).all()
+
+
+# ---------------------------------------------------------------------------- summaries
+@pytest.mark.parametrize("h_q,h_kv,d", HEADS)
+@pytest.mark.parametrize("page,lens", [(64, [37, 12, 63, 5, 12]), (16, [16, 3]), (128, [400, 130, 257, 300, 1] * 60), (32, list(range(1, 65)) * 20)])
+def test_sequences_that_end_in_the_same_page(P, torch, h_q, h_kv, d, page, lens):
+    """Forked at shorter lengths and summarised whole, before anyone has a page of its own: every page's summary is that of the sequence with the most tokens in it, in whatever order they come."""
+    rng = np.random.default_rng(len(lens))
+    n, B = max(lens), len(lens)
+    W = -(-n // page) + 1
+    cache = P.PagedKV(2 * W, page, h_kv, d)
+    row = rng.permutation(2 * W)[:W]
+    table = np.where(np.arange(W) < -(-np.array(lens)[:, None] // page), row, -1)
+    k, v = (torch.from_numpy(f16(rng, n, h_kv, d)).cuda() for _ in range(2))
+    whole = dev(torch, [row]), dev(torch, [n]), dev(torch, [0, n])
+    cache.append(k, v, *whole)
+    keys = cache.read(*whole, n)[0].cpu().numpy().astype(np.float64)
+    b = cache.key_bounds()
+    want, want_s = np.zeros(b[0].shape), np.zeros(b[1].shape, np.float32)
+    for j in range(-(-n // page)):
+        want[row[j], :, 0], want[row[j], :, 1], want_s[row[j]] = bounds64(keys[j * page:(j + 1) * page])
+    T = sum(lens)
+    for order in (np.arange(B), np.arange(B)[::-1], rng.permutation(B)):
+        b[0].fill_(0)
+        b[1].fill_(0)
+        at = np.array(lens)[order]
+        cache.summarise(b, dev(torch, table[order]), dev(torch, at), dev(torch, np.concatenate([[0], np.cumsum(at)])), T)
+        assert (b[0].cpu().numpy() == want).all() and (b[1].cpu().numpy() == want_s).all()
