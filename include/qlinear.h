@@ -377,7 +377,7 @@ ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q_dev, int64_t 
 /* Pages that requests share.  refs_dev [n_pages] int32, the caller's: how many entries of its page tables hold a page, 0: free.  The calls keep it so; it has to be so when they
  * begin.  Tables are those of the calls above (entries outside the pool: no page), changed in place; all decisions are made on the device from what the arrays hold when the kernels run.
  * qlinear_paged_fork: row i of children_dev (n rows of table_width columns) := the pages of the first lengths[i] tokens of row parents[i] of the table, -1 behind them and where parents[i] is no row; each of
- *   these pages has one holder more.  What the row held before is overwritten, not given back.  children_dev must not overlap the table (other rows of the same array are fine).  n <= QL_PAGED_MAX_SEQUENCES.
+ *   these pages has one holder more.  What the row held before is overwritten, not given back.  children_dev and the table must have no entry in common (other rows or columns of the same array are fine, between the table's too).  n <= QL_PAGED_MAX_SEQUENCES.
  * qlinear_paged_release: row rows[i] gives back the pages behind its first keep[i] tokens (keep NULL: all): entries -1, one holder less each.  Numbers that are no row are passed over; a row named twice gives
  *   back what any of the two says.  n <= 65535.
  * qlinear_paged_reserve: gives every sequence of the batch pages of its own for its new tokens (positions max(kv_len - rows, 0) to kv_len - 1, as far as the table has columns): a column without a page gets a free one,

@@ -689,7 +689,7 @@ class PagedKV:
 
     def fork(self, refs, page_table, parents, lengths, out=None, stream=None):
         """parents, lengths int32 [n] -> int32 [n, pages]: rows with the pages of the first lengths[i] tokens of row parents[i], -1 behind them; refs (int32 [n_pages], how many entries of the caller's page tables hold a
-        page) counts the new entries.  out: rows to write them to, which hold no pages; they must not overlap page_table."""
+        page) counts the new entries.  out: rows to write them to, which hold no pages; they and page_table have no entry in common."""
         y = _serving.paged_fork(self._native, refs, page_table, parents, lengths, out, self.n_pages, _raw(stream))
         if y is not None:
             return y

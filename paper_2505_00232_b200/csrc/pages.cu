@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cstdlib>
 
 #include "bounds.cuh"
 #include "pages.cuh"
@@ -18,11 +19,17 @@ bool table_ok(qlinear_paged_t h, const int32_t* table, int64_t ld, int32_t width
 {
     return h && rows >= 0 && width >= 0 && ld >= width && aligned(table, 4) && (table || rows == 0 || width == 0);
 }
+// Whether two page tables of the same width have no entry in common: rows between or beside each other's do not.
 bool apart(const int32_t* a, int64_t a_ld, int64_t a_rows, const int32_t* b, int64_t b_ld, int64_t b_rows, int64_t width)
 {
     if (a_rows == 0 || b_rows == 0 || width == 0) return true;
-    const auto end = [&](const int32_t* p, int64_t ld, int64_t rows) { return reinterpret_cast<uintptr_t>(p + (rows - 1) * ld + width); };
-    return end(a, a_ld, a_rows) <= reinterpret_cast<uintptr_t>(b) || end(b, b_ld, b_rows) <= reinterpret_cast<uintptr_t>(a);
+    const int64_t first = ((int64_t)reinterpret_cast<uintptr_t>(b) - (int64_t)reinterpret_cast<uintptr_t>(a)) / 4;   // of b's entries, from a's on
+    if (first >= (a_rows - 1) * a_ld + width || first + (b_rows - 1) * b_ld + width <= 0) return true;
+    for (int64_t j = 0; j < b_rows; ++j) {
+        const int64_t at = first + j * b_ld, i = std::min(std::max<int64_t>(at, 0) / a_ld, a_rows - 1);   // row i of a begins at or before it, unless that is row 0
+        if (std::abs(at - i * a_ld) < width || (i + 1 < a_rows && std::abs(at - (i + 1) * a_ld) < width)) return false;
+    }
+    return true;
 }
 bool workspace_ok(qlinear_paged_t h, const void* p, size_t bytes) { return p && aligned(p, 32) && bytes >= qlinear_paged_pages_workspace(h); }
 struct Workspace { int4 *copies, *need; int32_t *one, *two, *n_copies; };
