@@ -103,15 +103,12 @@ extern "C" ql_status qlinear_paged_compact(qlinear_paged_t h, int32_t* refs, int
     DeviceGuard guard(h->device);
     if (!guard.ok) { cudaGetLastError(); return QL_ERR_CUDA; }
     const Workspace w = parts_of(h, workspace);
-    const PagedCompactParams p{h->pool, B > 0 && table_width > 0 ? table : nullptr, refs, moved, w.one, w.two, w.copies, w.n_copies, static_cast<int8_t*>(bounds), scales, table_ld, B, table_width, h->d.n_pages,
-                               h->d.h_kv, h->log2_blocks, h->d.d_h};
+    const PagedCompactParams p{B > 0 && table_width > 0 ? table : nullptr, refs, moved, w.one, w.two, w.copies, w.n_copies, static_cast<int8_t*>(bounds), scales, table_ld, B, table_width, h->d.n_pages,
+                               h->d.h_kv, h->d.d_h};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = launch(paged_compact_kernel, p, dim3(1), dim3(kPlanThreads), 0, st, 1, h->pdl);
     if (e != cudaSuccess) return launched(e);
-    // a page in one run, or, where its bytes do not fit 32 bits' pieces, head by head
-    const int run = paged_block_bytes(h->d.d_h) << h->log2_blocks;
-    const bool whole = (int64_t)run * h->d.h_kv <= INT32_MAX - kCopyPiece;
-    const PagedCopyParams c{h->pool, w.copies, w.n_copies, whole ? 1 : h->d.h_kv, whole ? run * h->d.h_kv : run, 0, p};
+    const PagedCopyParams c{h->pool, w.copies, w.n_copies, 1, (int)page_bytes(&h->d), 0, p};
     return launched(launch(paged_copy_kernel, c, dim3(8 * h->shared.sms), dim3(kCopyThreads), 0, st, 1, h->pdl));
 }
 
