@@ -1,4 +1,9 @@
-"""Shared and sparse contexts at the edges of what their arrays may hold: summaries whose scales are no ordinary numbers, pages in which several sequences end."""
+"""Shared and sparse contexts at the edges of what their arrays may hold: summaries whose scales are no ordinary numbers, pages in which several sequences end, arrays against
+the rules whose work passes 32 bits."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
@@ -6,6 +11,7 @@ from test_contexts_gpu import bounds64, dev
 from test_paged_gpu import HEADS, f16
 
 pytestmark = pytest.mark.gpu
+SETTING = os.environ.get("QLINEAR_PAGED_SHARED")
 
 
 @pytest.fixture(scope="module")
@@ -144,3 +150,51 @@ def test_sequences_that_end_in_the_same_page(P, torch, h_q, h_kv, d, page, lens)
         at = np.array(lens)[order]
         cache.summarise(b, dev(torch, table[order]), dev(torch, at), dev(torch, np.concatenate([[0], np.cumsum(at)])), T)
         assert (b[0].cpu().numpy() == want).all() and (b[1].cpu().numpy() == want_s).all()
+
+
+# ---------------------------------------------------------------------------- what passes 32 bits is left undone
+@pytest.mark.skipif(SETTING not in ("1", "2"), reason="by its sizes the call is plain attention: run by the test below")
+def test_groups_named_a_thousand_times(P, torch):
+    """512 times the same group (every other one has no sequences): 512 * 313 * 16077 steps of the tiles (of 256 rows) or 512 * 10000 * 64316 blocks of the kernel of few rows (of 8), above 2^31 each.  Nothing is done."""
+    cache = P.PagedKV(8, 16, 1, 64)
+    T, G, W = 20000, 1023, 1 << 16
+    q = torch.randn((T, 4, 64), device="cuda").half()
+    out = torch.full((T, 4, 64), 7.5, dtype=torch.float16, device="cuda")
+    table = torch.zeros((2, W), dtype=torch.int32, device="cuda")
+    call = lambda groups: cache.attention_shared(q, table, dev(torch, [16 * W] * 2), dev(torch, [0, T // 2, T]), 8, dev(torch, [0, 2] * (groups // 2 + 1)), dev(torch, [16 * W - T] * (2 * (groups // 2) + 1)), out=out)
+    call(G)
+    assert (out == 7.5).all() and cache.device_status() == (0, 0)
+    call(1)                                                              # (as it should be: the first eight rows of each)
+    served = torch.zeros(T, dtype=torch.bool, device="cuda")
+    served[:8] = served[T // 2:T // 2 + 8] = True
+    assert (out[served] != 7.5).any() and (out[~served] == 7.5).all() and cache.device_status() == (0, 0)
+
+
+@pytest.mark.parametrize("setting", ["1", "2"])
+def test_groups_named_a_thousand_times_by(_built_library, setting):
+    cmd = [sys.executable, "-m", "pytest", os.path.abspath(__file__), "-m", "gpu", "-x", "-q", "-p", "no:cacheprovider", "-k", "test_groups_named_a_thousand_times and not by"]
+    r = subprocess.run(cmd, env=dict(os.environ, QLINEAR_PAGED_SHARED=setting), cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), timeout=300, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0 and "1 passed" in r.stdout, r.stdout[-4000:]
+
+
+def test_rows_named_a_thousand_times(P, torch):
+    """1024 sequences of the same 33.6 million rows: 2.15e9 blocks to read back, 2.15e9 columns to look at.  Nothing is written; the pool is short of more pages than a number says."""
+    cache = P.PagedKV(8, 16, 1, 64)
+    B, T = 2047, 33600000
+    start, lens = dev(torch, [0, T] * ((B + 1) // 2)), dev(torch, [T] * B)
+    refs, b = dev(torch, [1, 0, 2, 0, 0, 1, 1, 0]), cache.key_bounds()
+    b[0].fill_(9)
+    b[1].fill_(7.5)
+    table = torch.full((B, T // 16), -1, dtype=torch.int32, device="cuda")
+    missing = cache.reserve(refs, table, lens, start, T)
+    cache.summarise(b, table, lens, start, T)
+    assert missing.item() == 2 ** 31 - 1 and refs.tolist() == [1, 0, 2, 0, 0, 1, 1, 0] and table.max().item() == -1
+    assert (b[0] == 9).all() and (b[1] == 7.5).all()
+    del table
+    torch.cuda.empty_cache()
+    k, v = (torch.full((T, 1, 64), 7.5, dtype=torch.float16, device="cuda") for _ in range(2))
+    one = torch.zeros((B, 1), dtype=torch.int32, device="cuda")
+    assert P.lib.qlinear_paged_read(cache._h, one.data_ptr(), 1, 1, lens.data_ptr(), start.data_ptr(), B, T, k.data_ptr(), v.data_ptr(), torch.cuda.current_stream().cuda_stream) == P.QL_OK
+    assert (k == 7.5).all() and (v == 7.5).all() and cache.device_status() == (0, 0)
+    del k, v
+    torch.cuda.empty_cache()
