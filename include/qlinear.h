@@ -383,6 +383,7 @@ ql_status qlinear_paged_attention(qlinear_paged_t h, const void* q_dev, int64_t 
  * qlinear_paged_reserve: gives every sequence of the batch pages of its own for its new tokens (positions max(kv_len - rows, 0) to kv_len - 1, as far as the table has columns): a column without a page gets a free one,
  *   a page with more than one holder is replaced by a free one (one holder less; what it holds of the sequence's older tokens is copied).  In the order of sequences and columns they get the lowest
  *   free pages, whose refs become 1.  missing_dev[0] := 0; or, if the pool has too few free pages, how many it is short of, and nothing else is changed.  Pages whose last holder was replaced are free for the next call.
+ *   The copies are made in this cache's pool alone: a model with a cache per layer keeps refs and a page table per layer and makes the call for each.
  * qlinear_paged_compact: the live pages (refs > 0), n of them, take the places 0 to n - 1: those numbered n and up move to the free places below n, both in order, with contents, refs and, if given, the
  *   summaries (below).  The table's entries follow (an entry of a free page becomes -1); moved_dev [n_pages]: where each page is now, -1 for those that were free (for tables that the call does not see).
  *   workspace_dev: qlinear_paged_pages_workspace bytes of the caller's for reserve and compact, 32-byte aligned, overwritten; calls that may overlap need one each.
@@ -419,7 +420,9 @@ ql_status qlinear_paged_compact(qlinear_paged_t h, int32_t* refs_dev, int32_t* t
  *   far as all see it.  Sequences of no group, and groups that do not lie in [0, B) or that have less than two sequences, share nothing; no sequence may be in two groups.  n_groups + B <= QL_PAGED_MAX_SEQUENCES.
  *   Calls that by their sizes (the table's columns for the lengths: pass no more than are needed) would gain nothing by it are qlinear_paged_attention calls, with the limits of that; QLINEAR_PAGED_SHARED=0 makes all calls such, 1 and 2
  *   those without groups alone (beginnings by the kernel of few rows, where it serves, and of many).
- *   workspace_dev: qlinear_paged_attention_shared_workspace bytes, 32-byte aligned, overwritten.
+ *   The host has the table's columns alone to go by: a table much wider than the contexts are (a captured step's) has the shared kernels taken for short ones too, at up to 2.8 times the time of
+ *   qlinear_paged_attention (32 sequences of 1000 tokens, 131072 tokens of columns); contexts of the table's order gain.
+ *   workspace_dev: qlinear_paged_attention_shared_workspace bytes, 32-byte aligned, overwritten.  To be asked for with the call's own numbers: the size goes by the kernels that serve them, and fewer sequences, groups or columns may need more.
  * Asynchronous, allocate nothing; ordered against appends, summaries and moves of the same pages by the caller.  Errors as above. */
 ql_status qlinear_paged_summarise(qlinear_paged_t h, const int32_t* table, int64_t table_ld, int32_t table_width, const int32_t* kv_len, const int32_t* q_start, int32_t B, int32_t T,
                                   void* bounds_dev, float* scales_dev, void* cuda_stream);

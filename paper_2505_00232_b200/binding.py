@@ -719,7 +719,7 @@ class PagedKV:
         _check(lib.qlinear_paged_release(self._h, at[0], *table, at[1], at[2], n, _on_stream(self.device, stream)[0]), where)
 
     def reserve(self, refs, page_table, kv_len, q_start, T: int, stream=None):
-        """Gives every sequence of the batch pages of its own for its T new rows, before they are appended: free ones where the page table has none, copies where others hold the page too.  Returns int32 [1]: 0,
+        """Gives every sequence of the batch pages of its own for its T new rows, before they are appended: free ones where the page table has none, copies (in this cache's pool) where others hold the page too.  Returns int32 [1]: 0,
         or how many pages the pool is short of, in which case nothing has changed."""
         y = _serving.paged_reserve(self._native, refs, page_table, kv_len, q_start, T, self.n_pages, _raw(stream))
         if y is not None:

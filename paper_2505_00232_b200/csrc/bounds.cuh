@@ -277,8 +277,8 @@ __device__ __forceinline__ int select_scan(int v, int* total, int* sums)
 // the eight sums of a lane are added over those lanes by halves (each lane keeps the half of the sums that is its own: 8 exchanges for 8 sums, not 8 times log2 of the lanes).  Scores become ordered 32-bit keys in
 // the shared memory of the cluster's first CTA, which finds the budget-th largest digit by digit (8 bits, from the highest bit in which keys differ; rarely more than two rounds) and writes the columns down in order.  Tables
 // too wide for one CTA's shared memory (40960 columns) leave the keys where they are: the CTAs add their histograms through distributed shared memory.
-// Bound: the chain length -> page -> bounds -> meeting -> digits, 8 us (10.3 for a row of 8 heads and 2048 pages); for many rows the bytes of the bounds (2 d + 4 a page and KV head: 64 rows over 512 pages 22.5 us, 68 MB; with two CTAs of 512
-// threads an SM 27.8).
+// Bound: the chain length -> page -> bounds -> meeting -> digits, 8 us (10.3 for a row of 8 heads and 2048 pages).  For many rows latency still, with 35 % of the warps active: 64 rows over 512 pages take 22.5 us for 68 MB of bounds, 0.46 of the copy rate (with two CTAs of 512
+// threads an SM 27.8); 32 ragged rows use 33 % of the issue slots and 12 % of DRAM.
 template <int D>
 __global__ void __launch_bounds__(kSelectThreads, 4) paged_select_kernel(const PagedSelectParams p)
 {

@@ -139,6 +139,8 @@ struct SharedPlan {
 // own), few rows cost by their blocks of 16 tokens and 8 rows, tiles by their steps of 64 tokens.  us, plain, few rows and tiles, 8 KV heads of 128 and 4 queries each: 4 sequences over 1024 tokens 11.5, 14.9, 30.9; 16 over 2048 19.8, 20.5, 33.1;
 // 8 over 16384 41.0, 30.4, 43.4; 16 over 16384 71.5, 47.3, 44.5; two groups of 32 over 16384 259, 149, 75; 16 drafted tokens each, 4 over 16384 81.9, -, 43.6.  4 of 256 and 2: 4 over 16384 25.6, 18.4, 37.7; two groups of 32 257, 87, 61.
 // 2 of 64 and 7: 8 over 16384 15.4, 18.4, 32.2; two groups of 32 50, 51, 39.  What the estimate does not know is how long the beginnings are: 64 sequences of 2000 tokens of their own over 512 take 58.6 by its choice and 54.5 plain.
+// Nor how long the sequences are, where the table is wider: with 131072 tokens of columns and three quarters of every sequence shared, by its choice and plain, 8 KV heads and 4 queries each: 4 of 1000 16.5, 12.7; 32 of 1000 40.7, 22.6; 32 of 8000
+// 59.5, 73.8; 32 of 30000 123, 236.  1 of 128 and 12: 32 of 1000 40.9, 14.7; 32 of 8000 45.1, 28.7; 32 of 30000 59.9, 67.7.
 void shared_route(qlinear_paged_t h, int32_t B, int32_t T, int32_t max_q, int32_t n_groups, int32_t table_width, SharedPlan* a)
 {
     const int32_t d = h->d.d_h, V = n_groups + B, choice = paged_shared_choice();
